@@ -340,6 +340,30 @@ typedef struct {
 int cf_attn_calls(const cf_attn_call *calls, int64_t n, void *hip_stream);
 
 /*
+ * The same attention with a sliding window and sinks: query i of a segment, at position p = i + (Lk_g - Lq_g), sees key j iff
+ * j <= p and (j > p - window or j < n_sinks): its last `window` keys, itself among them, and the segment's first n_sinks keys.  A
+ * window of Lk_g or more is no window.  Positions are those of the whole sequence, as with the causal mask, so a slice behind a
+ * retained prefix reads of it what its rows see and leaves the rest of k, v, d_k and d_v untouched.
+ *   window   >= 1        n_sinks  >= 0
+ * cf_attn_window_fwd / cf_attn_window_bwd take the arguments of cf_attn_fwd / cf_attn_bwd (layouts, flags, q_tiles, dK/dV that are added
+ * to) and give their results and errors; window < 1, n_sinks < 0 or a NULL window -> CF_EINVAL.  Workspace: at least
+ * cf_attn_window_bwd_workspace_bytes(&f, w) bytes.
+ * Infinities and NaNs in an input reach only the rows that see it, whatever dtype and head_dim.
+ * Bitwise reproducible, except dK/dV in bf16, where workgroups that share a key tile meet in fp32 atomic adds;
+ * CF_FLAG_DKV_SINGLE_WRITER leaves every key tile to one workgroup (a segment's sinks are seen by all its rows: long slices then wait
+ * for that one).
+ * cf_count_window_pairs: cf_count_pairs for this mask.
+ */
+typedef struct {
+    int32_t window, n_sinks;
+} cf_attn_window;
+int cf_attn_window_fwd(const cf_attn_fwd_params *p, const cf_attn_window *w, void *hip_stream);
+int64_t cf_attn_window_bwd_workspace_bytes(const cf_attn_fwd_params *p, const cf_attn_window *w);
+int cf_attn_window_bwd(const cf_attn_bwd_params *p, const cf_attn_window *w, void *hip_stream);
+int64_t cf_count_window_pairs(const int32_t *cu_seqlens_q_host, const int32_t *cu_seqlens_k_host, int32_t n_segments,
+                              const cf_attn_window *w);
+
+/*
  * Measurement aid (not part of the paper's method): when both events (hipEvent_t, created by the
  * caller with timing enabled) are non-NULL, the NEXT cf_attn_fwd / cf_attn_bwd call on this thread
  * records `start` right before and `stop` right after its main kernel (forward: the attention

@@ -21,7 +21,7 @@ CF_PLAN_MERGE_TAILS = 1
 
 EXPORTS = ["cf_last_error", "cf_version", "cf_build_chunks", "cf_build_chunks_ex", "cf_attn_q_tiles", "cf_plan_free", "cf_plan_get",
            "cf_build_schedule", "cf_schedule_stats", "cf_attn_fwd", "cf_attn_bwd_workspace_bytes", "cf_attn_bwd", "cf_attn_fwd_batch", "cf_attn_bwd_batch",
-           "cf_attn_calls", "cf_count_pairs", "cf_profile_next_call", "cf_attn_bwd_static", "cf_sim_1f1b", "cf_sim_1f1b_sequences"]
+           "cf_attn_calls", "cf_attn_window_fwd", "cf_attn_window_bwd", "cf_attn_window_bwd_workspace_bytes", "cf_count_window_pairs", "cf_count_pairs", "cf_profile_next_call", "cf_attn_bwd_static", "cf_sim_1f1b", "cf_sim_1f1b_sequences"]
 
 
 class CfError(RuntimeError):
@@ -78,6 +78,10 @@ class AttnCall(C.Structure):
     _fields_ = [("params", C.c_void_p), ("backward", C.c_int32), ("reserved", C.c_int32)]
 
 
+class AttnWindow(C.Structure):
+    _fields_ = [("window", C.c_int32), ("n_sinks", C.c_int32)]
+
+
 _lib = None
 
 
@@ -107,6 +111,12 @@ def lib():
         L.cf_attn_fwd_batch.argtypes = [C.POINTER(AttnFwdParams), C.c_int32, C.c_void_p]
         L.cf_attn_bwd_batch.argtypes = [C.POINTER(AttnBwdParams), C.c_int32, C.c_void_p]
         L.cf_attn_calls.argtypes = [C.POINTER(AttnCall), C.c_int64, C.c_void_p]
+        L.cf_attn_window_fwd.argtypes = [C.POINTER(AttnFwdParams), C.POINTER(AttnWindow), C.c_void_p]
+        L.cf_attn_window_bwd.argtypes = [C.POINTER(AttnBwdParams), C.POINTER(AttnWindow), C.c_void_p]
+        L.cf_attn_window_bwd_workspace_bytes.argtypes = [C.POINTER(AttnFwdParams), C.POINTER(AttnWindow)]
+        L.cf_attn_window_bwd_workspace_bytes.restype = C.c_int64
+        L.cf_count_window_pairs.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(AttnWindow)]
+        L.cf_count_window_pairs.restype = C.c_int64
         L.cf_schedule_stats.argtypes = [C.c_void_p, C.c_int32, C.POINTER(SchedStats)]
         L.cf_profile_next_call.argtypes = [C.c_void_p, C.c_void_p]
         L.cf_count_pairs.argtypes = [C.c_void_p, C.c_void_p, C.c_int32]
@@ -226,6 +236,12 @@ def cf_count_pairs(cu_q, cu_k):
     a = np.ascontiguousarray(cu_q, dtype=np.int32)
     b = np.ascontiguousarray(cu_k, dtype=np.int32)
     return _check(lib().cf_count_pairs(a.ctypes.data_as(C.c_void_p), b.ctypes.data_as(C.c_void_p), len(a) - 1))
+
+
+def cf_count_window_pairs(cu_q, cu_k, window, n_sinks=0):
+    a = np.ascontiguousarray(cu_q, dtype=np.int32)
+    b = np.ascontiguousarray(cu_k, dtype=np.int32)
+    return _check(lib().cf_count_window_pairs(a.ctypes.data_as(C.c_void_p), b.ctypes.data_as(C.c_void_p), len(a) - 1, _window(window, n_sinks)))
 
 
 def cf_profile_next_call(start_event, stop_event):
@@ -365,3 +381,20 @@ def cf_attn_bwd(params, stream=None):
 
 def cf_attn_bwd_static(params, stream=None):
     _check(lib().cf_attn_bwd_static(C.byref(params), stream if stream is not None else _stream()))
+
+
+def _window(window, n_sinks):
+    return C.byref(AttnWindow(int(window), int(n_sinks)))
+
+
+def cf_attn_window_fwd(params, window, n_sinks=0, stream=None):
+    """cf_attn_fwd's call with a sliding window: a query sees its last `window` keys and its sequence's first n_sinks."""
+    _check(lib().cf_attn_window_fwd(C.byref(params), _window(window, n_sinks), stream if stream is not None else _stream()))
+
+
+def cf_attn_window_bwd_workspace_bytes(params, window, n_sinks=0):
+    return _check(lib().cf_attn_window_bwd_workspace_bytes(C.byref(params), _window(window, n_sinks)))
+
+
+def cf_attn_window_bwd(params, window, n_sinks=0, stream=None):
+    _check(lib().cf_attn_window_bwd(C.byref(params), _window(window, n_sinks), stream if stream is not None else _stream()))

@@ -508,3 +508,53 @@ extern "C" int cf_attn_calls(const cf_attn_call *calls, int64_t n, void *hip_str
     }
     return CF_OK;
 }
+
+// ---- a window and sinks -----------------------------------------------------------------------------------------
+namespace {
+
+// The window of a call, cut to its keys (a longer one hides nothing).
+int check_window(const cf_attn_window *w, int32_t n_kv_tokens, const char *who, cf::WindowMask *mask)
+{
+    if (!w) return cf::fail(CF_EINVAL, "%s: window is NULL", who);
+    if (w->window < 1 || w->n_sinks < 0)
+        return cf::fail(CF_EINVAL, "%s: need window >= 1 and n_sinks >= 0 (got %d, %d)", who, w->window, w->n_sinks);
+    *mask = {std::min(w->window, n_kv_tokens), std::min(w->n_sinks, n_kv_tokens)};
+    return CF_OK;
+}
+
+}  // namespace
+
+extern "C" int cf_attn_window_fwd(const cf_attn_fwd_params *p, const cf_attn_window *w, void *hip_stream)
+{
+    const char *who = "cf_attn_window_fwd";
+    cf::WindowMask mask;
+    if (int rc = check_fwd(p, who, false)) return rc;
+    if (int rc = check_window(w, p->n_kv_tokens, who, &mask)) return rc;
+    const hipError_t e = cf::launch_window_simple_fwd(*p, mask, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? CF_OK : hip_fail(who, e);
+}
+
+extern "C" int64_t cf_attn_window_bwd_workspace_bytes(const cf_attn_fwd_params *p, const cf_attn_window *w)
+{
+    const char *who = "cf_attn_window_bwd_workspace_bytes";
+    cf::WindowMask mask;
+    if (int rc = check_fwd(p, who, true)) return rc;
+    if (p->flags & ~kKnownFlags) return cf::fail(CF_EINVAL, "%s: unknown flags 0x%x", who, p->flags);
+    if (int rc = check_window(w, p->n_kv_tokens, who, &mask)) return rc;
+    return delta_bytes(*p);
+}
+
+extern "C" int cf_attn_window_bwd(const cf_attn_bwd_params *b, const cf_attn_window *w, void *hip_stream)
+{
+    const char *who = "cf_attn_window_bwd";
+    cf::WindowMask mask;
+    if (int rc = check_bwd_tensors(b, who)) return rc;
+    if (int rc = check_window(w, b->f.n_kv_tokens, who, &mask)) return rc;
+    const int64_t need = delta_bytes(b->f);
+    if (!b->workspace || !aligned(b->workspace, 256)) return cf::fail(CF_EINVAL, "%s: workspace must be non-NULL and 256-byte aligned", who);
+    if (b->workspace_bytes < need)
+        return cf::fail(CF_EINVAL, "%s: workspace has %lld bytes, %lld needed", who, (long long)b->workspace_bytes, (long long)need);
+    const cf::BwdWorkspace ws = {static_cast<float *>(b->workspace), nullptr, 0};
+    const hipError_t e = cf::launch_window_simple_bwd(*b, ws, mask, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? CF_OK : hip_fail(who, e);
+}

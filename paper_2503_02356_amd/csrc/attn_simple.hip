@@ -17,27 +17,6 @@ namespace {
 
 constexpr int kWaves = kScalarWaves;  // wavefronts per workgroup
 
-// Largest g in [0, n) with cu[g] <= row  (cu non-decreasing, cu[0] = 0, zero-length segments skipped).
-__device__ inline int find_segment(const int32_t *cu, int n, int row)
-{
-    int lo = 0, hi = n;  // invariant: cu[lo] <= row < cu[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (cu[mid] <= row) lo = mid; else hi = mid;
-    }
-    return lo;
-}
-
-__device__ inline SegmentRows segment_rows(const cf_attn_fwd_params &p, int g)
-{
-    const int q0 = p.cu_seqlens_q[g], k0 = p.cu_seqlens_k[g];
-    return {q0, p.cu_seqlens_q[g + 1] - q0, k0, p.cu_seqlens_k[g + 1] - k0};
-}
-__device__ inline SegmentRows segment_of_query(const cf_attn_fwd_params &p, int row)
-{
-    return segment_rows(p, find_segment(p.cu_seqlens_q, p.n_segments, row));
-}
-
 template <typename T, int D>
 __global__ __launch_bounds__(kWaves * 64) void simple_fwd_kernel(cf_attn_fwd_params p)
 {

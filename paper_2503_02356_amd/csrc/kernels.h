@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "chunkflow.h"
+#include "mask.h"
 
 namespace cf {
 
@@ -190,6 +191,10 @@ hipError_t launch_simple_bwd(const cf_attn_bwd_params &p, const BwdWorkspace &ws
 
 // delta[h][t] = sum_d dO[t][h][d] * O[t][h][d].
 hipError_t launch_delta(const cf_attn_bwd_params &p, const BwdWorkspace &ws, hipStream_t s);
+
+// The same with a window and sinks (attn_window.hip).
+hipError_t launch_window_simple_fwd(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s);
+hipError_t launch_window_simple_bwd(const cf_attn_bwd_params &b, const BwdWorkspace &ws, const WindowMask &mask, hipStream_t s);
 
 // head_dim 128, forward and dQ: 32x32x16 MFMAs instead of 16x16x32 (mfma_common.h)?  A launch that fills the chip is limited by power and
 // gains 2-7 % from the smaller ones.  On a chip that is mostly empty a wavefront is alone on its SIMD, and the time to issue twice as many

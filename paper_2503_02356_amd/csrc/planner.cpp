@@ -557,6 +557,27 @@ extern "C" int64_t cf_count_pairs(const int32_t *cu_q, const int32_t *cu_k, int3
     return pairs;
 }
 
+extern "C" int64_t cf_count_window_pairs(const int32_t *cu_q, const int32_t *cu_k, int32_t n_segments, const cf_attn_window *w)
+{
+    const char *who = "cf_count_window_pairs";
+    if (!cu_q || !cu_k || n_segments < 0 || !w) return cf::fail(CF_EINVAL, "%s: bad argument", who);
+    if (w->window < 1 || w->n_sinks < 0)
+        return cf::fail(CF_EINVAL, "%s: need window >= 1 and n_sinks >= 0 (got %d, %d)", who, w->window, w->n_sinks);
+    int64_t pairs = 0;
+    for (int32_t g = 0; g < n_segments; ++g) {
+        const int64_t lq = cu_q[g + 1] - cu_q[g], lk = cu_k[g + 1] - cu_k[g], off = lk - lq, W = w->window, S = w->n_sinks;
+        if (lq < 0 || off < 0) return cf::fail(CF_EINVAL, "%s: segment %d has Lq=%lld Lk=%lld", who, g, (long long)lq, (long long)lk);
+        // rows whose position is below x, and the sum of position - x + 1 over the others: what lies before a window or before that and the sinks
+        auto beyond = [&](int64_t x) {
+            const int64_t first = std::min(lk, std::max(off, x)), n = lk - first;
+            return n * (first - x + 1) + n * (n - 1) / 2;
+        };
+        // all keys up to a row's own, without those before its window, and of these the sinks again
+        pairs += lq * off + lq * (lq + 1) / 2 - beyond(W) + (beyond(W) - beyond(W + S));
+    }
+    return pairs;
+}
+
 extern "C" int64_t cf_attn_q_tiles(const int32_t *cu_q, const int32_t *cu_k, int32_t n_segments, cf_q_tile *out,
                                    int64_t capacity)
 {

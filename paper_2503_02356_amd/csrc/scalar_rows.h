@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include "chunkflow.h"
+#include "mask.h"
 
 namespace cf {
 
@@ -55,12 +56,34 @@ __device__ inline const T *row_of(const void *base, int row, int64_t stride_tok,
     return (const T *)base + (int64_t)row * stride_tok + (int64_t)head * stride_head;
 }
 
+// Largest g in [0, n) with cu[g] <= row  (cu non-decreasing, cu[0] = 0, zero-length segments skipped).
+__device__ inline int find_segment(const int32_t *cu, int n, int row)
+{
+    int lo = 0, hi = n;  // invariant: cu[lo] <= row < cu[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (cu[mid] <= row) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__device__ inline SegmentRows segment_rows(const cf_attn_fwd_params &p, int g)
+{
+    const int q0 = p.cu_seqlens_q[g], k0 = p.cu_seqlens_k[g];
+    return {q0, p.cu_seqlens_q[g + 1] - q0, k0, p.cu_seqlens_k[g + 1] - k0};
+}
+__device__ inline SegmentRows segment_of_query(const cf_attn_fwd_params &p, int row)
+{
+    return segment_rows(p, find_segment(p.cu_seqlens_q, p.n_segments, row));
+}
+
 // O and LSE of query row `row` of head h.
-template <typename T, int D, int UNROLL, typename Q>
-__device__ inline void scalar_fwd_row(const cf_attn_fwd_params &p, const SegmentRows &g, int row, int h, Q q)
+template <typename T, int D, int UNROLL, typename Q, typename Mask = CausalMask>
+__device__ inline void scalar_fwd_row(const cf_attn_fwd_params &p, const SegmentRows &g, int row, int h, Q q, const Mask &mask = Mask())
 {
     const int lane = threadIdx.x & 63, kh = h / (p.n_q_heads / p.n_kv_heads);
-    const int n_vis = g.lk - g.lq + (row - g.q0) + 1;
+    const KeysOfRow<Mask> keys(mask, g.lk - g.lq + (row - g.q0));
+    const int n_vis = keys.n;
     const T *kb = (const T *)p.k + (int64_t)kh * p.kv_stride_head;
     const T *vb = (const T *)p.v + (int64_t)kh * p.kv_stride_head;
     constexpr int DPL = D / 64;
@@ -70,7 +93,7 @@ __device__ inline void scalar_fwd_row(const cf_attn_fwd_params &p, const Segment
         const int j = j0 + lane;
         float s = -INFINITY;
         if (j < n_vis) {
-            const T *kj = kb + (int64_t)(g.k0 + j) * p.kv_stride_tok;
+            const T *kj = kb + (int64_t)(g.k0 + keys.key(j)) * p.kv_stride_tok;
             float d = 0.f;
             for_elements<D, UNROLL>([&](int x) { d += q(x) * ld(kj + x); });
             s = d * p.softmax_scale;
@@ -83,7 +106,7 @@ __device__ inline void scalar_fwd_row(const cf_attn_fwd_params &p, const Segment
         const int cnt = min(64, n_vis - j0);
         for (int jj = 0; jj < cnt; ++jj) {
             const float pj = __shfl(pr, jj);
-            const T *vj = vb + (int64_t)(g.k0 + j0 + jj) * p.kv_stride_tok;
+            const T *vj = vb + (int64_t)(g.k0 + keys.key(j0 + jj)) * p.kv_stride_tok;
             for (int t = 0; t < DPL; ++t) acc[t] += pj * ld(vj + lane + 64 * t);
         }
         m = m_new;
@@ -95,12 +118,13 @@ __device__ inline void scalar_fwd_row(const cf_attn_fwd_params &p, const Segment
 }
 
 // dQ of query row `row` of head h.
-template <typename T, int D, int UNROLL, typename B, typename Q, typename DO>
-__device__ inline void scalar_dq_row(const B &b, const SegmentRows &g, int row, int h, Q q, DO d_o, float delta)
+template <typename T, int D, int UNROLL, typename B, typename Q, typename DO, typename Mask = CausalMask>
+__device__ inline void scalar_dq_row(const B &b, const SegmentRows &g, int row, int h, Q q, DO d_o, float delta, const Mask &mask = Mask())
 {
     const auto &p = b.f;
     const int lane = threadIdx.x & 63, kh = h / (p.n_q_heads / p.n_kv_heads);
-    const int n_vis = g.lk - g.lq + (row - g.q0) + 1;
+    const KeysOfRow<Mask> keys(mask, g.lk - g.lq + (row - g.q0));
+    const int n_vis = keys.n;
     const T *kb = (const T *)p.k + (int64_t)kh * p.kv_stride_head;
     const T *vb = (const T *)p.v + (int64_t)kh * p.kv_stride_head;
     constexpr int DPL = D / 64;
@@ -111,8 +135,8 @@ __device__ inline void scalar_dq_row(const B &b, const SegmentRows &g, int row, 
         const int j = j0 + lane;
         float ds = 0.f;
         if (j < n_vis) {
-            const T *kj = kb + (int64_t)(g.k0 + j) * p.kv_stride_tok;
-            const T *vj = vb + (int64_t)(g.k0 + j) * p.kv_stride_tok;
+            const T *kj = kb + (int64_t)(g.k0 + keys.key(j)) * p.kv_stride_tok;
+            const T *vj = vb + (int64_t)(g.k0 + keys.key(j)) * p.kv_stride_tok;
             float s = 0.f, dp = 0.f;
             for_elements<D, UNROLL>([&](int x) {
                 s += q(x) * ld(kj + x);
@@ -123,7 +147,7 @@ __device__ inline void scalar_dq_row(const B &b, const SegmentRows &g, int row, 
         const int cnt = min(64, n_vis - j0);
         for (int jj = 0; jj < cnt; ++jj) {
             const float dj = __shfl(ds, jj);
-            const T *kj = kb + (int64_t)(g.k0 + j0 + jj) * p.kv_stride_tok;
+            const T *kj = kb + (int64_t)(g.k0 + keys.key(j0 + jj)) * p.kv_stride_tok;
             for (int t = 0; t < DPL; ++t) acc[t] += dj * ld(kj + lane + 64 * t);
         }
     }
@@ -133,23 +157,24 @@ __device__ inline void scalar_dq_row(const B &b, const SegmentRows &g, int row, 
 
 // What all query heads of key/value head kh add to dK and dV of key row `krow` (element lane + 64 t; dK without the scale).
 // delta(row, h): of a query row.
-template <typename T, int D, int UNROLL, typename B, typename K, typename V, typename Delta>
+template <typename T, int D, int UNROLL, typename B, typename K, typename V, typename Delta, typename Mask = CausalMask>
 __device__ inline void scalar_dkv_row(const B &b, const SegmentRows &g, int krow, int kh, K k, V v, Delta delta,
-                                      float (&dk)[D / 64], float (&dv)[D / 64])
+                                      float (&dk)[D / 64], float (&dv)[D / 64], const Mask &mask = Mask())
 {
     const auto &p = b.f;
     const int lane = threadIdx.x & 63, G = p.n_q_heads / p.n_kv_heads;
     const int j = krow - g.k0, prefix = g.lk - g.lq;
     const int i_first = j > prefix ? j - prefix : 0;  // first query row that sees this key
+    const int i_end = rows_that_see(mask, j, prefix, g.lq);
     constexpr int DPL = D / 64;
     for (int t = 0; t < DPL; ++t) dk[t] = dv[t] = 0.f;
     for (int h = kh * G; h < (kh + 1) * G; ++h) {
         const T *qb = (const T *)p.q + (int64_t)h * p.q_stride_head;
         const T *dob = (const T *)b.d_o + (int64_t)h * b.do_stride_head;
-        for (int i0 = i_first; i0 < g.lq; i0 += 64) {
+        for (int i0 = i_first; i0 < i_end; i0 += 64) {
             const int i = i0 + lane;
             float pr = 0.f, ds = 0.f;
-            if (i < g.lq) {
+            if (i < i_end) {
                 const T *qi = qb + (int64_t)(g.q0 + i) * p.q_stride_tok;
                 const T *doi = dob + (int64_t)(g.q0 + i) * b.do_stride_tok;
                 float s = 0.f, dp = 0.f;
@@ -160,7 +185,7 @@ __device__ inline void scalar_dkv_row(const B &b, const SegmentRows &g, int krow
                 pr = expf(s * p.softmax_scale - p.lse[(int64_t)h * p.n_tokens + g.q0 + i]);
                 ds = pr * (dp - delta(g.q0 + i, h));
             }
-            const int cnt = min(64, g.lq - i0);
+            const int cnt = min(64, i_end - i0);
             for (int ii = 0; ii < cnt; ++ii) {
                 const float pi = __shfl(pr, ii), di = __shfl(ds, ii);
                 const T *qi = qb + (int64_t)(g.q0 + i0 + ii) * p.q_stride_tok;
@@ -175,11 +200,12 @@ __device__ inline void scalar_dkv_row(const B &b, const SegmentRows &g, int krow
 }
 
 // delta of a query row, formed by each lane for itself: <dO, O>, and for rows that see at most 64 keys sum_j P_j <dO, v_j>.
-template <typename T, int D, typename B>
-__device__ inline float scalar_delta(const B &b, const SegmentRows &g, int row, int h)
+template <typename T, int D, typename B, typename Mask = CausalMask>
+__device__ inline float scalar_delta(const B &b, const SegmentRows &g, int row, int h, const Mask &mask = Mask())
 {
     const auto &p = b.f;
-    const int n_vis = g.lk - g.lq + (row - g.q0) + 1, kh = h / (p.n_q_heads / p.n_kv_heads);
+    const KeysOfRow<Mask> keys(mask, g.lk - g.lq + (row - g.q0));
+    const int n_vis = keys.n, kh = h / (p.n_q_heads / p.n_kv_heads);
     const T *d_o = row_of<T>(b.d_o, row, b.do_stride_tok, h, b.do_stride_head);
     float sum = 0.f;
     if (n_vis > 64) {
@@ -191,8 +217,8 @@ __device__ inline float scalar_delta(const B &b, const SegmentRows &g, int row, 
     const T *q = row_of<T>(p.q, row, p.q_stride_tok, h, p.q_stride_head);
     const float lse = p.lse[(int64_t)h * p.n_tokens + row];
     for (int j = 0; j < n_vis; ++j) {
-        const T *k = row_of<T>(p.k, g.k0 + j, p.kv_stride_tok, kh, p.kv_stride_head);
-        const T *v = row_of<T>(p.v, g.k0 + j, p.kv_stride_tok, kh, p.kv_stride_head);
+        const T *k = row_of<T>(p.k, g.k0 + keys.key(j), p.kv_stride_tok, kh, p.kv_stride_head);
+        const T *v = row_of<T>(p.v, g.k0 + keys.key(j), p.kv_stride_tok, kh, p.kv_stride_head);
         float s = 0.f, dp = 0.f;
 #pragma unroll 4
         for (int x = 0; x < D; ++x) {
