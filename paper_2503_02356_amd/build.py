@@ -37,7 +37,7 @@ def spilled_accumulators(report):
     """Kernels of a compiler resource report that update accumulators in place behind the compiler's back (the dK/dV kernels
     at head_dim 128; mfma_common.h, accumulate_in_place) and spill: a spilled accumulator would be stored while its last
     MFMA is still running.  -> [(kernel, what)]"""
-    return [(k, f"{what}: {n}") for k, what, n in _resources(report) if "mfma_dkv" in k and "ILi128E" in k and n != 0]
+    return [(k, f"{what}: {n}") for k, what, n in _resources(report) if re.search("mfma_(window_)?dkv", k) and "ILi128E" in k and n != 0]
 
 
 def spilled_operands(report):

@@ -197,8 +197,12 @@ __device__ __forceinline__ void for_rows_of(unsigned long long lanes, Visit visi
 }
 __device__ __forceinline__ bool finite(const f32x4 &x) { return cf::finite((x[0] + x[1]) + (x[2] + x[3])); }
 
-template <int D>
-__device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id)
+// Key blocks that no row sees for their windows are passed over; a block's pairs outside them are masked as those above the diagonal are.
+__device__ __forceinline__ bool out_of_window(const CausalMask &, int, int) { return false; }
+__device__ __forceinline__ bool out_of_window(const WindowMask &m, int position, int key) { return key <= position - m.window && key >= m.sinks; }
+
+template <int D, typename Mask>
+__device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id, const Mask &mask)
 {
     using S = Shape<D>;
     __shared__ f32x4 qs[S::J * 64];
@@ -209,7 +213,9 @@ __device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id
     TileLocation loc;
     if (!locate_tile(p.cu_seqlens_q, p.cu_seqlens_k, p.n_segments, p.n_tokens, RB, id / p.n_q_heads, loc)) return;
     const int lq = uniform(loc.len), lk = uniform(loc.other_len), off = lk - lq, q0 = uniform(loc.tile_in_seg) * RB;
-    const int rows = min(RB, lq - q0), n_kb = (q0 + rows + off + RB - 1) / RB;
+    const int rows = min(RB, lq - q0);
+    const KeyTiles<RB, Mask> key_blocks(mask, q0 + off, q0 + rows + off);
+    const int n_kb = key_blocks.n;
     const float *q = (const float *)p.q + (int64_t)loc.begin * p.q_stride_tok + (int64_t)h * p.q_stride_head;
     const float *k = (const float *)p.k + (int64_t)loc.other_begin * p.kv_stride_tok + (int64_t)kh * p.kv_stride_head;
     const float *v = (const float *)p.v + (int64_t)loc.other_begin * p.kv_stride_tok + (int64_t)kh * p.kv_stride_head;
@@ -218,7 +224,7 @@ __device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id
     const int amax = q0 + col + off;                 // last visible key of this lane's row
 
     f32x4 kf[S::J];
-    if (wave < n_kb) load_row<D>(k + (int64_t)min(wave * RB + col, lk - 1) * p.kv_stride_tok, quarter, kf);
+    if (wave < n_kb) load_row<D>(k + (int64_t)min(key_blocks.start(wave) + col, lk - 1) * p.kv_stride_tok, quarter, kf);
     stage_rows<D>(q, p.q_stride_tok, q0, lq - 1, qs);
     __syncthreads();
 
@@ -227,18 +233,19 @@ __device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id
     for (int x = 0; x < D / 16; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
     for (int kb = wave; kb < n_kb; kb += NW) {
+        const int k0 = key_blocks.start(kb);
         f32x4 x[4][S::NC];
-        auto load_v = [&] { load_columns<D>(v + (int64_t)(kb * RB) * p.kv_stride_tok, kv_row_bytes, lk - 1 - kb * RB, lane, x); };
+        auto load_v = [&] { load_columns<D>(v + (int64_t)k0 * p.kv_stride_tok, kv_row_bytes, lk - 1 - k0, lane, x); };
         if (D == 64) load_v();
         f32x4 s = row_product<D>(kf, qs, lane);
         if (D != 64) {
             __builtin_amdgcn_sched_barrier(0);       // V takes the registers of K: with both held D = 128 spills
             load_v();
         }
-        if (kb + NW < n_kb) load_row<D>(k + (int64_t)min((kb + NW) * RB + col, lk - 1) * p.kv_stride_tok, quarter, kf);
-        const int lim = amax - kb * RB - 4 * quarter;    // key 4 * quarter + i of the block is masked iff i > lim
+        if (kb + NW < n_kb) load_row<D>(k + (int64_t)min(key_blocks.start(kb + NW) + col, lk - 1) * p.kv_stride_tok, quarter, kf);
+        const int lim = amax - k0 - 4 * quarter;         // key 4 * quarter + i of the block is masked iff i > lim
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = i > lim ? -INFINITY : s[i] * c2;
+        for (int i = 0; i < 4; ++i) s[i] = i > lim || out_of_window(mask, amax, k0 + 4 * quarter + i) ? -INFINITY : s[i] * c2;
         const float m_new = fmaxf(m, max_over_quarters(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))));
         const float ref = m_new == -INFINITY ? 0.f : m_new;     // no visible key yet: every exponential is 0
         const float alpha = __builtin_amdgcn_exp2f(m - ref);
@@ -264,6 +271,7 @@ __device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id
     if (r < rows) {
         float M = m_s[0][r], L = 0.f;
         for (int w = 1; w < n; ++w) M = fmaxf(M, m_s[w][r]);
+        // (windowed: a wavefront may have had no key of the row; the row itself sees one, so that M is finite unless a score is not)
         f32x4 a = {0.f, 0.f, 0.f, 0.f};
         for (int w = 0; w < n; ++w) {
             const float g = __builtin_amdgcn_exp2f(m_s[w][r] - M);
@@ -278,12 +286,14 @@ __device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id
     for_rows_of<D>(__ballot(bad), [&](int first) {
         const int row = q0 + (wave * 64 + first) / (D / 4);
         const float *qr = q + (int64_t)row * p.q_stride_tok;
-        scalar_fwd_row<float, D, 4>(p, SegmentRows{loc.begin, lq, loc.other_begin, lk}, loc.begin + row, h, [&](int x) { return qr[x]; });
+        scalar_fwd_row<float, D, 4>(p, SegmentRows{loc.begin, lq, loc.other_begin, lk}, loc.begin + row, h, [&](int x) { return qr[x]; }, mask);
     });
 }
 
 template <int D>
-__global__ __launch_bounds__(NW * 64) void f32_fwd_kernel(cf_attn_fwd_params p) { f32_fwd_body<D>(p, blockIdx.x); }
+__global__ __launch_bounds__(NW * 64) void f32_fwd_kernel(cf_attn_fwd_params p) { f32_fwd_body<D>(p, blockIdx.x, CausalMask()); }
+template <int D>
+__global__ __launch_bounds__(NW * 64) void f32_window_fwd_kernel(cf_attn_fwd_params p, WindowMask mask) { f32_fwd_body<D>(p, blockIdx.x, mask); }
 
 // Several chunks in one launch; of a chunk's workgroups the first dkv_blocks[c] belong to its key rows and those of the chunks chained behind
 // it.
@@ -310,7 +320,7 @@ __global__ __launch_bounds__(NW * 64) void f32_fwd_batch_kernel(FwdBatch q)
 {
     int id = blockIdx.x;
     const int c = q.blocks.chunk_of(id);
-    f32_fwd_body<D>(q.p[c], id);
+    f32_fwd_body<D>(q.p[c], id, CausalMask());
 }
 
 // exp(s scale - lse).  The scores keep their natural units, in which LSE is exact, and the rounding of the product with log2e
@@ -323,8 +333,8 @@ __device__ __forceinline__ float probability(float s, float scale, float lse)
 }
 
 // dQ of 16 query rows of one head.
-template <int D>
-__device__ __forceinline__ void f32_dq_body(const BwdArgs &b, int id, char *smem)
+template <int D, typename Mask>
+__device__ __forceinline__ void f32_dq_body(const BwdArgs &b, int id, char *smem, const Mask &mask)
 {
     using S = Shape<D>;
     const BwdArgs::Fwd &p = b.f;
@@ -336,7 +346,9 @@ __device__ __forceinline__ void f32_dq_body(const BwdArgs &b, int id, char *smem
     TileLocation loc;
     if (!locate_tile(p.cu_seqlens_q, p.cu_seqlens_k, p.n_segments, p.n_tokens, RB, id / p.n_q_heads, loc)) return;
     const int lq = uniform(loc.len), lk = uniform(loc.other_len), off = lk - lq, q0 = uniform(loc.tile_in_seg) * RB;
-    const int rows = min(RB, lq - q0), n_kb = (q0 + rows + off + RB - 1) / RB;
+    const int rows = min(RB, lq - q0);
+    const KeyTiles<RB, Mask> key_blocks(mask, q0 + off, q0 + rows + off);
+    const int n_kb = key_blocks.n;
     const float *k = (const float *)p.k + (int64_t)loc.other_begin * p.kv_stride_tok + (int64_t)kh * p.kv_stride_head;
     const float *v = (const float *)p.v + (int64_t)loc.other_begin * p.kv_stride_tok + (int64_t)kh * p.kv_stride_head;
     const float *d_o = (const float *)b.d_o + (int64_t)loc.begin * b.do_stride_tok + (int64_t)h * b.do_stride_head;
@@ -364,15 +376,15 @@ __device__ __forceinline__ void f32_dq_body(const BwdArgs &b, int id, char *smem
         __shared__ float sums[kExactDeltaKeys / RB][RB];
         float sum = 0.f;
         if (wave < n_kb) {
-            const int row = min(wave * RB + col, lk - 1);
+            const int row = min(key_blocks.start(wave) + col, lk - 1);
             f32x4 f[S::J];
             load_row<D>(k + (int64_t)row * p.kv_stride_tok, quarter, f);
             const f32x4 s = row_product<D>(f, qs, lane);
             load_row<D>(v + (int64_t)row * p.kv_stride_tok, quarter, f);
             const f32x4 dp = row_product<D>(f, dos, lane);
-            const int lim = amax - wave * RB - 4 * quarter;
+            const int lim = amax - key_blocks.start(wave) - 4 * quarter;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum += i > lim ? 0.f : probability(s[i], p.softmax_scale, lse) * dp[i];
+            for (int i = 0; i < 4; ++i) sum += i > lim || out_of_window(mask, amax, key_blocks.start(wave) + 4 * quarter + i) ? 0.f : probability(s[i], p.softmax_scale, lse) * dp[i];
             sum = sum_over_quarters(sum);
             if (quarter == 0) sums[wave][col] = sum;
         }
@@ -390,17 +402,17 @@ __device__ __forceinline__ void f32_dq_body(const BwdArgs &b, int id, char *smem
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) dq[x] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int kb = wave; kb < n_kb; kb += NW) {
-        const int row = min(kb * RB + col, lk - 1);
+        const int k0 = key_blocks.start(kb), row = min(k0 + col, lk - 1);
         f32x4 kf[S::J], vf[S::J];
         load_row<D>(k + (int64_t)row * p.kv_stride_tok, quarter, kf);
         load_row<D>(v + (int64_t)row * p.kv_stride_tok, quarter, vf);
         put_rows<D>(kf, parts + wave * S::PART, lane);
         const f32x4 s = row_product<D>(kf, qs, lane);
         f32x4 dp = row_product<D>(vf, dos, lane);
-        const int lim = amax - kb * RB - 4 * quarter;
+        const int lim = amax - k0 - 4 * quarter;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float pv = i > lim ? 0.f : probability(s[i], p.softmax_scale, lse);
+            const float pv = i > lim || out_of_window(mask, amax, k0 + 4 * quarter + i) ? 0.f : probability(s[i], p.softmax_scale, lse);
             dp[i] = pv * (dp[i] - dlt);
         }
         add_column_product<D>(parts + wave * S::PART, lane, dp, dq);
@@ -419,20 +431,20 @@ __device__ __forceinline__ void f32_dq_body(const BwdArgs &b, int id, char *smem
         const int row = loc.begin + q0 + (wave * 64 + first) / (D / 4);
         const SegmentRows g{loc.begin, lq, loc.other_begin, lk};
         const float *qr = row_of<float>(p.q, row, p.q_stride_tok, h, p.q_stride_head), *dr = row_of<float>(b.d_o, row, b.do_stride_tok, h, b.do_stride_head);
-        scalar_dq_row<float, D, 4>(b, g, row, h, [&](int x) { return qr[x]; }, [&](int x) { return dr[x]; }, scalar_delta<float, D>(b, g, row, h));
+        scalar_dq_row<float, D, 4>(b, g, row, h, [&](int x) { return qr[x]; }, [&](int x) { return dr[x]; }, scalar_delta<float, D>(b, g, row, h, mask), mask);
     });
 }
 
 // dK, dV of 16 key rows of one key/value head: (query head of the group, 16-row query block) pairs dealt over the
 // wavefronts.
-template <int D, bool CHAINS>
-__device__ __forceinline__ void f32_dkv_body(const BwdArgs &b, int id, char *smem, float (*stat)[2 * RB])
+template <int D, bool CHAINS, typename Mask>
+__device__ __forceinline__ void f32_dkv_body(const BwdArgs &b, int id, char *smem, float (*stat)[2 * RB], const Mask &mask)
 {
     using S = Shape<D>;
     // In D = 128's kernel of chains dK/dV fills the 128 registers, and what the compiler keeps of the lane from one use to the next, or over
     // a chain of slices, it makes room for by spilling (26 registers, reloaded in the loop over blocks: 3 packed chunks of 532 tokens, 4 heads,
     // 79 us a step, 71 with none; the 4799 tokens above 791 -> 757).
-    constexpr bool ANEW = CHAINS && D == 128;
+    constexpr bool ANEW = (CHAINS || Mask::windowed) && D == 128;
     const BwdArgs::Fwd &p = b.f;
     f32x4 *ks = (f32x4 *)smem, *vs = (f32x4 *)(smem + S::OPERAND);
     float *parts = (float *)(smem + S::OPERANDS);    // of each wavefront: its block's rows, in the end its results
@@ -443,7 +455,8 @@ __device__ __forceinline__ void f32_dkv_body(const BwdArgs &b, int id, char *sme
     const int lk = uniform(loc.len), lq = uniform(loc.other_len), off = lk - lq;
     // (tiles are numbered from a segment's end; its FIRST key tiles are seen by the most rows: start with those)
     const int k0 = ((lk + RB - 1) / RB - 1 - uniform(loc.tile_in_seg)) * RB, rows = min(RB, lk - k0);
-    const int qb_first = max(0, k0 - off) / RB, n_qb = (lq + RB - 1) / RB - qb_first;
+    const QueryTiles<RB> seen_by(mask, k0, k0 + rows, off, lq);
+    const int qb_first = seen_by.first, n_qb = seen_by.end - qb_first;
     if (n_qb <= 0) return;
     const int n_items = G * n_qb;
     stage_rows<D, ANEW>((const float *)p.k + (int64_t)loc.begin * p.kv_stride_tok + (int64_t)kh * p.kv_stride_head, p.kv_stride_tok, k0, lk - 1, ks);
@@ -490,11 +503,11 @@ __device__ __forceinline__ void f32_dkv_body(const BwdArgs &b, int id, char *sme
         const f32x4 l4 = *(const f32x4 *)(st + 4 * q4);
         f32x4 d4 = *(const f32x4 *)(st + RB + 4 * q4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = lim > i ? 0.f : probability(s[i], p.softmax_scale, l4[i]);
+        for (int i = 0; i < 4; ++i) s[i] = lim > i || out_of_window(mask, q0 + off + 4 * q4 + i, k0 + key) ? 0.f : probability(s[i], p.softmax_scale, l4[i]);
         if (q0 + off == 0) {
             // rows that see this key block and no other: delta = sum_j P_j dP_j (as dQ has it for more rows)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) d4[i] = sum_over_16_lanes(lim > i ? 0.f : s[i] * dp[i]);
+            for (int i = 0; i < 4; ++i) d4[i] = sum_over_16_lanes(lim > i || out_of_window(mask, q0 + off + 4 * q4 + i, k0 + key) ? 0.f : s[i] * dp[i]);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) dp[i] = s[i] * (dp[i] - d4[i]);
@@ -537,7 +550,7 @@ __device__ __forceinline__ void f32_dkv_body(const BwdArgs &b, int id, char *sme
             const float *kr = row_of<float>(p.k, krow, p.kv_stride_tok, kh, p.kv_stride_head), *vr = row_of<float>(p.v, krow, p.kv_stride_tok, kh, p.kv_stride_head);
             float gk[D / 64], gv[D / 64];
             scalar_dkv_row<float, D, 4>(b, g, krow, kh, [&](int x) { return kr[x]; }, [&](int x) { return vr[x]; },
-                                        [&](int row, int h) { return scalar_delta<float, D>(b, g, row, h); }, gk, gv);
+                                        [&](int row, int h) { return scalar_delta<float, D>(b, g, row, h, mask); }, gk, gv, mask);
             float *dst = (is_k ? b.d_k : b.d_v) + (int64_t)krow * b.dkv_stride_tok + (int64_t)kh * b.dkv_stride_head;
 #pragma unroll
             for (int x = 0; x < D / 64; ++x) dst[end_lane + 64 * x] += is_k ? gk[x] * p.softmax_scale : gv[x];
@@ -555,8 +568,17 @@ __global__ __launch_bounds__(NW * 64) void f32_bwd_kernel(BwdArgs b, int dkv_blo
     __shared__ __attribute__((aligned(16))) char smem[BwdLds<D>::bytes];
     __shared__ __attribute__((aligned(16))) float stat[NW][2 * RB];
     const int id = blockIdx.x;
-    if (id < dkv_blocks) f32_dkv_body<D, false>(b, id, smem, stat);
-    else f32_dq_body<D>(b, id - dkv_blocks, smem);
+    if (id < dkv_blocks) f32_dkv_body<D, false>(b, id, smem, stat, CausalMask());
+    else f32_dq_body<D>(b, id - dkv_blocks, smem, CausalMask());
+}
+template <int D>
+__global__ __launch_bounds__(NW * 64) void f32_window_bwd_kernel(BwdArgs b, int dkv_blocks, WindowMask mask)
+{
+    __shared__ __attribute__((aligned(16))) char smem[BwdLds<D>::bytes];
+    __shared__ __attribute__((aligned(16))) float stat[NW][2 * RB];
+    const int id = blockIdx.x;
+    if (id < dkv_blocks) f32_dkv_body<D, false>(b, id, smem, stat, mask);
+    else f32_dq_body<D>(b, id - dkv_blocks, smem, mask);
 }
 // Slices of one sequence add to the same dK/dV rows.  One workgroup adds to 16 of them for all slices of the launch, slice by
 // slice as the calls would, so that a split sequence does not take a launch per slice, each ending with one
@@ -568,11 +590,11 @@ __global__ __launch_bounds__(NW * 64) void f32_bwd_batch_kernel(BwdBatch q)
     __shared__ __attribute__((aligned(16))) float stat[NW][2 * RB];
     int id = blockIdx.x, c = q.blocks.chunk_of(id);
     if (id >= q.dkv_blocks[c]) {
-        f32_dq_body<D>(q.p[c], id - q.dkv_blocks[c], smem);
+        f32_dq_body<D>(q.p[c], id - q.dkv_blocks[c], smem, CausalMask());
         return;
     }
     for (;;) {
-        f32_dkv_body<D, true>(q.p[c], id, smem, stat);
+        f32_dkv_body<D, true>(q.p[c], id, smem, stat, CausalMask());
         c = q.next[c];
         if (c < 0) return;
         __syncthreads();                             // the rows that other wavefronts have written, and LDS
@@ -649,6 +671,25 @@ hipError_t launch_f32_bwd_batch(const cf_attn_bwd_params *const *chunks, int n, 
     const dim3 grid((unsigned)q.blocks.end);
     if (chunks[0]->f.head_dim == 64) f32_bwd_batch_kernel<64><<<grid, NW * 64, 0, s>>>(q);
     else f32_bwd_batch_kernel<128><<<grid, NW * 64, 0, s>>>(q);
+    return hipGetLastError();
+}
+
+hipError_t launch_window_f32_fwd(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s)
+{
+    const int64_t blocks = launch_blocks(p, false);
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks);
+    if (p.head_dim == 64) f32_window_fwd_kernel<64><<<grid, NW * 64, 0, s>>>(p, mask);
+    else f32_window_fwd_kernel<128><<<grid, NW * 64, 0, s>>>(p, mask);
+    return hipGetLastError();
+}
+hipError_t launch_window_f32_bwd(const cf_attn_bwd_params &b, const WindowMask &mask, hipStream_t s)
+{
+    if (launch_blocks(b.f, true) > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    const int dkv = (int)key_blocks(b.f);
+    const dim3 grid((unsigned)launch_blocks(b.f, true));
+    if (b.f.head_dim == 64) f32_window_bwd_kernel<64><<<grid, NW * 64, 0, s>>>(b, dkv, mask);
+    else f32_window_bwd_kernel<128><<<grid, NW * 64, 0, s>>>(b, dkv, mask);
     return hipGetLastError();
 }
 

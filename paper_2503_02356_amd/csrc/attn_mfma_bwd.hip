@@ -51,9 +51,10 @@ constexpr float kLog2e = 1.44269504088896340736f;
 // more, since short sequences leave half of them idle.  By a rule on the call, as the bits have to follow from it alone, a step's slices and
 // packed chunks need a launch each, and that costs more than it gives: 705 -> 743, 401 -> 403, 219 -> 219, 58.6 -> 66.0.
 // 64 or 128 keys took 4-30 % longer than 32, split heads with atomic adds 4 % less.)
-template <int D>
+// LIST: the work comes from a list whose items meet in atomic adds, at either head_dim (windowed calls): shared tiles then.
+template <int D, bool LIST = false>
 struct DkvShape {
-    static constexpr int KW = D == 64 ? 1 : 4, QW = 4 / KW;
+    static constexpr int KW = D == 64 && !LIST ? 1 : 4, QW = 4 / KW;
     static constexpr int BKV = 32 * KW;               // key rows per workgroup
     static constexpr bool OWN = QW > 1;               // every wavefront has tiles of its own
     static constexpr int BQ = OWN ? 32 : 64;          // query rows per tile
@@ -86,12 +87,19 @@ constexpr int kSlots = 512, kSplitTarget = 48, kFineMost = 64, kSmallMost = 8;
 constexpr int kDurationBuckets = 256;
 
 // sum over segments of ceil(Lk / 128) <= n_kv_tokens / 128 + n_segments
-__host__ __device__ inline int64_t key_tiles_most(const cf_attn_fwd_params &p) { return (int64_t)p.n_kv_tokens / BKV + p.n_segments; }
+__host__ __device__ inline int64_t key_tiles_most(const cf_attn_fwd_params &p, const CausalMask & = CausalMask()) { return (int64_t)p.n_kv_tokens / BKV + p.n_segments; }
+// Windowed: of those that some row sees: of a segment's Lq + window - 1 last keys and of its sinks
+inline int64_t key_tiles_most(const cf_attn_fwd_params &p, const WindowMask &m)
+{
+    const int64_t seen = p.n_tokens / BKV + p.n_segments * (2 + ((int64_t)m.window - 1) / BKV + ((int64_t)m.sinks + BKV - 1) / BKV + 1);
+    return std::min(key_tiles_most(p), seen);
+}
 // Items cut inside heads: one per key tile and, beyond that, as many as one key/value head's pairs hold 1.6 / kSlots of all pairs
 // (2.2: fewer).  Whole heads: G per key tile.
-__host__ __device__ inline int64_t dkv_items_most(const cf_attn_fwd_params &p)
+template <typename Mask = CausalMask>
+__host__ __device__ inline int64_t dkv_items_most(const cf_attn_fwd_params &p, const Mask &mask = Mask())
 {
-    const int64_t tiles = key_tiles_most(p), G = p.n_q_heads / p.n_kv_heads, cuts = kSlots * 10 / 16 / p.n_kv_heads + 1;
+    const int64_t tiles = key_tiles_most(p, mask), G = p.n_q_heads / p.n_kv_heads, cuts = kSlots * 10 / 16 / p.n_kv_heads + 1;
     return tiles * G > tiles + cuts ? tiles * G : tiles + cuts;
 }
 
@@ -127,7 +135,9 @@ struct ListCuts {
 // of its own).
 // Segment bounds pass through LDS 256 at a time (one coalesced load instead of a chain of dependent ones); a wavefront
 // takes every fourth segment, its lanes the key tiles.
-__device__ __forceinline__ void build_dkv_worklist(const BwdArgs::Fwd &p, int *wl, int capacity, int slots)
+// one_writer: one item to a key tile, however long.
+template <typename Mask = CausalMask>
+__device__ __forceinline__ void build_dkv_worklist(const BwdArgs::Fwd &p, int *wl, int capacity, int slots, const Mask &mask = Mask(), bool one_writer = false)
 {
     __shared__ int bucket[kDurationBuckets];        // items per duration, then the next free slot of each duration
     __shared__ int seg_lq[256], seg_lk[256];
@@ -148,7 +158,8 @@ __device__ __forceinline__ void build_dkv_worklist(const BwdArgs::Fwd &p, int *w
             for (int s = wave; s < n; s += 4) {
                 const int lq = seg_lq[s], lk = seg_lk[s], off = lk - lq;
                 for (int kt0 = lane * BKV; kt0 < lk; kt0 += 64 * BKV) {
-                    const int n_qt = (lq + BQ - 1) / BQ - max(0, kt0 - off) / BQ;
+                    const QueryTiles<BQ> q_tiles(mask, kt0, min(kt0 + BKV, lk), off, lq);
+                    const int n_qt = q_tiles.end - q_tiles.first;
                     if (n_qt > 0) visit(base + s, kt0, n_qt);
                 }
             }
@@ -164,7 +175,8 @@ __device__ __forceinline__ void build_dkv_worklist(const BwdArgs::Fwd &p, int *w
     auto for_each_item = [&](auto &&visit) {
         for_each_tile([&](int seg, int kt0, int n_qt) {
             bool heads;
-            const int sp = cuts.items(n_qt, G, cut_heads, heads);
+            int sp = cuts.items(n_qt, G, cut_heads, heads);
+            if (Mask::windowed && one_writer) sp = 1;
             // equal shares of the heads or of the pairs, the first few with one more
             const int whole = heads ? G : G * n_qt, unit = heads ? n_qt : 1;
             const int base = sp == 1 ? whole : whole / sp, longer = whole - base * sp;
@@ -202,11 +214,11 @@ __device__ __forceinline__ void build_dkv_worklist(const BwdArgs::Fwd &p, int *w
 
 // One stage: Q tile, dO tile, LSE[64] (log2 units), -delta[64] (the dQ kernel stores it negated); OWN: one for each wavefront.  Two stages
 // (OWN: a wavefront's part of the first) also hold the end-of-kernel transpose scratch (32 rows of D floats per wavefront).
-template <int D>
+template <int D, bool LIST = false>
 struct DkvStage {
-    static constexpr int BQ = DkvShape<D>::BQ;
-    static constexpr bool OWN = DkvShape<D>::OWN;
-    static constexpr int tile_bytes = BQ * 2 * D, one = 2 * tile_bytes + 2 * 64 * 4, bytes = DkvShape<D>::QW * one;
+    static constexpr int BQ = DkvShape<D, LIST>::BQ;
+    static constexpr bool OWN = DkvShape<D, LIST>::OWN;
+    static constexpr int tile_bytes = BQ * 2 * D, one = 2 * tile_bytes + 2 * 64 * 4, bytes = DkvShape<D, LIST>::QW * one;
     static constexpr int scratch_bytes = 32 * D * 4;
     static_assert(OWN ? one >= scratch_bytes : bytes >= 2 * scratch_bytes, "wavefronts turn their results around in a stage");
 };
@@ -246,16 +258,19 @@ struct KeyArgs {
 // rounding would be the largest error in dK/dV.  At D = 64 P and dS enter every product with all their 24 bits instead, as
 // three bf16 operands.
 // RING: operand fragments in flight (below).  wave: of this wavefront.
-template <int D, bool FUSED_HEADS, int RING = 4>
+// WindowMask: of a block's pairs those outside the window are hidden as those above the diagonal are; blocks that a wavefront's keys
+// have no part in are passed over; where no row sees more than 128 keys every pair is a RESIDUAL one.
+template <int D, bool FUSED_HEADS, int RING = 4, typename Mask = CausalMask>
 __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restrict__ delta, int id,
-                                         const int *__restrict__ wl, char *st0, char *st1, int wave = wave_id())
+                                         const int *__restrict__ wl, char *st0, char *st1, int wave = wave_id(), const Mask &mask = Mask())
 {
-    using Stage = DkvStage<D>;
+    constexpr bool LIST = Mask::windowed;
+    using Stage = DkvStage<D, LIST>;
     constexpr int M = D == 64 ? 32 : 16;
     using F = Mfma<M>;
     constexpr int KS = D / F::K, DB = D / 32, N = F::N32, BLOCK = 32 * 2 * D;
-    constexpr int QW = DkvShape<D>::QW, BQ = DkvShape<D>::BQ, BKV = DkvShape<D>::BKV;
-    constexpr bool OWN = DkvShape<D>::OWN;
+    constexpr int QW = DkvShape<D, LIST>::QW, BQ = DkvShape<D, LIST>::BQ, BKV = DkvShape<D, LIST>::BKV;
+    constexpr bool OWN = DkvShape<D, LIST>::OWN;
     static_assert(FUSED_HEADS || QW == 1, "atomic updates are made by the wavefront that owns the keys");
     const BwdArgs::Fwd &p = b.f;
     const int key_wave = wave / QW, query_wave = wave % QW;
@@ -291,8 +306,9 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
         lq = q_seg1 - q_seg0, lk = k_seg1 - k_seg0;
     }
     const int off = lk - lq;
-    const int qt_first = max(0, kt0 - off) / BQ;     // first query tile with a row that sees any key of this tile
-    const int qt_end = (lq + BQ - 1) / BQ;
+    const QueryTiles<BQ> seen_by(mask, kt0, min(kt0 + BKV, lk), off, lq);
+    const int qt_first = seen_by.first;              // first query tile with a row that sees any key of this tile
+    const int qt_end = seen_by.end;
     if (qt_first >= qt_end) return;                  // whole workgroup leaves before any barrier
     if (FUSED_HEADS) n_pairs = G * (qt_end - qt_first);
     // (head, query tile) pairs, head by head; OWN: this wavefront's, every QW-th
@@ -307,7 +323,8 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
         st0 += query_wave * Stage::one, st1 += query_wave * Stage::one;
     }
     // query tiles below qt_head are RESIDUAL ones for this key tile
-    const int qt_head = kt0 == 0 && off < 128 ? (128 - off + BQ - 1) / BQ : 0;
+    int qt_head = kt0 == 0 && off < 128 ? (128 - off + BQ - 1) / BQ : 0;
+    if constexpr (Mask::windowed) qt_head = mask.few(128) ? qt_end : qt_head;
 
     const int kw0 = kt0 + 32 * key_wave;                 // first key of this wavefront (segment-local)
     const bool wave_active = kw0 < lk;
@@ -385,6 +402,7 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
     auto do_block = [&](int mb, const char *stage, bool residual) {
         const int q0 = cur_qt * BQ + mb * 32;
         if (q0 + 31 + off < kw0 || q0 >= lq) return;     // no row of the block sees a key of this wavefront, or none is a row
+        if (before_window(mask, q0 + off, kw0, 32)) return;
         const char *qs = stage, *dos = stage + Stage::tile_bytes;
         const float *stats = (const float *)(stage + 2 * Stage::tile_bytes) + mb * 32 + fresh_lane() / F::M * 4;
         // The A operands of the block's four products pass through a ring of fragments, each requested RING uses
@@ -453,6 +471,18 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
             for (int kb = 0; kb < N; ++kb)
 #pragma unroll
                 for (int i = 0; i < NS; ++i) s[i / F::R][kb][i % F::R] = lim > F::place(i) - F::M * kb ? 0.f : s[i / F::R][kb][i % F::R];
+        }
+        if constexpr (Mask::windowed) {
+            if (crosses_window(mask, q0 + off, kw0, 32)) {
+                const int lane_ = fresh_lane();
+#pragma unroll
+                for (int kb = 0; kb < N; ++kb) {
+                    const int key = kw0 + F::M * kb + lane_ % F::M;
+                    const int far = key < mask.sinks ? 64 : key + mask.window - off - q0 - lane_ / F::M * 4;     // rows from here on do not see it
+#pragma unroll
+                    for (int i = 0; i < NS; ++i) s[i / F::R][kb][i % F::R] = F::place(i) >= far ? 0.f : s[i / F::R][kb][i % F::R];
+                }
+            }
         }
 #pragma unroll
         for (int qb = 0; qb < N; ++qb)
@@ -529,9 +559,9 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
         if (wave_active) {
             const bool residual = cur_qt < qt_head;
 #pragma unroll 1
-            for (int i = 0; i < DkvShape<D>::BLOCKS; ++i) {
+            for (int i = 0; i < DkvShape<D, LIST>::BLOCKS; ++i) {
                 do_block(i, stage, residual);
-                if (DkvShape<D>::BLOCKS == 2) at.flip(BLOCK);
+                if (DkvShape<D, LIST>::BLOCKS == 2) at.flip(BLOCK);
             }
         }
         if (OWN) {
@@ -610,7 +640,8 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
                 }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const bool leave = D == 64 && __ballot(!finite(v[e][0])) != 0;
+                bool leave = false;
+                if (D == 64 || Mask::windowed) leave = __ballot(!finite(D == 64 ? v[e][0] : v[e][0] + v[e][D / 64 - 1])) != 0;
                 if (leave && r0 + e < rows_valid) left_out |= 1u << (r0 + e);
                 if (!leave && r0 + e < rows_valid) {
                     float *row = rows + (int64_t)(r0 + e) * b.dkv_stride_tok + end_lane;
@@ -627,7 +658,29 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
     };
     add_rows(dv, 1.f, b.d_v, not_finite[0]);
     add_rows(dk, p.softmax_scale, b.d_k, not_finite[1]);
-    if (D == 64) {
+    if constexpr (Mask::windowed) {
+        // This item's pairs of those rows, once more pair by pair: of each of its query heads the rows of its query tiles.
+        for (unsigned rows = not_finite[0] | not_finite[1]; rows != 0; rows &= rows - 1) {
+            const int r = __builtin_ctz(rows), krow = k_seg0 + kw0 + r, n_qt = qt_end - qt_first;
+            const unsigned short *kr = row_of<unsigned short>(p.k, krow, p.kv_stride_tok, kh, p.kv_stride_head);
+            const unsigned short *vr = row_of<unsigned short>(p.v, krow, p.kv_stride_tok, kh, p.kv_stride_head);
+            float gk[D / 64] = {}, gv[D / 64] = {};
+            for (int from = first_pair; from < first_pair + n_pairs;) {
+                const int head = from / n_qt, tile = from - head * n_qt, tiles = min(n_qt - tile, first_pair + n_pairs - from);
+                const int row = (qt_first + tile) * BQ;
+                scalar_dkv_rows<unsigned short, D, 4>(b, SegmentRows{q_seg0, lq, k_seg0, lk}, krow, kh * G + head, row, min(row + tiles * BQ, lq),
+                                                      [&](int x) { return ld(kr + x); }, [&](int x) { return ld(vr + x); },
+                                                      [&](int row, int h) { return -delta[(int64_t)h * p.n_tokens + row]; }, gk, gv, mask);
+                from += tiles;
+            }
+            const int64_t at = (int64_t)krow * b.dkv_stride_tok + (int64_t)kh * b.dkv_stride_head + end_lane;
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+                if (not_finite[0] >> r & 1) unsafeAtomicAdd(b.d_v + at + 64 * c, gv[c]);
+                if (not_finite[1] >> r & 1) unsafeAtomicAdd(b.d_k + at + 64 * c, gk[c] * p.softmax_scale);
+            }
+        }
+    } else if (D == 64) {
         for (unsigned rows = not_finite[0] | not_finite[1]; rows != 0; rows &= rows - 1) {
             const int r = __builtin_ctz(rows), krow = k_seg0 + kw0 + r;
             const unsigned short *kr = row_of<unsigned short>(p.k, krow, p.kv_stride_tok, kh, p.kv_stride_head);
@@ -651,6 +704,15 @@ __global__ __launch_bounds__(256, 2) void mfma_dkv_kernel(BwdArgs b, const float
     __shared__ __attribute__((aligned(16))) char st0[DkvStage<D>::bytes];
     __shared__ __attribute__((aligned(16))) char st1[DkvStage<D>::bytes];
     dkv_body<D, FUSED_HEADS>(b, delta, blockIdx.x, wl, st0, st1);
+}
+
+// One call with a window: the keys that some row sees, by a work list at either head_dim.
+template <int D>
+__global__ __launch_bounds__(256, 2) void mfma_window_dkv_kernel(BwdArgs b, const float *__restrict__ delta, const int *__restrict__ wl, WindowMask mask)
+{
+    __shared__ __attribute__((aligned(16))) char st0[DkvStage<D, true>::bytes];
+    __shared__ __attribute__((aligned(16))) char st1[DkvStage<D, true>::bytes];
+    dkv_body<D, false, D == 128 ? 3 : 4>(b, delta, blockIdx.x, wl, st0, st1, wave_id(), mask);
 }
 
 // Several chunks' backward in one launch.
@@ -708,8 +770,9 @@ struct KvStage {
 // the others (one query head per workgroup left the wavefronts without rows idle), the second run takes one or two key tiles from
 // LDS, where the first has left them, and no tile's second half is computed where no row sees it.  Steps of 16 packed chunks, 28 / 4
 // heads: 512 tokens around 37 each 297 -> 269 us, 8192 around 600 9.31 -> 9.05 ms; 16 / 4 heads, D = 64, 16.7k tokens 979 -> 940 us.
-template <int D, int M>
-__device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ delta, int id, char *stage_a, char *stage_b)
+// WindowMask: key tiles as in the forward kernel; where no row sees more than 128 keys every tile is a head tile.
+template <int D, int M, typename Mask = CausalMask>
+__device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ delta, int id, char *stage_a, char *stage_b, const Mask &mask = Mask())
 {
     using F = Mfma<M>;
     constexpr int KS = D / F::K, DB = D / F::M, N = F::N32, KVTILE_BYTES = KvStage<D>::tile_bytes;
@@ -739,7 +802,8 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
     }
     const int off = lk - lq;
     const int q_tile0 = tile_in_seg * BM;
-    const bool head = q_tile0 + off < 128;
+    bool head = q_tile0 + off < 128;
+    if constexpr (Mask::windowed) head = head || mask.few(128);
     // The tile's 4 G units (32-row block, query head of the group) are dealt out four at a time, block-major (as in the
     // forward kernel).
     const int unit = 4 * j + wave;
@@ -748,7 +812,8 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
     const int rows_valid = min(BM, lq - q_tile0);
     if (q_tile0 + (4 * j) / G * 32 >= lq) return;    // all four units lie beyond the last row
     const int kmax = q_tile0 + min(rows_valid, ((4 * j + 3) / G + 1) * 32) + off;   // keys [0, kmax) are visible to some row of the workgroup
-    const int n_tiles = (kmax + BN - 1) / BN;
+    const KeyTiles<BN, Mask> key_tiles(mask, q_tile0 + (4 * j) / G * 32 + off, kmax);
+    const int n_tiles = key_tiles.n;
     const int wq0 = q_tile0 + blk * 32;
     const int wave_kmax = min(kmax, wq0 + 32 + off);
     const bool wave_active = wq0 < lq;
@@ -811,18 +876,19 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
     auto sweep = [&](auto delta_pass_tag, int staged) {
         constexpr bool DELTA_PASS = decltype(delta_pass_tag)::value;
         if (staged == 0) {
-            issue_tile(0, stage_a);
+            issue_tile(key_tiles.start(0), stage_a);
             wait_lds_dma();
             __syncthreads();
         }
         auto do_tile = [&](int t, const char *stage, char *next_stage) {
-            const int tile_start = t * BN;
+            const int tile_start = key_tiles.start(t);
             const char *ks_ = stage;
             const char *vs_ = stage + KVTILE_BYTES;
-            if (t + 1 < n_tiles && t + 1 >= staged) issue_tile(tile_start + BN, next_stage);
+            if (t + 1 < n_tiles && t + 1 >= staged) issue_tile(key_tiles.next(t, tile_start), next_stage);
 
             if (wave_active && tile_start < wave_kmax) {
-                const bool need_mask = tile_start + BN - 1 > wq0 + off;
+                bool need_mask = tile_start + BN - 1 > wq0 + off;
+                if constexpr (Mask::windowed) need_mask = need_mask || crosses_window(mask, wq0 + off, tile_start, BN);
                 // element i of a query (register i % R of key block i / R) is key tile_start + 32*mb + place(i) + 4*group:
                 // masked iff the compile-time part of that exceeds lim
                 const int lim = amax - tile_start - group * 4;
@@ -830,6 +896,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
 #pragma unroll
                 for (int mb = 0; mb < 2; ++mb) {
                     if (mb == 1 && tile_start + 32 >= wave_kmax) break;      // no row sees the second half
+                    if (before_window(mask, wq0 + off, tile_start + 32 * mb, 32)) continue;
                     // S^T and dP^T for 32 keys.
                     // All 16 fragments are requested before the first MFMA: the LDS latency is paid once per
                     // block, not once per MFMA.
@@ -887,10 +954,14 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
 #pragma unroll
                         for (int i = 0; i < NS; ++i) {
                             float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / F::R][qb][i % F::R], c2, -lse2[qb]));
-                            const bool hidden = need_mask && mb * 32 + F::place(i) - F::M * qb > lim;
+                            bool hidden = need_mask && mb * 32 + F::place(i) - F::M * qb > lim;
+                            if constexpr (Mask::windowed) {
+                                const int key = mb * 32 + F::place(i);
+                                hidden = hidden || (key - F::M * qb <= lim - mask.window && key >= mask.sinks - tile_start - group * 4);
+                            }
                             if (hidden) pv = 0.f;
                             // (dP of a hidden pair may be anything)
-                            if (DELTA_PASS) dsum[qb] += D == 64 && hidden ? 0.f : pv * dp[i / F::R][qb][i % F::R];
+                            if (DELTA_PASS) dsum[qb] += (D == 64 || Mask::windowed) && hidden ? 0.f : pv * dp[i / F::R][qb][i % F::R];
                             else dp[i / F::R][qb][i % F::R] = pv * (dp[i / F::R][qb][i % F::R] - dlt[qb]);
                         }
                     if (DELTA_PASS) continue;
@@ -956,13 +1027,13 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
         store_rows_bf16<D, M>(dq, scale, scratch, lq - wq0, [&](int r) {
             return (char *)b.d_q + ((int64_t)(q_seg0 + wq0 + r) * b.dq_stride_tok + (int64_t)h * b.dq_stride_head) * 2;
         });
-        if constexpr (D == 64) {
-            for_rows_not_finite<D>(dq, p.softmax_scale, lq - wq0, [&](int r) {
+        if constexpr (D == 64 || Mask::windowed) {
+            for_rows_not_finite<D, M>(dq, scale, lq - wq0, [&](int r) {
                 const int row = q_seg0 + wq0 + r;
                 const unsigned short *qr = row_of<unsigned short>(p.q, row, p.q_stride_tok, h, p.q_stride_head);
                 const unsigned short *dr = row_of<unsigned short>(b.d_o, row, b.do_stride_tok, h, b.do_stride_head);
-                scalar_dq_row<unsigned short, 64, 4>(b, SegmentRows{q_seg0, lq, k_seg0, lk}, row, h, [&](int x) { return ld(qr + x); },
-                                                  [&](int x) { return ld(dr + x); }, __shfl(dlt[0], r));
+                scalar_dq_row<unsigned short, D, 4>(b, SegmentRows{q_seg0, lq, k_seg0, lk}, row, h, [&](int x) { return ld(qr + x); },
+                                                  [&](int x) { return ld(dr + x); }, __shfl(dlt[r / M], r % M), mask);
             });
         }
     }
@@ -983,6 +1054,18 @@ __global__ __launch_bounds__(256, 2) void mfma_dq_kernel(BwdArgs b, float *__res
     __shared__ __attribute__((aligned(16))) char stage_a[KvStage<D>::bytes];
     __shared__ __attribute__((aligned(16))) char stage_b[KvStage<D>::bytes];
     dq_body<D, M>(b, delta, (int)blockIdx.x - (wl != nullptr ? 1 : 0), stage_a, stage_b);
+}
+
+template <int D, int M>
+__global__ __launch_bounds__(256, 2) void mfma_window_dq_kernel(BwdArgs b, float *__restrict__ delta, int *wl, int capacity, int one_writer, WindowMask mask)
+{
+    if (blockIdx.x == 0) {
+        build_dkv_worklist(b.f, wl, capacity, kSlots, mask, one_writer != 0);
+        return;
+    }
+    __shared__ __attribute__((aligned(16))) char stage_a[KvStage<D>::bytes];
+    __shared__ __attribute__((aligned(16))) char stage_b[KvStage<D>::bytes];
+    dq_body<D, M>(b, delta, (int)blockIdx.x - 1, stage_a, stage_b, mask);
 }
 
 // Several chunks, heaviest first: dQ and delta of a chunk depend on nothing another chunk's backward writes, so the last,
@@ -1190,6 +1273,32 @@ int64_t mfma_bwd_blocks(const cf_attn_fwd_params &p)
 {
     const int64_t items = p.head_dim == 64 ? 0 : dkv_items_most(p);
     return std::max(q_tiles_most(p) * p.n_q_heads + 1, std::max(kv_tiles_most(p), items) * p.n_kv_heads);
+}
+
+// Windowed calls: room for the list, and launches.
+int64_t window_worklist_capacity(const cf_attn_fwd_params &p, const WindowMask &mask) { return dkv_items_most(p, mask); }
+int64_t window_launch_size(const cf_attn_fwd_params &p, const WindowMask &mask)
+{
+    return std::max(q_tiles_most(p) * p.n_q_heads + 1, window_worklist_capacity(p, mask) * p.n_kv_heads) * 256;
+}
+
+template <int D>
+static hipError_t run_window_bwd(const cf_attn_bwd_params &b, const BwdWorkspace &ws, const WindowMask &mask, hipStream_t s)
+{
+    const int64_t dq_blocks = q_tiles_most(b.f) * b.f.n_q_heads + 1, dkv_blocks = ws.worklist_items * b.f.n_kv_heads;
+    if (dq_blocks > 0x7fffffffLL || dkv_blocks > 0x7fffffffLL || ws.worklist_items > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    const int one_writer = (b.f.flags & CF_FLAG_DKV_SINGLE_WRITER) != 0, capacity = (int)ws.worklist_items;
+    const dim3 grid((unsigned)dq_blocks);
+    if (D == 64 || wide_mfma(b.f)) mfma_window_dq_kernel<D, 32><<<grid, 256, 0, s>>>(b, ws.delta, ws.worklist, capacity, one_writer, mask);
+    else if constexpr (D == 128) mfma_window_dq_kernel<D, 16><<<grid, 256, 0, s>>>(b, ws.delta, ws.worklist, capacity, one_writer, mask);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    mfma_window_dkv_kernel<D><<<dim3((unsigned)dkv_blocks), 256, 0, s>>>(b, ws.delta, ws.worklist, mask);
+    return hipGetLastError();
+}
+hipError_t launch_window_mfma_bwd(const cf_attn_bwd_params &b, const BwdWorkspace &ws, const WindowMask &mask, hipStream_t s)
+{
+    return b.f.head_dim == 64 ? run_window_bwd<64>(b, ws, mask, s) : run_window_bwd<128>(b, ws, mask, s);
 }
 
 int64_t dkv_worklist_least(const cf_attn_fwd_params &p) { return key_tiles_most(p) * (p.n_q_heads / p.n_kv_heads); }

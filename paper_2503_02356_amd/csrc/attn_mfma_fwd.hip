@@ -38,8 +38,10 @@ struct Stage {
 // id: index of the workgroup among those of this chunk; SHARED: of several chunks in a launch
 // D = 64 keeps what the scalar kernels keep in fp32: the second product takes P with all its 24 bits, as three bf16 operands
 // (three MFMAs), exponentials and row sums are formed so that the errors of O and LSE against fp64 are no larger than theirs.
-template <int D, int M, bool SHARED>
-__device__ __forceinline__ void fwd_body(const cf_attn_fwd_params &p, int id, char *stage_a, char *stage_b)
+// WindowMask: key tiles that no row of the workgroup sees, between its sinks and its windows, are passed over, and so are those that
+// no row of a wavefront sees; the mask is applied where a tile crosses the diagonal or a window's far end.
+template <int D, int M, bool SHARED, typename Mask>
+__device__ __forceinline__ void fwd_body(const cf_attn_fwd_params &p, int id, char *stage_a, char *stage_b, const Mask &mask)
 {
     using F = Mfma<M>;
     constexpr int KS = D / F::K, DB = D / F::M, KB = BN / F::M, QB = F::N32, TILE_BYTES = Stage<D>::tile_bytes;
@@ -83,7 +85,8 @@ __device__ __forceinline__ void fwd_body(const cf_attn_fwd_params &p, int id, ch
     const int rows_valid = min(BM, lq - q_tile0);
     if (q_tile0 + (4 * j) / G * 32 >= lq) return;    // all four units lie beyond the last row
     const int kmax = q_tile0 + min(rows_valid, ((4 * j + 3) / G + 1) * 32) + off;   // keys [0, kmax) are visible to some row of the workgroup
-    const int n_tiles = (kmax + BN - 1) / BN;
+    const KeyTiles<BN, Mask> key_tiles(mask, q_tile0 + (4 * j) / G * 32 + off, kmax);
+    const int n_tiles = key_tiles.n;
 
     const int wq0 = q_tile0 + blk * 32;              // first row of this wavefront (segment-local)
     const int wave_kmax = min(kmax, wq0 + 32 + off); // keys this wavefront needs (<= 0 rows valid: nothing)
@@ -124,15 +127,15 @@ __device__ __forceinline__ void fwd_body(const cf_attn_fwd_params &p, int id, ch
         dma.issue(kbase + (int64_t)tile_start * kv_row_bytes, lk - 1 - tile_start, stage);
         dma.issue(vbase + (int64_t)tile_start * kv_row_bytes, lk - 1 - tile_start, stage + TILE_BYTES);
     };
-    issue_tile(0, stage_a);
+    issue_tile(key_tiles.start(0), stage_a);
     wait_lds_dma();
     __syncthreads();
 
     auto do_tile = [&](int t, const char *stage, char *next_stage) {
-        const int tile_start = t * BN;
-        if (t + 1 < n_tiles) issue_tile(tile_start + BN, next_stage);
+        const int tile_start = key_tiles.start(t);
+        if (t + 1 < n_tiles) issue_tile(key_tiles.next(t, tile_start), next_stage);
 
-        if (wave_active && tile_start < wave_kmax) {
+        if (wave_active && tile_start < wave_kmax && !before_window(mask, wq0 + off, tile_start, BN)) {
             // ---- S^T = K Q^T : KB key blocks by QB query blocks
             // All 16 K fragments (D = 128) are requested before the first MFMA: the LDS latency is paid once per tile,
             // not once per MFMA (the matrix unit then consumes them in arrival order).
@@ -168,6 +171,16 @@ __device__ __forceinline__ void fwd_body(const cf_attn_fwd_params &p, int id, ch
                     for (int i = 0; i < NS; ++i)
                         if (F::place(i) - F::M * qb > lim) s[i / F::R][qb][i % F::R] = -INFINITY;
             }
+            if constexpr (Mask::windowed) {
+                if (crosses_window(mask, wq0 + off, tile_start, BN)) {
+                    const int far = amax - mask.window - tile_start - group * 4, sink = mask.sinks - tile_start - group * 4;
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                        for (int i = 0; i < NS; ++i)
+                            if (F::place(i) - F::M * qb <= far && F::place(i) >= sink) s[i / F::R][qb][i % F::R] = -INFINITY;
+                }
+            }
             // ---- online softmax (log2 domain)
             // Lazy rescale: the running reference m_run only moves when a row's new maximum exceeds it by more than
             // 2^kLazy; until then P = exp2(s - m_run) <= 2^kLazy, exact enough in the fp32 sums and in bf16 alike,
@@ -187,7 +200,8 @@ __device__ __forceinline__ void fwd_body(const cf_attn_fwd_params &p, int id, ch
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
                     const float mx = max_over_groups<M>(mx2[qb]), m_new = mx > m_run[qb] + kLazy<D> ? mx : m_run[qb];
-                    const float alpha = __builtin_amdgcn_exp2f((m_run[qb] - m_new) * kUnit);   // first tile: exp2(-inf) = 0
+                    // first tile: exp2(-inf) = 0.  (Windowed: a row may see none of the tiles so far, and -inf - -inf is none of its factors.)
+                    const float alpha = Mask::windowed && m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m_run[qb] - m_new) * kUnit);
                     m_run[qb] = m_new;
                     l_run[qb] *= alpha;
 #pragma unroll
@@ -198,10 +212,11 @@ __device__ __forceinline__ void fwd_body(const cf_attn_fwd_params &p, int id, ch
             constexpr int CHAINS = D == 64 ? 8 : 1;
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
+                const float m_ref = Mask::windowed && m_run[qb] == -INFINITY ? 0.f : m_run[qb];
                 float rs[CHAINS] = {};
 #pragma unroll
                 for (int i = 0; i < NS; ++i) {
-                    const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / F::R][qb][i % F::R], c2, -m_run[qb]) * kUnit);
+                    const float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / F::R][qb][i % F::R], c2, -m_ref) * kUnit);
                     s[i / F::R][qb][i % F::R] = pv;
                     rs[i % CHAINS] += pv;
                 }
@@ -265,11 +280,11 @@ __device__ __forceinline__ void fwd_body(const cf_attn_fwd_params &p, int id, ch
         // One rounding in every kernel: where a product and a sum end up in different blocks, the compiler rounds both.
         p.lse[(int64_t)h * p.n_tokens + q_seg0 + iq] = __builtin_fmaf(m, D == 64 ? 1.f : 0.69314718055994530942f, __logf(l));
     }
-    if constexpr (D == 64) {
-        for_rows_not_finite<D>(o_acc, scale[0], lq - wq0, [&](int r) {
+    if constexpr (D == 64 || Mask::windowed) {
+        for_rows_not_finite<D, M>(o_acc, scale, lq - wq0, [&](int r) {
             const int row = q_seg0 + wq0 + r;
             const unsigned short *qr = row_of<unsigned short>(p.q, row, p.q_stride_tok, h, p.q_stride_head);
-            scalar_fwd_row<unsigned short, 64, 4>(p, SegmentRows{q_seg0, lq, k_seg0, lk}, row, h, [&](int x) { return ld(qr + x); });
+            scalar_fwd_row<unsigned short, D, 4>(p, SegmentRows{q_seg0, lq, k_seg0, lk}, row, h, [&](int x) { return ld(qr + x); }, mask);
         });
     }
 }
@@ -281,7 +296,15 @@ __global__ __launch_bounds__(256, 2) void mfma_fwd_kernel(cf_attn_fwd_params p)
     // loads of the next tile cannot alias the reads of the current one, or it waits for them too early.
     __shared__ __attribute__((aligned(16))) char stage_a[Stage<D>::bytes];
     __shared__ __attribute__((aligned(16))) char stage_b[Stage<D>::bytes];
-    fwd_body<D, M, false>(p, blockIdx.x, stage_a, stage_b);
+    fwd_body<D, M, false>(p, blockIdx.x, stage_a, stage_b, CausalMask());
+}
+
+template <int D, int M>
+__global__ __launch_bounds__(256, 2) void mfma_window_fwd_kernel(cf_attn_fwd_params p, WindowMask mask)
+{
+    __shared__ __attribute__((aligned(16))) char stage_a[Stage<D>::bytes];
+    __shared__ __attribute__((aligned(16))) char stage_b[Stage<D>::bytes];
+    fwd_body<D, M, false>(p, blockIdx.x, stage_a, stage_b, mask);
 }
 
 // Several chunks in one launch.  The host
@@ -300,8 +323,8 @@ __global__ __launch_bounds__(256, 2) void mfma_fwd_batch_kernel(FwdBatch b)
     __shared__ __attribute__((aligned(16))) char stage_b[Stage<D>::bytes];
     int id = blockIdx.x;
     const int c = b.blocks.chunk_of(id);
-    if (M == 32 || (M == 0 && (b.wide >> c & 1))) fwd_body<D, 32, true>(b.p[c], id, stage_a, stage_b);
-    else if constexpr (M != 32) fwd_body<D, 16, true>(b.p[c], id, stage_a, stage_b);
+    if (M == 32 || (M == 0 && (b.wide >> c & 1))) fwd_body<D, 32, true>(b.p[c], id, stage_a, stage_b, CausalMask());
+    else if constexpr (M != 32) fwd_body<D, 16, true>(b.p[c], id, stage_a, stage_b, CausalMask());
 }
 
 // Upper bound on the number of 128-row tiles: sum_g ceil(Lq_g / BM) <= T / BM + n_segments.
@@ -346,6 +369,17 @@ hipError_t launch_mfma_fwd(const cf_attn_fwd_params &p, hipStream_t s)
     const hipError_t e = hipGetLastError();
     if (hook.stop) (void)hipEventRecord(hook.stop, s);
     return e;
+}
+
+hipError_t launch_window_mfma_fwd(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s)
+{
+    const int64_t blocks = fwd_blocks(p);
+    if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+    const dim3 grid((unsigned)blocks);
+    if (p.head_dim == 64) mfma_window_fwd_kernel<64, 32><<<grid, 256, 0, s>>>(p, mask);
+    else if (wide_mfma(p)) mfma_window_fwd_kernel<128, 32><<<grid, 256, 0, s>>>(p, mask);
+    else mfma_window_fwd_kernel<128, 16><<<grid, 256, 0, s>>>(p, mask);
+    return hipGetLastError();
 }
 
 }  // namespace cf

@@ -58,7 +58,7 @@ CF_BOTH int rows_that_see(const WindowMask &m, int j, int prefix, int lq)
 }
 
 // The key tiles of `TILE` keys that rows at positions [first_position, keys) see, `keys` being one more than the last of them: tile t starts
-// at key start(t).
+// at key start(t), the one behind it at next(t, start(t)).
 template <int TILE, typename Mask>
 struct KeyTiles;
 template <int TILE>
@@ -66,6 +66,7 @@ struct KeyTiles<TILE, CausalMask> {
     int n;
     CF_BOTH KeyTiles(const CausalMask &, int, int keys) : n((keys + TILE - 1) / TILE) {}
     CF_BOTH int start(int t) const { return t * TILE; }
+    CF_BOTH int next(int, int start) const { return start + TILE; }
 };
 template <int TILE>
 struct KeyTiles<TILE, WindowMask> {
@@ -78,6 +79,7 @@ struct KeyTiles<TILE, WindowMask> {
         n = (keys + TILE - 1) / TILE - gap;
     }
     CF_BOTH int start(int t) const { return (t < sinks ? t : t + gap) * TILE; }
+    CF_BOTH int next(int t, int) const { return start(t + 1); }
 };
 
 // The query tiles of `TILE` rows, [first, end), with a row that sees one of the keys [key, key_end) of a segment.

@@ -23,6 +23,7 @@
 #include <stdint.h>
 
 #include "chunkflow.h"
+#include "mask.h"
 
 namespace cf {
 
@@ -285,6 +286,19 @@ struct TileDma {
         }
     }
 };
+// Of the rows of a 32-row block whose first one is at `position` and a tile of `keys` keys from `start` on: does none of them see the
+// tile, since it lies before their windows and holds no sink, and does one of them not see a key of it for that?  (Of what the causal
+// mask leaves.)
+__device__ __forceinline__ bool before_window(const CausalMask &, int, int, int) { return false; }
+__device__ __forceinline__ bool before_window(const WindowMask &m, int position, int start, int keys)
+{
+    return start + keys <= position + 1 - m.window && start >= m.sinks;
+}
+__device__ __forceinline__ bool crosses_window(const WindowMask &m, int position, int start, int keys)
+{
+    return start <= position + 31 - m.window && start + keys > m.sinks;
+}
+
 // Makes a pointer / an int that is the same in every lane known as such to the compiler.
 template <typename T>
 __device__ __forceinline__ T *uniform(T *p)
@@ -381,18 +395,22 @@ __device__ __forceinline__ void store_rows_bf16(const RowBlock<D, M> &acc, const
     }
 }
 
-// visit(r), by the whole wavefront, for every row r < rows_valid of a 32 x D block (as above, D = 64: a lane owns row lane % 32) whose
-// results, scaled, are not finite.
-template <int D, typename Visit>
-__device__ __forceinline__ void for_rows_not_finite(const RowBlock<D, 32> &acc, float scale, int rows_valid, Visit visit)
+// visit(r), by the whole wavefront, for every row r < rows_valid of a 32 x D block (as above) whose results, scaled, are not finite.
+template <int D, int M, typename Visit>
+__device__ __forceinline__ void for_rows_not_finite(const RowBlock<D, M> &acc, const float (&scale)[Mfma<M>::N32], int rows_valid, Visit visit)
 {
-    float zero = scale * 0.f;                        // stays 0 while everything is finite
+    unsigned rows = 0;
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j)
+    for (int n = 0; n < Mfma<M>::N32; ++n) {
+        float zero = scale[n] * 0.f;                 // stays 0 while everything is finite
 #pragma unroll
-        for (int i = 0; i < 16; ++i) zero = __builtin_fmaf(acc[j][0][i], 0.f, zero);
-    const unsigned long long lanes = __ballot(zero != 0.f);
-    unsigned rows = (unsigned)lanes | (unsigned)(lanes >> 32);
+        for (int j = 0; j < D / M; ++j)
+#pragma unroll
+            for (int i = 0; i < Mfma<M>::R; ++i) zero = __builtin_fmaf(acc[j][n][i], 0.f, zero);
+        const unsigned long long lanes = __ballot(zero != 0.f);
+        const unsigned halves = (unsigned)lanes | (unsigned)(lanes >> 32);
+        rows |= M == 32 ? halves : ((halves | halves >> 16) & 0xffff) << (16 * n);
+    }
     if (rows_valid < 32) rows &= (1u << rows_valid) - 1;
     for (; rows != 0; rows &= rows - 1) visit(__builtin_ctz(rows));
 }

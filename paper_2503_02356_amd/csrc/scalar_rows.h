@@ -155,6 +155,44 @@ __device__ inline void scalar_dq_row(const B &b, const SegmentRows &g, int row, 
     for (int t = 0; t < DPL; ++t) st(dq + lane + 64 * t, acc[t] * p.softmax_scale);
 }
 
+// What query head h's rows [row, end) of the segment add to dK and dV of key row `krow` (element lane + 64 t; dK without the scale).
+template <typename T, int D, int UNROLL, typename B, typename K, typename V, typename Delta, typename Mask>
+__device__ inline void scalar_dkv_rows(const B &b, const SegmentRows &g, int krow, int h, int row, int end, K k, V v, Delta delta,
+                                       float (&dk)[D / 64], float (&dv)[D / 64], const Mask &mask)
+{
+    const auto &p = b.f;
+    const int lane = threadIdx.x & 63, j = krow - g.k0, prefix = g.lk - g.lq;
+    row = max(row, j - prefix);
+    end = min(end, rows_that_see(mask, j, prefix, g.lq));
+    const T *qb = (const T *)p.q + (int64_t)h * p.q_stride_head;
+    const T *dob = (const T *)b.d_o + (int64_t)h * b.do_stride_head;
+    for (int i0 = row; i0 < end; i0 += 64) {
+        const int i = i0 + lane;
+        float pr = 0.f, ds = 0.f;
+        if (i < end) {
+            const T *qi = qb + (int64_t)(g.q0 + i) * p.q_stride_tok;
+            const T *doi = dob + (int64_t)(g.q0 + i) * b.do_stride_tok;
+            float s = 0.f, dp = 0.f;
+            for_elements<D, UNROLL>([&](int x) {
+                s += ld(qi + x) * k(x);
+                dp += ld(doi + x) * v(x);
+            });
+            pr = expf(s * p.softmax_scale - p.lse[(int64_t)h * p.n_tokens + g.q0 + i]);
+            ds = pr * (dp - delta(g.q0 + i, h));
+        }
+        const int cnt = min(64, end - i0);
+        for (int ii = 0; ii < cnt; ++ii) {
+            const float pi = __shfl(pr, ii), di = __shfl(ds, ii);
+            const T *qi = qb + (int64_t)(g.q0 + i0 + ii) * p.q_stride_tok;
+            const T *doi = dob + (int64_t)(g.q0 + i0 + ii) * b.do_stride_tok;
+            for (int t = 0; t < D / 64; ++t) {
+                dv[t] += pi * ld(doi + lane + 64 * t);
+                dk[t] += di * ld(qi + lane + 64 * t);
+            }
+        }
+    }
+}
+
 // What all query heads of key/value head kh add to dK and dV of key row `krow` (element lane + 64 t; dK without the scale).
 // delta(row, h): of a query row.
 template <typename T, int D, int UNROLL, typename B, typename K, typename V, typename Delta, typename Mask = CausalMask>

@@ -24,7 +24,7 @@ def attention(q, k, v, scale, seen, d_o=None):
     total = e.sum(1, keepdim=True)
     P = e / torch.where(total == 0, 1.0, total)
     vz, kz = torch.where(seen.any(0)[:, None], v, 0.0), torch.where(seen.any(0)[:, None], k, 0.0)
-    r = dict(o=P @ vz, lse=(top + torch.log(total))[:, 0], o_abs=P @ vz.abs(), score_abs=float(((q.abs() @ kz.abs().T) * scale).max()))
+    r = dict(o=P @ vz, lse=(top + torch.log(total))[:, 0], o_abs=P @ vz.abs(), score_abs=float((q.abs() @ kz.abs().T).max()) * abs(scale))
     if d_o is not None:
         dP = d_o @ vz.T
         delta = (P * dP).sum(1, keepdim=True)
@@ -32,9 +32,9 @@ def attention(q, k, v, scale, seen, d_o=None):
         r.update(dq=scale * dS @ kz, dk=scale * dS.T @ q, dv=P.T @ d_o)
         big = P * (dP.abs() + delta.abs())
         delta_abs = (d_o * r["o"]).abs().sum(1, keepdim=True)
-        r.update(dq_abs=scale * big @ kz.abs(), dk_abs=scale * big.T @ q.abs(), dv_abs=P.T @ d_o.abs(),
-                 dq_round=scale * dS.abs() @ kz.abs(), dk_round=scale * dS.abs().T @ q.abs(),
-                 dq_delta=scale * (P * delta_abs) @ kz.abs(), dk_delta=scale * (P * delta_abs).T @ q.abs())
+        r.update(dq_abs=abs(scale) * big @ kz.abs(), dk_abs=abs(scale) * big.T @ q.abs(), dv_abs=P.T @ d_o.abs(),
+                 dq_round=abs(scale) * dS.abs() @ kz.abs(), dk_round=abs(scale) * dS.abs().T @ q.abs(),
+                 dq_delta=abs(scale) * (P * delta_abs) @ kz.abs(), dk_delta=abs(scale) * (P * delta_abs).T @ q.abs())
     return r
 
 

@@ -3,6 +3,7 @@ kernels go over, and the 64-bit formulas that the GPU tests compare with."""
 import ctypes
 import itertools
 import os
+import re
 import subprocess
 
 import numpy as np
@@ -10,7 +11,9 @@ import pytest
 import torch
 
 from paper_2503_02356_amd import binding as B
+from paper_2503_02356_amd import build
 from tests import plain_window as W
+from tests.test_build_checks import REPORT, accumulator_faults
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -191,3 +194,20 @@ def test_formulas_against_differences_and_differentiation():
                 y[at] += sign
                 both.append(loss(*[y if i == n else z for i, z in enumerate((q, k, v))]))
             assert abs((both[0] - both[1]) / 2e-5 - float(r[name][at])) < 1e-8
+
+
+@pytest.mark.skipif(not os.path.exists(build.HIPCC), reason="needs hipcc")
+def test_nothing_else_touches_an_accumulator_of_the_windowed_kernel(tmp_path):
+    """As for the kernels without a window (tests/test_build_checks.py): at head_dim 128 its accumulators are updated in place."""
+    out = str(tmp_path / "bwd.s")
+    subprocess.run([build.HIPCC] + build.HIP_FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", build.CSRC, "--cuda-device-only", "-S",
+                    os.path.join(build.CSRC, "attn_mfma_bwd.hip"), "-o", out], check=True, stderr=subprocess.DEVNULL)
+    (name, body), = re.findall(r"^(\S*mfma_window_dkv\S*ILi128E\S*):.*?\n(.*?)^\.Lfunc_end", open(out).read(), re.M | re.S)
+    n, regs, faults = accumulator_faults(body)
+    assert n > 0 and regs == 128 and faults == [], (name, n, regs, faults[:5])
+
+
+def test_a_spilled_accumulator_of_the_windowed_kernel_fails_the_build():
+    report = REPORT.replace("16mfma_dkv_kernel", "23mfma_window_dkv_kernel")
+    assert build.spilled_accumulators(report.format(scratch=0, spill=0)) == []
+    assert len(build.spilled_accumulators(report.format(scratch=8, spill=2))) == 2
