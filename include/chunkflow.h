@@ -364,6 +364,74 @@ int64_t cf_count_window_pairs(const int32_t *cu_seqlens_q_host, const int32_t *c
                               const cf_attn_window *w);
 
 /*
+ * Attention of new tokens over a paged cache (forward only): evaluating or serving what has been trained, in the same chunks -- a slice
+ * of a long sequence behind its earlier ones, several sequences packed, or one new token of each of many sequences.
+ *   Keys and values stand in pages of page_size tokens, k_pages / v_pages [n_pages][page_size][Hkv][D].  Key j of sequence g is row
+ *   j % page_size of page block_table[g * table_stride + j / page_size].  The sequence has kv_lens[g] keys, of which the last Lq_g (those of
+ *   rows [cu_seqlens_q[g], cu_seqlens_q[g+1]) of q) are its new tokens' own, already in the pages (cf_kv_append).
+ *   Query row i of sequence g has position p = kv_lens[g] - Lq_g + i and sees the keys j <= p; with window > 0 of these only
+ *   j > p - window or j < n_sinks (as in cf_attn_window_fwd; window 0: n_sinks must be 0).
+ *   A page number outside [0, n_pages) is no page: its keys are hidden (pages that a window has left behind can be given back and
+ *   marked -1), and so are keys behind the table's last column.  A row that sees no key has o = 0 and lse = -infinity.
+ *   Sequences may be empty (Lq_g = 0).  Rows of q and o from cu_seqlens_q[n_seqs] on (a padded batch) are neither read nor written.
+ * Key and value rows that no row of a call sees are not read, whatever stands there (the rest of a page may be uninitialised).
+ * Infinities and NaNs in a key or value reach only the rows that see it.  Results are bitwise reproducible.
+ * cu_seqlens_q is NOT validated (as in cf_attn_fwd); kv_lens and block_table may hold anything: no access leaves the pages.
+ * max_kv_len is the longest kv_lens that the caller expects (0: as many as the table's columns hold); it decides how the work is cut, not
+ * what is computed.  Long caches with few rows are cut along the keys; the parts are joined through the workspace, at least
+ * cf_attn_paged_workspace_bytes(p) bytes (may be 0; then NULL is fine), 256-byte aligned, not preserved, which calls that overlap may
+ * not share.
+ */
+typedef struct {
+    int32_t dtype;                      /* CF_BF16 or CF_FP32: q, pages, o                       */
+    int32_t flags;                      /* 0 or CF_FLAG_SCALAR_KERNELS                           */
+    int32_t n_q_heads, n_kv_heads;      /* n_q_heads % n_kv_heads == 0                           */
+    int32_t head_dim;                   /* 64 or 128                                             */
+    float softmax_scale;                /* finite                                                */
+    int32_t n_tokens;                   /* rows of q and o, >= 1; n_tokens * n_q_heads < 2^31    */
+    int32_t n_seqs;                     /* >= 1                                                  */
+    const int32_t *cu_seqlens_q;        /* device, [n_seqs+1]                                    */
+    const int32_t *kv_lens;             /* device, [n_seqs]                                      */
+    const int32_t *block_table;         /* device, [n_seqs][pages_per_seq]                       */
+    int64_t table_stride;               /* elements from row to row, >= pages_per_seq            */
+    int32_t pages_per_seq;              /* >= 1; pages_per_seq * page_size < 2^31                */
+    int32_t page_size;                  /* a power of two, 16 .. 65536                           */
+    int32_t n_pages;                    /* >= 1                                                  */
+    int32_t max_kv_len;                 /* >= 0                                                  */
+    int32_t window, n_sinks;            /* >= 0                                                  */
+    const void *q;                      /* device, [T][Hq][D]                                    */
+    int64_t q_stride_tok, q_stride_head;
+    const void *k_pages, *v_pages;      /* device, same strides for both                         */
+    int64_t page_stride, kv_stride_tok, kv_stride_head;
+    void *o;                            /* device, [T][Hq][D], written                           */
+    int64_t o_stride_tok, o_stride_head;
+    float *lse;                         /* device, [Hq][T], written, or NULL                     */
+    void *workspace;
+    int64_t workspace_bytes;
+} cf_attn_paged_params;
+/* Errors: as cf_attn_fwd for what the two have in common; the ranges above -> CF_EINVAL. */
+int64_t cf_attn_paged_workspace_bytes(const cf_attn_paged_params *p);
+int cf_attn_paged_fwd(const cf_attn_paged_params *p, void *hip_stream);
+
+/*
+ * Writes new tokens' keys and values into the pages: row i of sequence g of k, v [T][Hkv][D] goes to key position kv_lens[g] - Lq_g + i
+ * (kv_lens already counts the new tokens).  Rows whose position is negative, behind the table's last column or in no page are dropped; so
+ * are rows from cu_seqlens_q[n_seqs] on.  Two rows of a call may not go to the same place.  Everything else in the pages stays.
+ */
+typedef struct {
+    int32_t dtype, n_kv_heads, head_dim;
+    int32_t n_tokens, n_seqs;
+    int32_t pages_per_seq, page_size, n_pages;
+    int64_t table_stride;
+    const int32_t *cu_seqlens_q, *kv_lens, *block_table;
+    const void *k, *v;                  /* device, [T][Hkv][D], same strides for both            */
+    int64_t kv_stride_tok, kv_stride_head;
+    void *k_pages, *v_pages;
+    int64_t page_stride, page_stride_tok, page_stride_head;
+} cf_kv_append_params;
+int cf_kv_append(const cf_kv_append_params *p, void *hip_stream);
+
+/*
  * Measurement aid (not part of the paper's method): when both events (hipEvent_t, created by the
  * caller with timing enabled) are non-NULL, the NEXT cf_attn_fwd / cf_attn_bwd call on this thread
  * records `start` right before and `stop` right after its main kernel (forward: the attention

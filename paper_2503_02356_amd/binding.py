@@ -21,7 +21,8 @@ CF_PLAN_MERGE_TAILS = 1
 
 EXPORTS = ["cf_last_error", "cf_version", "cf_build_chunks", "cf_build_chunks_ex", "cf_attn_q_tiles", "cf_plan_free", "cf_plan_get",
            "cf_build_schedule", "cf_schedule_stats", "cf_attn_fwd", "cf_attn_bwd_workspace_bytes", "cf_attn_bwd", "cf_attn_fwd_batch", "cf_attn_bwd_batch",
-           "cf_attn_calls", "cf_attn_window_fwd", "cf_attn_window_bwd", "cf_attn_window_bwd_workspace_bytes", "cf_count_window_pairs", "cf_count_pairs", "cf_profile_next_call", "cf_attn_bwd_static", "cf_sim_1f1b", "cf_sim_1f1b_sequences"]
+           "cf_attn_calls", "cf_attn_window_fwd", "cf_attn_window_bwd", "cf_attn_window_bwd_workspace_bytes", "cf_count_window_pairs",
+           "cf_attn_paged_fwd", "cf_attn_paged_workspace_bytes", "cf_kv_append", "cf_count_pairs", "cf_profile_next_call", "cf_attn_bwd_static", "cf_sim_1f1b", "cf_sim_1f1b_sequences"]
 
 
 class CfError(RuntimeError):
@@ -82,6 +83,28 @@ class AttnWindow(C.Structure):
     _fields_ = [("window", C.c_int32), ("n_sinks", C.c_int32)]
 
 
+class AttnPagedParams(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("flags", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("softmax_scale", C.c_float), ("n_tokens", C.c_int32), ("n_seqs", C.c_int32),
+                ("cu_seqlens_q", C.c_void_p), ("kv_lens", C.c_void_p), ("block_table", C.c_void_p), ("table_stride", C.c_int64),
+                ("pages_per_seq", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_kv_len", C.c_int32),
+                ("window", C.c_int32), ("n_sinks", C.c_int32),
+                ("q", C.c_void_p), ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64),
+                ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_int64), ("kv_stride_tok", C.c_int64),
+                ("kv_stride_head", C.c_int64),
+                ("o", C.c_void_p), ("o_stride_tok", C.c_int64), ("o_stride_head", C.c_int64), ("lse", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class KvAppendParams(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("n_tokens", C.c_int32), ("n_seqs", C.c_int32),
+                ("pages_per_seq", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("table_stride", C.c_int64),
+                ("cu_seqlens_q", C.c_void_p), ("kv_lens", C.c_void_p), ("block_table", C.c_void_p),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("kv_stride_tok", C.c_int64), ("kv_stride_head", C.c_int64),
+                ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_stride", C.c_int64), ("page_stride_tok", C.c_int64),
+                ("page_stride_head", C.c_int64)]
+
+
 _lib = None
 
 
@@ -117,6 +140,10 @@ def lib():
         L.cf_attn_window_bwd_workspace_bytes.restype = C.c_int64
         L.cf_count_window_pairs.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(AttnWindow)]
         L.cf_count_window_pairs.restype = C.c_int64
+        L.cf_attn_paged_workspace_bytes.argtypes = [C.POINTER(AttnPagedParams)]
+        L.cf_attn_paged_workspace_bytes.restype = C.c_int64
+        L.cf_attn_paged_fwd.argtypes = [C.POINTER(AttnPagedParams), C.c_void_p]
+        L.cf_kv_append.argtypes = [C.POINTER(KvAppendParams), C.c_void_p]
         L.cf_schedule_stats.argtypes = [C.c_void_p, C.c_int32, C.POINTER(SchedStats)]
         L.cf_profile_next_call.argtypes = [C.c_void_p, C.c_void_p]
         L.cf_count_pairs.argtypes = [C.c_void_p, C.c_void_p, C.c_int32]
@@ -398,3 +425,72 @@ def cf_attn_window_bwd_workspace_bytes(params, window, n_sinks=0):
 
 def cf_attn_window_bwd(params, window, n_sinks=0, stream=None):
     _check(lib().cf_attn_window_bwd(C.byref(params), _window(window, n_sinks), stream if stream is not None else _stream()))
+
+
+def _check_paged(cu_q, kv_lens, block_table, k_pages, v_pages):
+    for t in (cu_q, kv_lens, block_table):
+        assert t.is_cuda and t.element_size() == 4 and not t.is_floating_point()
+    assert cu_q.is_contiguous() and kv_lens.is_contiguous() and block_table.stride(1) == 1
+    assert block_table.shape[0] == kv_lens.numel() == cu_q.numel() - 1
+    assert k_pages.is_cuda and k_pages.stride(3) == 1 and k_pages.stride() == v_pages.stride() and k_pages.shape == v_pages.shape
+
+
+def make_paged_params(q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, scale, max_kv_len=0, window=0, n_sinks=0, flags=0,
+                      workspace=None):
+    """q, o [T,Hq,D]; k_pages, v_pages [n_pages,page_size,Hkv,D]; lse [Hq,T] fp32 or None; cu_q [n_seqs+1], kv_lens [n_seqs], block_table
+    [n_seqs,pages] int32 device tensors.  workspace: uint8 device tensor, or None: one of the size that the call needs is made here and
+    kept with the parameters."""
+    import torch
+    T, Hq, D = q.shape
+    _check_paged(cu_q, kv_lens, block_table, k_pages, v_pages)
+    assert q.is_cuda and q.stride(2) == 1 and o.stride(2) == 1 and q.dtype == k_pages.dtype == v_pages.dtype == o.dtype
+    assert o.shape == q.shape and k_pages.shape[3] == D
+    assert lse is None or (lse.is_contiguous() and tuple(lse.shape) == (Hq, T) and lse.dtype == torch.float32)
+    p = AttnPagedParams()
+    p.dtype, p.flags, p.n_q_heads, p.n_kv_heads, p.head_dim = _dtype_code(q), int(flags), Hq, k_pages.shape[2], D
+    p.softmax_scale, p.n_tokens, p.n_seqs = float(scale), T, kv_lens.numel()
+    p.cu_seqlens_q, p.kv_lens, p.block_table = cu_q.data_ptr(), kv_lens.data_ptr(), block_table.data_ptr()
+    p.table_stride, p.pages_per_seq = block_table.stride(0) if block_table.shape[0] > 1 else block_table.shape[1], block_table.shape[1]
+    p.page_size, p.n_pages, p.max_kv_len = k_pages.shape[1], k_pages.shape[0], int(max_kv_len)
+    p.window, p.n_sinks = int(window), int(n_sinks)
+    p.q, p.q_stride_tok, p.q_stride_head = q.data_ptr(), q.stride(0), q.stride(1)
+    p.k_pages, p.v_pages = k_pages.data_ptr(), v_pages.data_ptr()
+    p.page_stride, p.kv_stride_tok, p.kv_stride_head = k_pages.stride(0), k_pages.stride(1), k_pages.stride(2)
+    p.o, p.o_stride_tok, p.o_stride_head = o.data_ptr(), o.stride(0), o.stride(1)
+    p.lse = lse.data_ptr() if lse is not None else None
+    if workspace is None:
+        need = cf_attn_paged_workspace_bytes(p)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    if workspace is not None:
+        p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    p._keepalive = (q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, workspace)      # see make_fwd_params
+    return p
+
+
+def cf_attn_paged_workspace_bytes(params):
+    return _check(lib().cf_attn_paged_workspace_bytes(C.byref(params)))
+
+
+def cf_attn_paged_fwd(params, stream=None):
+    _check(lib().cf_attn_paged_fwd(C.byref(params), stream if stream is not None else _stream()))
+
+
+def make_kv_append_params(k, v, k_pages, v_pages, cu_q, kv_lens, block_table):
+    """k, v [T,Hkv,D] (views with the same strides); the rest as in make_paged_params."""
+    _check_paged(cu_q, kv_lens, block_table, k_pages, v_pages)
+    assert k.is_cuda and k.stride(2) == 1 and k.stride() == v.stride() and k.shape == v.shape
+    assert k.dtype == v.dtype == k_pages.dtype == v_pages.dtype and tuple(k.shape[1:]) == tuple(k_pages.shape[2:])
+    p = KvAppendParams()
+    p.dtype, p.n_kv_heads, p.head_dim, p.n_tokens, p.n_seqs = _dtype_code(k), k.shape[1], k.shape[2], k.shape[0], kv_lens.numel()
+    p.pages_per_seq, p.page_size, p.n_pages = block_table.shape[1], k_pages.shape[1], k_pages.shape[0]
+    p.table_stride = block_table.stride(0) if block_table.shape[0] > 1 else block_table.shape[1]
+    p.cu_seqlens_q, p.kv_lens, p.block_table = cu_q.data_ptr(), kv_lens.data_ptr(), block_table.data_ptr()
+    p.k, p.v, p.kv_stride_tok, p.kv_stride_head = k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1)
+    p.k_pages, p.v_pages = k_pages.data_ptr(), v_pages.data_ptr()
+    p.page_stride, p.page_stride_tok, p.page_stride_head = k_pages.stride(0), k_pages.stride(1), k_pages.stride(2)
+    p._keepalive = (k, v, k_pages, v_pages, cu_q, kv_lens, block_table)      # see make_fwd_params
+    return p
+
+
+def cf_kv_append(params, stream=None):
+    _check(lib().cf_kv_append(C.byref(params), stream if stream is not None else _stream()))

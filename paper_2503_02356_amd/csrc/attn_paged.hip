@@ -1,0 +1,221 @@
+// Attention of new tokens over a paged cache, and writing into the cache.
+//
+// Scalar kernels: one wavefront per (query row, head), pair by pair, fp32 arithmetic.  They serve the cross-check flag and what the matrix
+// kernels do not cover.  Tiles of 64 keys are gone through in order, a lane to a key; a hidden key is never read.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "common.h"
+#include "pages.h"
+#include "scalar_rows.h"
+
+namespace cf {
+namespace {
+
+constexpr int kWaves = 4;        // wavefronts per workgroup of the scalar kernels
+
+struct PagedArgs {
+    cf_attn_paged_params p;
+    WindowMask mask;             // no window: one of all keys
+    int shift;                   // log2(page_size)
+    __device__ __forceinline__ PageTable table(int seq) const
+    {
+        return PageTable{p.block_table + (int64_t)seq * p.table_stride, p.pages_per_seq, shift, p.n_pages};
+    }
+    __device__ __forceinline__ NewRows rows(int seq) const { return NewRows(p.cu_seqlens_q[seq], p.cu_seqlens_q[seq + 1], p.kv_lens[seq]); }
+};
+
+// One row's softmax over the visible keys of tiles [first, end) of `tiles`: maximum (natural units), sum and unnormalised result, element
+// lane + 64 t.
+template <typename T, int D>
+struct RowSums {
+    float m = -INFINITY, z = 0.f, acc[D / 64] = {};
+};
+template <typename T, int D, int UNROLL, typename Q>
+__device__ inline RowSums<T, D> paged_row(const PagedArgs &a, const PageTable &table, int position, int kh, const KeyTiles<64, WindowMask> &tiles,
+                                          int first, int end, Q q)
+{
+    const cf_attn_paged_params &p = a.p;
+    const int lane = threadIdx.x & 63;
+    RowSums<T, D> r;
+    for (int t = first; t < end; ++t) {
+        const int j = tiles.start(t) + lane;
+        const bool seen = j <= position && (j > position - a.mask.window || j < a.mask.sinks);
+        const int page = seen ? table.page_of(j) : -1;
+        const int64_t at = (int64_t)max(page, 0) * p.page_stride + (int64_t)table.row_in_page(j) * p.kv_stride_tok + (int64_t)kh * p.kv_stride_head;
+        float s = -INFINITY;
+        if (page >= 0) {
+            const T *k = (const T *)p.k_pages + at;
+            float d = 0.f;
+            for_elements<D, UNROLL>([&](int x) { d += q(x) * ld(k + x); });
+            s = d * p.softmax_scale;
+        }
+        const unsigned long long some = __ballot(page >= 0);
+        if (some == 0) continue;
+        const float m_new = fmaxf(r.m, wave_max(s)), ref = m_new == -INFINITY ? 0.f : m_new;
+        const float pr = page >= 0 ? expf(s - ref) : 0.f, corr = expf(r.m - ref);
+        r.z = r.z * corr + wave_sum(pr);
+        for (int x = 0; x < D / 64; ++x) r.acc[x] *= corr;
+        for (unsigned long long left = some; left != 0; left &= left - 1) {
+            const int jj = __ffsll((long long)left) - 1;
+            const float pj = __shfl(pr, jj);
+            const int64_t row = __shfl(at, jj);
+            const T *v = (const T *)p.v_pages + row;
+            for (int x = 0; x < D / 64; ++x) r.acc[x] += pj * ld(v + lane + 64 * x);
+        }
+        r.m = m_new;
+    }
+    return r;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(PagedArgs a)
+{
+    const cf_attn_paged_params &p = a.p;
+    __shared__ float sq[kWaves][D];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, h = blockIdx.y;
+    const int64_t row = (int64_t)blockIdx.x * kWaves + wave;
+    if (row >= min(p.n_tokens, p.cu_seqlens_q[p.n_seqs])) return;      // whole wavefront leaves together; no barrier below
+    const int seq = find_segment(p.cu_seqlens_q, p.n_seqs, (int)row);
+    const NewRows rows = a.rows(seq);
+    const PageTable table = a.table(seq);
+    const int position = rows.position((int)row - rows.q0);
+    const T *q = row_of<T>(p.q, (int)row, p.q_stride_tok, h, p.q_stride_head);
+    for (int t = 0; t < D / 64; ++t) sq[wave][lane + 64 * t] = ld(q + lane + 64 * t);
+    __builtin_amdgcn_wave_barrier();
+    const KeyTiles<64, WindowMask> tiles(a.mask, position, at_most(position + 1, table.capacity()));
+    const RowSums<T, D> r = paged_row<T, D, 0>(a, table, position, h / (p.n_q_heads / p.n_kv_heads), tiles, 0, tiles.n, [&](int x) { return sq[wave][x]; });
+    T *o = (T *)p.o + row * p.o_stride_tok + (int64_t)h * p.o_stride_head;
+    const bool none = r.m == -INFINITY && r.z == 0.f;
+    for (int t = 0; t < D / 64; ++t) st(o + lane + 64 * t, none ? 0.f : r.acc[t] / r.z);
+    if (lane == 0 && p.lse) p.lse[(int64_t)h * p.n_tokens + row] = none ? -INFINITY : r.m + logf(r.z);
+}
+
+// 16 bytes a thread: a token's key (blockIdx.y 0) or value row, all heads.
+__global__ __launch_bounds__(256) void kv_append_kernel(cf_kv_append_params p, int shift, int units)
+{
+    const int bytes = p.dtype == CF_BF16 ? 2 : 4, per_row = units * p.n_kv_heads;      // units: 16-byte pieces of a head's row
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = id / per_row;
+    if (row >= min(p.n_tokens, p.cu_seqlens_q[p.n_seqs])) return;
+    const int rest = (int)(id - row * per_row), h = rest / units, unit = rest - h * units;
+    const int seq = find_segment(p.cu_seqlens_q, p.n_seqs, (int)row);
+    const NewRows rows(p.cu_seqlens_q[seq], p.cu_seqlens_q[seq + 1], p.kv_lens[seq]);
+    const PageTable table{p.block_table + (int64_t)seq * p.table_stride, p.pages_per_seq, shift, p.n_pages};
+    const int position = rows.position((int)row - rows.q0), page = table.page_of(position);
+    if (page < 0) return;
+    const char *from = (const char *)(blockIdx.y ? p.v : p.k) + (row * p.kv_stride_tok + (int64_t)h * p.kv_stride_head) * bytes;
+    char *to = (char *)(blockIdx.y ? p.v_pages : p.k_pages) +
+               ((int64_t)page * p.page_stride + (int64_t)table.row_in_page(position) * p.page_stride_tok + (int64_t)h * p.page_stride_head) * bytes;
+    ((uint4 *)to)[unit] = ((const uint4 *)from)[unit];
+}
+
+template <typename T, int D>
+hipError_t run_rows(const PagedArgs &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)(((int64_t)a.p.n_tokens + kWaves - 1) / kWaves), (unsigned)a.p.n_q_heads);
+    paged_rows_kernel<T, D><<<grid, kWaves * 64, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) % n) == 0; }
+
+int check_common(const char *who, int dtype, int D, int n_tokens, int n_seqs, const int32_t *cu, const int32_t *lens, const int32_t *table,
+                 int64_t table_stride, int pages, int page_size, int n_pages)
+{
+    if (dtype != CF_BF16 && dtype != CF_FP32) return fail(CF_EUNSUPPORTED, "%s: dtype %d not supported", who, dtype);
+    if (D != 64 && D != 128) return fail(CF_EUNSUPPORTED, "%s: head_dim %d not supported (64 or 128)", who, D);
+    if (n_tokens < 1 || n_seqs < 1) return fail(CF_EINVAL, "%s: need n_tokens >= 1 and n_seqs >= 1 (got %d, %d)", who, n_tokens, n_seqs);
+    if (page_size < 16 || page_size > 65536 || (page_size & (page_size - 1)))
+        return fail(CF_EINVAL, "%s: page_size %d must be a power of two from 16 to 65536", who, page_size);
+    if (n_pages < 1 || pages < 1 || (int64_t)pages * page_size > 0x7fffffffLL || table_stride < pages)
+        return fail(CF_EINVAL, "%s: need n_pages >= 1, 1 <= pages_per_seq <= table_stride, pages_per_seq * page_size < 2^31 (got %d, %d, %lld)", who,
+                    n_pages, pages, (long long)table_stride);
+    if (!cu || !lens || !table) return fail(CF_EINVAL, "%s: NULL device pointer", who);
+    if (!aligned(cu, 4) || !aligned(lens, 4) || !aligned(table, 4)) return fail(CF_EINVAL, "%s: misaligned descriptor", who);
+    return CF_OK;
+}
+
+int check_strides(const char *who, int dtype, int D, std::initializer_list<int64_t> strides)
+{
+    const int64_t vec = dtype == CF_BF16 ? 8 : 4;
+    for (int64_t s : strides)
+        if (s < D || s % vec != 0)
+            return fail(CF_EINVAL, "%s: stride %lld must be >= head_dim and a multiple of %lld elements", who, (long long)s, (long long)vec);
+    return CF_OK;
+}
+
+int check_paged(const cf_attn_paged_params *p, const char *who, bool sizes_only, PagedArgs *a)
+{
+    if (!p) return fail(CF_EINVAL, "%s: params is NULL", who);
+    if (p->n_q_heads < 1 || p->n_kv_heads < 1 || p->n_q_heads % p->n_kv_heads != 0 || p->n_q_heads > 65535)
+        return fail(CF_EINVAL, "%s: n_q_heads %d must be a positive multiple of n_kv_heads %d, at most 65535", who, p->n_q_heads, p->n_kv_heads);
+    static const int32_t dummy[1] = {0};
+    const int32_t *cu = sizes_only ? dummy : p->cu_seqlens_q, *lens = sizes_only ? dummy : p->kv_lens, *table = sizes_only ? dummy : p->block_table;
+    if (int rc = check_common(who, p->dtype, p->head_dim, p->n_tokens, p->n_seqs, cu, lens, table, p->table_stride, p->pages_per_seq, p->page_size,
+                              p->n_pages))
+        return rc;
+    if ((int64_t)p->n_tokens * p->n_q_heads > 0x7fffffffLL)
+        return fail(CF_EINVAL, "%s: n_tokens * n_q_heads = %lld must be below 2^31", who, (long long)p->n_tokens * p->n_q_heads);
+    if (p->flags & ~CF_FLAG_SCALAR_KERNELS) return fail(CF_EINVAL, "%s: unknown flags 0x%x", who, p->flags);
+    if (p->max_kv_len < 0 || p->window < 0 || p->n_sinks < 0 || (p->window == 0 && p->n_sinks != 0))
+        return fail(CF_EINVAL, "%s: need max_kv_len, window, n_sinks >= 0 and no sinks without a window (got %d, %d, %d)", who, p->max_kv_len, p->window,
+                    p->n_sinks);
+    a->p = *p;
+    const int capacity = p->pages_per_seq * p->page_size;
+    a->mask = p->window == 0 ? WindowMask{0x7fffffff, 0} : WindowMask{p->window, std::min(p->n_sinks, capacity)};
+    a->shift = __builtin_ctz((unsigned)p->page_size);
+    if (sizes_only) return CF_OK;
+    if (!p->q || !p->k_pages || !p->v_pages || !p->o) return fail(CF_EINVAL, "%s: NULL device pointer", who);
+    if (!(p->softmax_scale - p->softmax_scale == 0.f)) return fail(CF_EINVAL, "%s: softmax_scale is not finite", who);
+    if (int rc = check_strides(who, p->dtype, p->head_dim, {p->q_stride_tok, p->q_stride_head, p->page_stride, p->kv_stride_tok, p->kv_stride_head,
+                                                            p->o_stride_tok, p->o_stride_head}))
+        return rc;
+    if (!aligned(p->q, 16) || !aligned(p->k_pages, 16) || !aligned(p->v_pages, 16) || !aligned(p->o, 16) || !aligned(p->lse, 4))
+        return fail(CF_EINVAL, "%s: q, pages and o must be 16-byte aligned", who);
+    return CF_OK;
+}
+
+}  // namespace
+}  // namespace cf
+
+extern "C" int64_t cf_attn_paged_workspace_bytes(const cf_attn_paged_params *p)
+{
+    cf::PagedArgs a;
+    if (int rc = cf::check_paged(p, "cf_attn_paged_workspace_bytes", true, &a)) return rc;
+    return 0;
+}
+
+extern "C" int cf_attn_paged_fwd(const cf_attn_paged_params *p, void *hip_stream)
+{
+    const char *who = "cf_attn_paged_fwd";
+    cf::PagedArgs a;
+    if (int rc = cf::check_paged(p, who, false, &a)) return rc;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    hipError_t e;
+    if (p->dtype == CF_FP32) e = p->head_dim == 64 ? cf::run_rows<float, 64>(a, s) : cf::run_rows<float, 128>(a, s);
+    else e = p->head_dim == 64 ? cf::run_rows<unsigned short, 64>(a, s) : cf::run_rows<unsigned short, 128>(a, s);
+    return e == hipSuccess ? CF_OK : cf::fail(CF_EHIP, "%s: %s", who, hipGetErrorString(e));
+}
+
+extern "C" int cf_kv_append(const cf_kv_append_params *p, void *hip_stream)
+{
+    const char *who = "cf_kv_append";
+    if (!p) return cf::fail(CF_EINVAL, "%s: params is NULL", who);
+    if (p->n_kv_heads < 1 || p->n_kv_heads > 65535) return cf::fail(CF_EINVAL, "%s: n_kv_heads %d must be from 1 to 65535", who, p->n_kv_heads);
+    if (int rc = cf::check_common(who, p->dtype, p->head_dim, p->n_tokens, p->n_seqs, p->cu_seqlens_q, p->kv_lens, p->block_table, p->table_stride,
+                                  p->pages_per_seq, p->page_size, p->n_pages))
+        return rc;
+    if (!p->k || !p->v || !p->k_pages || !p->v_pages) return cf::fail(CF_EINVAL, "%s: NULL device pointer", who);
+    if (int rc = cf::check_strides(who, p->dtype, p->head_dim, {p->kv_stride_tok, p->kv_stride_head, p->page_stride, p->page_stride_tok, p->page_stride_head}))
+        return rc;
+    if (!cf::aligned(p->k, 16) || !cf::aligned(p->v, 16) || !cf::aligned(p->k_pages, 16) || !cf::aligned(p->v_pages, 16))
+        return cf::fail(CF_EINVAL, "%s: k, v and pages must be 16-byte aligned", who);
+    const int units = p->head_dim * (p->dtype == CF_BF16 ? 2 : 4) / 16;
+    const int64_t blocks = ((int64_t)p->n_tokens * p->n_kv_heads * units + 255) / 256;
+    if (blocks * 256 > 0xffffffffLL) return cf::fail(CF_EINVAL, "%s: %d tokens of %d heads are more than one launch holds", who, p->n_tokens, p->n_kv_heads);
+    cf::kv_append_kernel<<<dim3((unsigned)blocks, 2), 256, 0, static_cast<hipStream_t>(hip_stream)>>>(*p, __builtin_ctz((unsigned)p->page_size), units);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? CF_OK : cf::fail(CF_EHIP, "%s: %s", who, hipGetErrorString(e));
+}
