@@ -7,67 +7,12 @@
 #include <algorithm>
 
 #include "common.h"
-#include "pages.h"
-#include "scalar_rows.h"
+#include "paged.h"
 
 namespace cf {
 namespace {
 
 constexpr int kWaves = 4;        // wavefronts per workgroup of the scalar kernels
-
-struct PagedArgs {
-    cf_attn_paged_params p;
-    WindowMask mask;             // no window: one of all keys
-    int shift;                   // log2(page_size)
-    __device__ __forceinline__ PageTable table(int seq) const
-    {
-        return PageTable{p.block_table + (int64_t)seq * p.table_stride, p.pages_per_seq, shift, p.n_pages};
-    }
-    __device__ __forceinline__ NewRows rows(int seq) const { return NewRows(p.cu_seqlens_q[seq], p.cu_seqlens_q[seq + 1], p.kv_lens[seq]); }
-};
-
-// One row's softmax over the visible keys of tiles [first, end) of `tiles`: maximum (natural units), sum and unnormalised result, element
-// lane + 64 t.
-template <typename T, int D>
-struct RowSums {
-    float m = -INFINITY, z = 0.f, acc[D / 64] = {};
-};
-template <typename T, int D, int UNROLL, typename Q>
-__device__ inline RowSums<T, D> paged_row(const PagedArgs &a, const PageTable &table, int position, int kh, const KeyTiles<64, WindowMask> &tiles,
-                                          int first, int end, Q q)
-{
-    const cf_attn_paged_params &p = a.p;
-    const int lane = threadIdx.x & 63;
-    RowSums<T, D> r;
-    for (int t = first; t < end; ++t) {
-        const int j = tiles.start(t) + lane;
-        const bool seen = j <= position && (j > position - a.mask.window || j < a.mask.sinks);
-        const int page = seen ? table.page_of(j) : -1;
-        const int64_t at = (int64_t)max(page, 0) * p.page_stride + (int64_t)table.row_in_page(j) * p.kv_stride_tok + (int64_t)kh * p.kv_stride_head;
-        float s = -INFINITY;
-        if (page >= 0) {
-            const T *k = (const T *)p.k_pages + at;
-            float d = 0.f;
-            for_elements<D, UNROLL>([&](int x) { d += q(x) * ld(k + x); });
-            s = d * p.softmax_scale;
-        }
-        const unsigned long long some = __ballot(page >= 0);
-        if (some == 0) continue;
-        const float m_new = fmaxf(r.m, wave_max(s)), ref = m_new == -INFINITY ? 0.f : m_new;
-        const float pr = page >= 0 ? expf(s - ref) : 0.f, corr = expf(r.m - ref);
-        r.z = r.z * corr + wave_sum(pr);
-        for (int x = 0; x < D / 64; ++x) r.acc[x] *= corr;
-        for (unsigned long long left = some; left != 0; left &= left - 1) {
-            const int jj = __ffsll((long long)left) - 1;
-            const float pj = __shfl(pr, jj);
-            const int64_t row = __shfl(at, jj);
-            const T *v = (const T *)p.v_pages + row;
-            for (int x = 0; x < D / 64; ++x) r.acc[x] += pj * ld(v + lane + 64 * x);
-        }
-        r.m = m_new;
-    }
-    return r;
-}
 
 template <typename T, int D>
 __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(PagedArgs a)
@@ -90,6 +35,38 @@ __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(PagedArgs a)
     const bool none = r.m == -INFINITY && r.z == 0.f;
     for (int t = 0; t < D / 64; ++t) st(o + lane + 64 * t, none ? 0.f : r.acc[t] / r.z);
     if (lane == 0 && p.lse) p.lse[(int64_t)h * p.n_tokens + row] = none ? -INFINITY : r.m + logf(r.z);
+}
+
+// O and LSE of the rows from their parts: a wavefront to a row, a lane to a part's maximum and sum, then to some elements of the result.
+// Reads each part once; the parts' order is fixed, so are the bits.
+template <typename T, int D>
+__global__ __launch_bounds__(kWaves * 64) void paged_join_kernel(PagedArgs a)
+{
+    const cf_attn_paged_params &p = a.p;
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = (int64_t)min(p.n_tokens, p.cu_seqlens_q[p.n_seqs]) * p.n_q_heads, all = (int64_t)p.n_tokens * p.n_q_heads;
+    const int64_t r = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (r >= rows) return;
+    float2 ml = {-INFINITY, 0.f};
+    if (lane < a.parts) ml = a.part_ml[r * a.parts + lane];
+    const float M = wave_max(ml.x), ref = M == -INFINITY ? 0.f : M;
+    const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - ref);
+    const float L = wave_sum(w * ml.y);
+    constexpr int E = D / 64;
+    float acc[E] = {};
+    for (unsigned long long left = __ballot(ml.x != -INFINITY); left != 0; left &= left - 1) {
+        const int x = __ffsll((long long)left) - 1;
+        const float wx = __shfl(w, x);
+        const float *o = a.part_o + ((int64_t)x * all + r) * D;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += wx * o[lane * E + e];
+    }
+    const int64_t row = r / p.n_q_heads, h = r - row * p.n_q_heads;
+    T *o = (T *)p.o + row * p.o_stride_tok + h * p.o_stride_head;
+    const float inv = M == -INFINITY ? 0.f : 1.f / L;
+#pragma unroll
+    for (int e = 0; e < E; ++e) st(o + lane * E + e, acc[e] * inv);
+    if (lane == 0 && p.lse) p.lse[h * p.n_tokens + row] = M == -INFINITY ? -INFINITY : __builtin_fmaf(M, 0.69314718055994530942f, logf(L));
 }
 
 // 16 bytes a thread: a token's key (blockIdx.y 0) or value row, all heads.
@@ -116,6 +93,13 @@ hipError_t run_rows(const PagedArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)(((int64_t)a.p.n_tokens + kWaves - 1) / kWaves), (unsigned)a.p.n_q_heads);
     paged_rows_kernel<T, D><<<grid, kWaves * 64, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t run_join(const PagedArgs &a, hipStream_t s)
+{
+    paged_join_kernel<T, D><<<dim3((unsigned)(((int64_t)a.p.n_tokens * a.p.n_q_heads + kWaves - 1) / kWaves)), kWaves * 64, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -177,14 +161,42 @@ int check_paged(const cf_attn_paged_params *p, const char *who, bool sizes_only,
     return CF_OK;
 }
 
+// Largest launch, in work-items: a HIP launch holds fewer than 2^32.
+bool launchable(const PagedArgs &a)
+{
+    const int64_t tiles = (int64_t)a.p.n_tokens * (a.p.n_q_heads / a.p.n_kv_heads) / 128 + a.p.n_seqs;
+    return tiles * a.p.n_kv_heads * a.parts * 256 <= 0xffffffffLL;
+}
+// The matrix kernel's offsets inside a group of 16 keys have 32 bits.  (Wider rows and calls beyond one launch: a wavefront to a row.)
+bool use_mfma(const PagedArgs &a)
+{
+    return a.p.dtype == CF_BF16 && !(a.p.flags & CF_FLAG_SCALAR_KERNELS) && a.p.kv_stride_tok < (1 << 25) && launchable(a);
+}
+// Chooses the parts; bytes of workspace.
+int64_t cut(PagedArgs &a)
+{
+    a.parts = 1, a.tiles_per_part = 0x7fffffff, a.part_o = nullptr, a.part_ml = nullptr;
+    if (a.p.dtype == CF_BF16 && !(a.p.flags & CF_FLAG_SCALAR_KERNELS)) cut_paged_mfma(a);
+    if (a.parts == 1) return 0;
+    const int64_t rows = (int64_t)a.p.n_tokens * a.p.n_q_heads;
+    return a.parts * rows * (a.p.head_dim * 4 + 8);
+}
+
 }  // namespace
+
+hipError_t launch_paged_join(const PagedArgs &a, hipStream_t s)
+{
+    if (a.p.dtype == CF_FP32) return a.p.head_dim == 64 ? run_join<float, 64>(a, s) : run_join<float, 128>(a, s);
+    return a.p.head_dim == 64 ? run_join<unsigned short, 64>(a, s) : run_join<unsigned short, 128>(a, s);
+}
+
 }  // namespace cf
 
 extern "C" int64_t cf_attn_paged_workspace_bytes(const cf_attn_paged_params *p)
 {
     cf::PagedArgs a;
     if (int rc = cf::check_paged(p, "cf_attn_paged_workspace_bytes", true, &a)) return rc;
-    return 0;
+    return cf::cut(a);
 }
 
 extern "C" int cf_attn_paged_fwd(const cf_attn_paged_params *p, void *hip_stream)
@@ -192,9 +204,20 @@ extern "C" int cf_attn_paged_fwd(const cf_attn_paged_params *p, void *hip_stream
     const char *who = "cf_attn_paged_fwd";
     cf::PagedArgs a;
     if (int rc = cf::check_paged(p, who, false, &a)) return rc;
+    const int64_t need = cf::cut(a);
+    if (need > 0) {
+        if (!p->workspace || !cf::aligned(p->workspace, 256)) return cf::fail(CF_EINVAL, "%s: workspace must be non-NULL and 256-byte aligned", who);
+        if (p->workspace_bytes < need)
+            return cf::fail(CF_EINVAL, "%s: workspace has %lld bytes, %lld needed", who, (long long)p->workspace_bytes, (long long)need);
+        a.part_o = static_cast<float *>(p->workspace);
+        a.part_ml = reinterpret_cast<float2 *>(a.part_o + (int64_t)a.parts * p->n_tokens * p->n_q_heads * p->head_dim);
+    }
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     hipError_t e;
-    if (p->dtype == CF_FP32) e = p->head_dim == 64 ? cf::run_rows<float, 64>(a, s) : cf::run_rows<float, 128>(a, s);
+    if (cf::use_mfma(a)) {
+        e = cf::launch_paged_mfma(a, s);
+        if (e == hipSuccess && a.parts > 1) e = cf::launch_paged_join(a, s);
+    } else if (p->dtype == CF_FP32) e = p->head_dim == 64 ? cf::run_rows<float, 64>(a, s) : cf::run_rows<float, 128>(a, s);
     else e = p->head_dim == 64 ? cf::run_rows<unsigned short, 64>(a, s) : cf::run_rows<unsigned short, 128>(a, s);
     return e == hipSuccess ? CF_OK : cf::fail(CF_EHIP, "%s: %s", who, hipGetErrorString(e));
 }

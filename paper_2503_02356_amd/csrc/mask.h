@@ -76,7 +76,7 @@ struct KeyTiles<TILE, WindowMask> {
         const int first = at_least(0, first_position + 1 - m.window);
         sinks = (at_most(m.sinks, first) + TILE - 1) / TILE;
         gap = at_least(0, first / TILE - sinks);
-        n = (keys + TILE - 1) / TILE - gap;
+        n = at_least((keys + TILE - 1) / TILE - gap, sinks);        // (keys: fewer than the positions where a cache holds fewer)
     }
     CF_BOTH int start(int t) const { return (t < sinks ? t : t + gap) * TILE; }
     CF_BOTH int next(int t, int) const { return start(t + 1); }

@@ -142,13 +142,14 @@ def test_pages_that_are_none(dtype, D, flags):
     assert (got["o"][43 + 20:43 + 22] == 0).all() and torch.isinf(got["lse"][:, 63:65]).all() and (got["o"][40:43] == 0).all()
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (30, 20), (60, 3)])
 @pytest.mark.parametrize("dtype,D,flags", KINDS)
-def test_lengths_beyond_the_table(dtype, D, flags):
+def test_lengths_beyond_the_table(dtype, D, flags, window, sinks):
     """kv_lens may promise more keys than the table has columns for; those are hidden."""
-    b = Batch([(4, 100), (1, 64)], 4, 2, D, dtype, 16, seed=4)
+    b = Batch([(4, 100), (1, 64), (40, 300)], 4, 2, D, dtype, 16, window, sinks, seed=4)
     b.append()
     narrow = b.table[:, :3]                          # 48 keys of each
-    p = B.make_paged_params(b.q, b.kp, b.vp, b.o, b.lse, b.cu, b.lens, narrow, b.scale, flags=flags)
+    p = B.make_paged_params(b.q, b.kp, b.vp, b.o, b.lse, b.cu, b.lens, narrow, b.scale, window=window, n_sinks=sinks, flags=flags)
     B.cf_attn_paged_fwd(p)
     torch.cuda.synchronize()
     b.table_host = b.table_host.copy()

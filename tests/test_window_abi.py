@@ -151,6 +151,9 @@ int main()
                                 return printf("rows that see\n"), 1;
                     ++n;
                 }
+    const WindowMask few = {10, 20};                                 // a row far behind the last key that there is: its sinks
+    const KeyTiles<16, WindowMask> left(few, 500, 48);
+    if (left.n != 2 || left.start(0) != 0 || left.start(1) != 16) return printf("sinks\n"), 1;
     const int far = 0x7fffffff;                                      // the largest sizes leave no 32 bits
     const WindowMask m = {far, far};
     const KeysOfRow<WindowMask> k(m, far - 1);
