@@ -954,14 +954,22 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
 #pragma unroll
                         for (int i = 0; i < NS; ++i) {
                             float pv = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / F::R][qb][i % F::R], c2, -lse2[qb]));
-                            bool hidden = need_mask && mb * 32 + F::place(i) - F::M * qb > lim;
-                            if constexpr (Mask::windowed) {
-                                const int key = mb * 32 + F::place(i);
-                                hidden = hidden || (key - F::M * qb <= lim - mask.window && key >= mask.sinks - tile_start - group * 4);
-                            }
+                            const bool hidden = need_mask && mb * 32 + F::place(i) - F::M * qb > lim;
                             if (hidden) pv = 0.f;
+                            if constexpr (Mask::windowed) {
+                                const bool between = (unsigned)(mb * 32 + F::place(i) - (mask.sinks - tile_start - group * 4)) < hidden_keys(mask, amax + F::M * qb);
+                                if (between) pv = 0.f;
+                                if (DELTA_PASS) {        // (dP of a hidden pair may be anything)
+                                    float x = hidden ? 0.f : pv * dp[i / F::R][qb][i % F::R];
+                                    if (between) x = 0.f;
+                                    dsum[qb] += x;
+                                } else {
+                                    dp[i / F::R][qb][i % F::R] = pv * (dp[i / F::R][qb][i % F::R] - dlt[qb]);
+                                }
+                                continue;
+                            }
                             // (dP of a hidden pair may be anything)
-                            if (DELTA_PASS) dsum[qb] += (D == 64 || Mask::windowed) && hidden ? 0.f : pv * dp[i / F::R][qb][i % F::R];
+                            if (DELTA_PASS) dsum[qb] += D == 64 && hidden ? 0.f : pv * dp[i / F::R][qb][i % F::R];
                             else dp[i / F::R][qb][i % F::R] = pv * (dp[i / F::R][qb][i % F::R] - dlt[qb]);
                         }
                     if (DELTA_PASS) continue;

@@ -173,12 +173,14 @@ __device__ __forceinline__ void fwd_body(const cf_attn_fwd_params &p, int id, ch
             }
             if constexpr (Mask::windowed) {
                 if (crosses_window(mask, wq0 + off, tile_start, BN)) {
-                    const int far = amax - mask.window - tile_start - group * 4, sink = mask.sinks - tile_start - group * 4;
+                    const int from = mask.sinks - tile_start - group * 4;
 #pragma unroll
-                    for (int qb = 0; qb < QB; ++qb)
+                    for (int qb = 0; qb < QB; ++qb) {
+                        const unsigned gap = hidden_keys(mask, amax + F::M * qb);
 #pragma unroll
                         for (int i = 0; i < NS; ++i)
-                            if (F::place(i) - F::M * qb <= far && F::place(i) >= sink) s[i / F::R][qb][i % F::R] = -INFINITY;
+                            if ((unsigned)(F::place(i) - from) < gap) s[i / F::R][qb][i % F::R] = -INFINITY;
+                    }
                 }
             }
             // ---- online softmax (log2 domain)

@@ -52,14 +52,22 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join_kernel(PagedArgs a)
     const float M = wave_max(ml.x), ref = M == -INFINITY ? 0.f : M;
     const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - ref);
     const float L = wave_sum(w * ml.y);
-    constexpr int E = D / 64;
+    // (parts without keys hold anything, and count 0 times: whatever it is, it is left out.  Eight at a time: a latency for eight)
+    constexpr int E = D / 64, AT_ONCE = 8;
     float acc[E] = {};
-    for (unsigned long long left = __ballot(ml.x != -INFINITY); left != 0; left &= left - 1) {
-        const int x = __ffsll((long long)left) - 1;
-        const float wx = __shfl(w, x);
-        const float *o = a.part_o + ((int64_t)x * all + r) * D;
+    const float *o_parts = a.part_o + r * D + lane * E;
+    for (int x0 = 0; x0 < a.parts; x0 += AT_ONCE) {
+        float v[AT_ONCE][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] += wx * o[lane * E + e];
+        for (int x = 0; x < AT_ONCE; ++x)
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[x][e] = o_parts[(int64_t)min(x0 + x, a.parts - 1) * all * D + e];
+#pragma unroll
+        for (int x = 0; x < AT_ONCE; ++x) {
+            const float wx = x0 + x < a.parts ? __shfl(w, x0 + x) : 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] += wx == 0.f ? 0.f : wx * v[x][e];
+        }
     }
     const int64_t row = r / p.n_q_heads, h = r - row * p.n_q_heads;
     T *o = (T *)p.o + row * p.o_stride_tok + h * p.o_stride_head;
@@ -161,16 +169,10 @@ int check_paged(const cf_attn_paged_params *p, const char *who, bool sizes_only,
     return CF_OK;
 }
 
-// Largest launch, in work-items: a HIP launch holds fewer than 2^32.
-bool launchable(const PagedArgs &a)
-{
-    const int64_t tiles = (int64_t)a.p.n_tokens * (a.p.n_q_heads / a.p.n_kv_heads) / 128 + a.p.n_seqs;
-    return tiles * a.p.n_kv_heads * a.parts * 256 <= 0xffffffffLL;
-}
 // The matrix kernel's offsets inside a group of 16 keys have 32 bits.  (Wider rows and calls beyond one launch: a wavefront to a row.)
 bool use_mfma(const PagedArgs &a)
 {
-    return a.p.dtype == CF_BF16 && !(a.p.flags & CF_FLAG_SCALAR_KERNELS) && a.p.kv_stride_tok < (1 << 25) && launchable(a);
+    return a.p.dtype == CF_BF16 && !(a.p.flags & CF_FLAG_SCALAR_KERNELS) && a.p.kv_stride_tok < (1 << 25) && paged_mfma_launch_size(a) <= 0xffffffffLL;
 }
 // Chooses the parts; bytes of workspace.
 int64_t cut(PagedArgs &a)

@@ -31,19 +31,60 @@ constexpr float kLazy = 8.f;                 // log2 units a row maximum may exc
 
 __device__ __align__(16) unsigned zeros[64];                 // a row of zeros
 
-// A part of a tile, as its workgroup finds it.
+// The call's arguments, loaded (again) where this is called.  What a workgroup needs only at its end would stand in scalar registers all the
+// way, and there are too few of them: those of the loops over keys would go to and fro instead.
+__device__ __forceinline__ const PagedArgs &arguments()
+{
+    auto p = (const CF_CONSTANT PagedArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const PagedArgs *)p;
+}
+
+// A tile: up to BM token-head rows of a sequence and a key/value head.
 struct TileRows {
     int seq, q0;                 // sequence, its first row of q
     int row0, rows;              // first row of the tile among the sequence's token-head rows, and how many it has
     int first_position;
+    int G, kh;                   // query heads of a key/value head, key/value head
+
+    __device__ __forceinline__ int token(int x) const { return (row0 + x) / G; }
+    __device__ __forceinline__ int position(int x) const { return at_least(-1, first_position + token(x)); }
+    // row of q and head of the tile's row x
+    __device__ __forceinline__ void find(int x, int64_t &row, int &head) const
+    {
+        const int i = token(x);
+        row = q0 + i, head = kh * G + (row0 + x - i * G);
+    }
+    __device__ __forceinline__ int64_t flat(const PagedArgs &a, int x) const
+    {
+        int64_t row;
+        int h;
+        find(x, row, h);
+        return row * a.p.n_q_heads + h;
+    }
+    __device__ __forceinline__ char *out(const PagedArgs &a, int x) const
+    {
+        int64_t row;
+        int h;
+        find(x, row, h);
+        return (char *)a.p.o + (row * a.p.o_stride_tok + (int64_t)h * a.p.o_stride_head) * 2;
+    }
+    __device__ __forceinline__ void put_lse(const PagedArgs &a, int x, float lse) const
+    {
+        int64_t row;
+        int h;
+        find(x, row, h);
+        if (a.p.lse) a.p.lse[(int64_t)h * a.p.n_tokens + row] = lse;
+    }
 };
 
-// Tile `rank`, counted from the last one of the last sequence: sequence g has the ranks from cu[g] * G / 128 + g on.
-__device__ __forceinline__ bool find_tile(const PagedArgs &a, int G, int rank, TileRows &t)
+// Tile `rank`, counted from the last one of the last sequence: sequence g has the ranks from cu[g] * G / BM + g on.
+template <int BM>
+__device__ __forceinline__ bool find_tile(const PagedArgs &a, int rank, TileRows &t)
 {
     const cf_attn_paged_params &p = a.p;
     const int32_t *cu = p.cu_seqlens_q;
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, G = t.G;
     const int place = (int)((int64_t)p.n_tokens * G / BM) + p.n_seqs - 1 - rank;
     int lo = 0, hi = p.n_seqs;
     while (hi - lo > 64) {
@@ -65,133 +106,109 @@ __device__ __forceinline__ bool find_tile(const PagedArgs &a, int G, int rank, T
     return t.rows > 0;
 }
 
-// Copies ROWS keys of a head, from key `start` (a multiple of 16) on, into a swizzled LDS tile, by WAVES wavefronts: groups of 16 keys, each
-// in one page.  pages[g]: the page of group g, -1: none.  last: the last key that may be read.
-template <int ROWS, int D, int WAVES>
-struct PagedDma {
-    static constexpr int RPI = 512 / D, UNITS = D / 8, PARTS = ROWS / (RPI * WAVES), GROUPS = ROWS / 16;
-    int wv, r;                   // this wavefront among those that copy; this lane's row of an instruction
-    unsigned unit16[(RPI * WAVES) % 16 == 0 ? 1 : 16 / (RPI * WAVES)];
+// Where a workgroup's keys stand.
+struct KeySource {
+    const int32_t *table;        // the sequence's row
+    int shift, n_pages, last;    // last: the last key that may be read
     unsigned row_bytes;
-    static constexpr int KINDS = (RPI * WAVES) % 16 == 0 ? 1 : 16 / (RPI * WAVES);
+    int64_t page_bytes;
+    const char *k, *v;           // of this head
+    __device__ __forceinline__ KeySource(const PagedArgs &a, const TileRows &t, int keys)
+        : table(a.p.block_table + (int64_t)t.seq * a.p.table_stride), shift(a.shift), n_pages(a.p.n_pages), last(keys - 1),
+          row_bytes((unsigned)(a.p.kv_stride_tok * 2)), page_bytes(a.p.page_stride * 2),
+          k((const char *)a.p.k_pages + (int64_t)t.kh * a.p.kv_stride_head * 2), v((const char *)a.p.v_pages + (int64_t)t.kh * a.p.kv_stride_head * 2)
+    {
+    }
+    // The page of keys key .. (a group that lies in one page), -1: none, or behind the last key.
+    __device__ __forceinline__ int page_of(int key) const
+    {
+        const int page = table[min(key, last) >> shift];
+        return page >= 0 && page < n_pages && key <= last ? page : -1;
+    }
+    __device__ __forceinline__ int64_t offset(int page, int key) const
+    {
+        return page * page_bytes + (int64_t)(key & ((1 << shift) - 1)) * row_bytes;
+    }
+};
 
-    __device__ __forceinline__ void init(int64_t row_bytes_, int wave)
+// Copies a group of GROUP consecutive keys of one page into its place in a swizzled LDS tile, WAVES wavefronts together (an instruction of
+// one of them: RPI rows).
+template <int D, int GROUP, int WAVES>
+struct GroupDma {
+    static constexpr int RPI = 512 / D, UNITS = D / 8, COPIES = GROUP / (RPI * WAVES);
+    static constexpr int KINDS = (RPI * WAVES) % 16 == 0 ? 1 : 16 / (RPI * WAVES);
+    static_assert(COPIES >= 1, "a group is at least an instruction of each");
+    int wv, r;                   // of the wavefronts that copy together; this lane's row of its first instruction
+    unsigned row_bytes, unit16[KINDS], lane_off[KINDS];
+    __device__ __forceinline__ void init(unsigned row_bytes_, int wave)
     {
         const int lane = threadIdx.x & 63;
         wv = wave;
-        r = lane / UNITS;
-        row_bytes = (unsigned)row_bytes_;
+        r = RPI * wave + lane / UNITS;
+        row_bytes = row_bytes_;
 #pragma unroll
-        for (int i = 0; i < KINDS; ++i) unit16[i] = ((lane % UNITS) ^ swz<D>(RPI * (WAVES * i + wv) + r)) * 16;
+        for (int i = 0; i < KINDS; ++i) {
+            unit16[i] = ((lane % UNITS) ^ swz<D>(RPI * WAVES * i + r)) * 16;
+            lane_off[i] = (unsigned)r * row_bytes + unit16[i];
+        }
     }
-    // base(page, row in group's page): address of a key's row
-    template <typename Base>
-    __device__ __forceinline__ void issue(int start, int last, const int (&pages)[GROUPS], char *tile, Base base) const
+    __device__ __forceinline__ void copy(__amdgpu_buffer_rsrc_t rsrc, char *lds, int c, unsigned off, unsigned scalar_off) const
     {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (CF_LDS void *)(lds + (c * WAVES + wv) * 1024), 16, (int)off, (int)scalar_off, 0, 0);
+    }
+    // room: rows of the group that may be read, less one; rows behind them read the last of these
+    __device__ __forceinline__ void issue(const char *src, int room, char *lds) const
+    {
+        const __amdgpu_buffer_rsrc_t rsrc = TileDma<64, D>::descriptor(src);
+        if (room >= GROUP - 1) {
 #pragma unroll
-        for (int c = 0; c < PARTS; ++c) {
-            const int first = RPI * (WAVES * c + wv);        // of the instruction's rows in the tile (wave-uniform)
-            int page;
-            if constexpr (RPI * WAVES <= 16) {
-                page = pages[RPI * WAVES * c / 16];
-            } else {                                          // (64-wide heads, four wavefronts: two groups to a step)
-                page = wv < 2 ? pages[RPI * WAVES * c / 16] : pages[RPI * WAVES * c / 16 + 1];
-            }
-            const int key = start + first, room = last - key;            // rows of the instruction up to the last key: room + 1
-            const bool some = page >= 0 && room >= 0;
-            const char *src = some ? base(page, key) : (const char *)zeros;
-            unsigned off = (unsigned)min(r, room) * row_bytes;
-            off = some ? off : 0;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(TileDma<64, D>::descriptor(uniform(src)), (CF_LDS void *)(tile + (c * WAVES + wv) * 1024), 16,
-                                                     (int)(off + unit16[c % KINDS]), 0, 0, 0);
+            for (int c = 0; c < COPIES; ++c)
+                copy(rsrc, lds, c, lane_off[c % KINDS], RPI * WAVES * c * row_bytes);
+        } else {
+#pragma unroll
+            for (int c = 0; c < COPIES; ++c)
+                copy(rsrc, lds, c, (unsigned)min(r + RPI * WAVES * c, room) * row_bytes + unit16[c % KINDS], 0);
         }
     }
 };
 
-// What both bodies need of a call.
+// The queries of the tile's row x, 8 elements from d on; a negative scale is put on them, a scale of 0 makes them 0 (the row maximum is
+// taken before scaling, which needs a positive factor).
+__device__ __forceinline__ bf16x8 query(const PagedArgs &a, const TileRows &t, int x, int d)
+{
+    int64_t row;
+    int h;
+    t.find(x, row, h);
+    i32x4 w = *(const i32x4 *)((const char *)a.p.q + (row * a.p.q_stride_tok + (int64_t)h * a.p.q_stride_head + d) * 2);
+    const int flip = a.p.softmax_scale < 0.f ? 0x80008000 : 0, keep = a.p.softmax_scale == 0.f ? 0 : -1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = (w[e] ^ flip) & keep;
+    return __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ float score_factor(const PagedArgs &a) { return a.p.softmax_scale == 0.f ? 1.f : fabsf(a.p.softmax_scale) * kLog2e; }
+
+// One row over the key tiles [first, end), pair by pair, into the call's tensors or as a part (a row whose result is not finite).
 template <int D>
-struct Setup {
-    const PagedArgs &a;
-    const TileRows &t;
-    PageTable table;
-    int G, kh;
-    int64_t key_row_bytes, page_bytes;
-    const char *k, *v;
-    float c2;
-    unsigned flip;               // sign of the scale, on two bf16
-    bool zero;                   // scale 0: every score is 0
-    __device__ __forceinline__ Setup(const PagedArgs &a_, const TileRows &t_, int G_, int kh_)
-        : a(a_), t(t_), table(a_.table(t_.seq)), G(G_), kh(kh_), key_row_bytes(a_.p.kv_stride_tok * 2), page_bytes(a_.p.page_stride * 2),
-          k((const char *)a_.p.k_pages + (int64_t)kh_ * a_.p.kv_stride_head * 2), v((const char *)a_.p.v_pages + (int64_t)kh_ * a_.p.kv_stride_head * 2)
-    {
-        zero = a.p.softmax_scale == 0.f;
-        flip = a.p.softmax_scale < 0.f ? 0x80008000u : 0u;
-        c2 = zero ? 1.f : fabsf(a.p.softmax_scale) * kLog2e;
+__device__ __forceinline__ void row_again(const PagedArgs &a, const TileRows &t, int x, const KeyTiles<BN, WindowMask> &tiles, int first, int end, int part)
+{
+    const int lane = threadIdx.x & 63;
+    int64_t row;
+    int h;
+    t.find(x, row, h);
+    const unsigned short *q = row_of<unsigned short>(a.p.q, (int)row, a.p.q_stride_tok, h, a.p.q_stride_head);
+    const RowSums<unsigned short, D> r = paged_row<unsigned short, D, 4>(a, a.table(t.seq), t.position(x), t.kh, tiles, first, end, [&](int e) { return ld(q + e); });
+    const bool none = r.m == -INFINITY && r.z == 0.f;
+    if (a.parts > 1) {
+        const int64_t flat = t.flat(a, x);
+        float *o = a.part_o + ((int64_t)part * a.p.n_tokens * a.p.n_q_heads + flat) * D;
+        for (int e = 0; e < D / 64; ++e) o[lane + 64 * e] = r.acc[e];
+        if (lane == 0) a.part_ml[flat * a.parts + part] = make_float2(r.m * kLog2e, r.z);
+    } else {
+        unsigned short *o = (unsigned short *)t.out(a, x);
+        for (int e = 0; e < D / 64; ++e) st(o + lane + 64 * e, none ? 0.f : r.acc[e] / r.z);
+        if (lane == 0) t.put_lse(a, x, none ? -INFINITY : r.m + logf(r.z));
     }
-    // token-head row x of the tile: its token of q, head, position
-    __device__ __forceinline__ int token(int x) const { return (t.row0 + x) / G; }
-    __device__ __forceinline__ int position(int x) const { return at_least(-1, t.first_position + token(x)); }
-    __device__ __forceinline__ int64_t flat(int x) const
-    {
-        const int i = token(x);
-        return (int64_t)(t.q0 + i) * a.p.n_q_heads + kh * G + (t.row0 + x - i * G);
-    }
-    __device__ __forceinline__ bf16x8 query(int x, int d) const
-    {
-        const int i = token(x), h = kh * G + (t.row0 + x - i * G);
-        i32x4 w = *(const i32x4 *)((const char *)a.p.q + ((int64_t)(t.q0 + i) * a.p.q_stride_tok + (int64_t)h * a.p.q_stride_head + d) * 2);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = zero ? 0 : w[e] ^ (int)flip;
-        return __builtin_bit_cast(bf16x8, w);
-    }
-    __device__ __forceinline__ char *out(int x) const
-    {
-        const int i = token(x), h = kh * G + (t.row0 + x - i * G);
-        return (char *)a.p.o + ((int64_t)(t.q0 + i) * a.p.o_stride_tok + (int64_t)h * a.p.o_stride_head) * 2;
-    }
-    __device__ __forceinline__ float *lse(int x) const
-    {
-        const int i = token(x), h = kh * G + (t.row0 + x - i * G);
-        return a.p.lse + (int64_t)h * a.p.n_tokens + t.q0 + i;
-    }
-    __device__ __forceinline__ const char *key_row(const char *base, int page, int key) const
-    {
-        return base + (int64_t)page * page_bytes + (int64_t)table.row_in_page(key) * key_row_bytes;
-    }
-    // The pages of GROUPS groups of 16 keys from `start` on.
-    template <int GROUPS>
-    __device__ __forceinline__ void find_pages(int start, int last, int (&pages)[GROUPS]) const
-    {
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            const int page = table.row[min(start + 16 * g, last) >> table.shift];
-            pages[g] = page >= 0 && page < table.n_pages && start + 16 * g <= last ? page : -1;
-        }
-    }
-    // One row over the part's keys, pair by pair (a row whose result is not finite).
-    template <typename Tiles>
-    __device__ __forceinline__ RowSums<unsigned short, D> again(int x, const Tiles &tiles, int first, int end) const
-    {
-        const int i = token(x), h = kh * G + (t.row0 + x - i * G);
-        const unsigned short *q = row_of<unsigned short>(a.p.q, t.q0 + i, a.p.q_stride_tok, h, a.p.q_stride_head);
-        return paged_row<unsigned short, D, 4>(a, table, position(x), kh, tiles, first, end, [&](int e) { return ld(q + e); });
-    }
-    // Its result: into the call's tensors, or as a part.
-    __device__ __forceinline__ void put_again(int x, const RowSums<unsigned short, D> &r, int part) const
-    {
-        const int lane = threadIdx.x & 63;
-        const bool none = r.m == -INFINITY && r.z == 0.f;
-        if (a.parts > 1) {
-            float *o = a.part_o + ((int64_t)part * a.p.n_tokens * a.p.n_q_heads + flat(x)) * D;
-            for (int e = 0; e < D / 64; ++e) o[lane + 64 * e] = r.acc[e];
-            if (lane == 0) a.part_ml[flat(x) * a.parts + part] = make_float2(r.m * kLog2e, r.z);
-        } else {
-            unsigned short *o = (unsigned short *)out(x);
-            for (int e = 0; e < D / 64; ++e) st(o + lane + 64 * e, none ? 0.f : r.acc[e] / r.z);
-            if (lane == 0 && a.p.lse) *lse(x) = none ? -INFINITY : r.m + logf(r.z);
-        }
-    }
-};
+}
 
 // One block of KB x 16 keys, for QB x 16 rows: scores of a K tile, masks, the running softmax, P.
 template <int D, int KB, int QB>
@@ -245,13 +262,13 @@ struct Rows {
             }
         }
         if (start <= highest - mask.window && start + 16 * KB > mask.sinks) {
-            const int sink = mask.sinks - start - group * 4;
+            const int from = mask.sinks - start - group * 4;
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
-                const int far = pos[qb] - mask.window - start - group * 4;
+                const unsigned gap = hidden_keys(mask, pos[qb]);
 #pragma unroll
                 for (int i = 0; i < NS; ++i)
-                    if (F::place(i) <= far && F::place(i) >= sink) s[i / F::R][qb][i % F::R] = -INFINITY;
+                    if ((unsigned)(F::place(i) - from) < gap) s[i / F::R][qb][i % F::R] = -INFINITY;
             }
         }
         if (groups != 0) {
@@ -326,116 +343,160 @@ struct Rows {
 };
 
 // Many rows: 32 to a wavefront, key tiles shared.
-template <int D>
-__device__ __forceinline__ void many_rows(const Setup<D> &c, const KeyTiles<BN, WindowMask> &tiles, int first, int end, int last, int part, char *stage_a,
-                                          char *stage_b)
+// WHOLE: a page holds 64 keys or more, so that a key tile has one base, else one for each 16 keys.  A tile that is not full, or that has a
+// group of no page, is copied group by group.
+template <int D, bool WHOLE>
+__device__ __forceinline__ void many_rows(const PagedArgs &a, const TileRows &t, const KeyTiles<BN, WindowMask> &tiles, int first, int end, int keys,
+                                          int part, char *stage_a, char *stage_b)
 {
-    constexpr int TILE = BN * 2 * D;
-    const PagedArgs &a = c.a;
+    constexpr int TILE = BN * 2 * D, GROUP = 16 * 2 * D, WAVES = D == 128 ? 4 : 2;      // (wavefronts that a group's rows take)
     const int wave = wave_id(), col = F::column(), group = F::group();
-    const int x0 = 32 * wave, rows = at_most(32, c.t.rows - x0);           // this wavefront's rows of the tile (rows <= 0: none)
+    const int x0 = 32 * wave, rows = at_most(32, t.rows - x0);           // this wavefront's rows of the tile (rows <= 0: none)
+    const KeySource src(a, t, keys);
+    TileDma<BN, D> tile_dma;
+    tile_dma.init(src.row_bytes);
+    GroupDma<D, 16, WAVES> group_dma;
+    group_dma.init(src.row_bytes, wave % WAVES);
+    int pages[WHOLE ? 1 : 4];
+    unsigned hidden = 0;
+    auto find_pages = [&](int start) {
+#pragma unroll
+        for (int g = 0; g < (WHOLE ? 1 : 4); ++g) pages[g] = src.page_of(start + 16 * g);
+    };
+    auto issue = [&](int start, char *stage) {
+        bool plain = start + BN - 1 <= src.last;
+#pragma unroll
+        for (int g = 0; g < (WHOLE ? 1 : 4); ++g) plain = plain && pages[g] >= 0;
+        hidden = 0;
+        if (plain) {
+            if constexpr (WHOLE) {
+                const int64_t at = src.offset(pages[0], start);
+                tile_dma.issue(src.k + at, BN - 1, stage);
+                tile_dma.issue(src.v + at, BN - 1, stage + TILE);
+            } else {
+#pragma unroll
+                for (int c = 0; c < WAVES; ++c) {
+                    const int g = D == 128 ? c : 2 * c + (wave >> 1), page = D == 128 ? pages[c] : wave < 2 ? pages[2 * c] : pages[2 * c + 1];
+                    const int64_t at = src.offset(page, start + 16 * g);
+                    group_dma.issue(src.k + at, 15, stage + g * GROUP);
+                    group_dma.issue(src.v + at, 15, stage + TILE + g * GROUP);
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int g = 0; g < 4; ++g) {
+                const int key = start + 16 * g, page = src.page_of(key);
+                const int64_t at = page < 0 ? 0 : src.offset(page, key);
+                const int room = page < 0 ? 0 : src.last - key;
+                hidden |= (unsigned)(page < 0) << g;
+                if (D == 64 && (wave >> 1) != (g & 1)) continue;
+                group_dma.issue(page < 0 ? (const char *)zeros : src.k + at, room, stage + g * GROUP);
+                group_dma.issue(page < 0 ? (const char *)zeros : src.v + at, room, stage + TILE + g * GROUP);
+            }
+        }
+    };
+    find_pages(tiles.start(first));
+    issue(tiles.start(first), stage_a);
+    if (first + 1 < end) find_pages(tiles.start(first + 1));
+
     Rows<D, BN / 16, 2> r;
     r.clear();
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
-        const int x = min(x0 + 16 * qb + col, c.t.rows - 1);
-        r.pos[qb] = c.position(x);
+        const int x = min(x0 + 16 * qb + col, t.rows - 1);
+        r.pos[qb] = t.position(x);
 #pragma unroll
-        for (int ks = 0; ks < D / F::K; ++ks) r.q[qb][ks] = c.query(x, ks * F::K + group * 8);
+        for (int ks = 0; ks < D / F::K; ++ks) r.q[qb][ks] = query(a, t, x, ks * F::K + group * 8);
     }
-    const int lowest = c.position(at_most(x0, c.t.rows - 1)), highest = c.position(at_most(x0 + 31, c.t.rows - 1));
+    const int lowest = t.position(at_most(x0, t.rows - 1)), highest = t.position(at_most(x0 + 31, t.rows - 1));
+    const float c2 = score_factor(a);
+    const WindowMask mask = a.mask;
     const LaneOffsets<D, 16> lo = lane_offsets<D, 16>();
-    PagedDma<BN, D, 4> dma;
-    dma.init(c.key_row_bytes, wave);
-    int pages[4];
-    unsigned hidden = 0;
-    auto issue = [&](int start, char *stage) {
-        dma.issue(start, last, pages, stage, [&](int page, int key) { return c.key_row(c.k, page, key); });
-        dma.issue(start, last, pages, stage + TILE, [&](int page, int key) { return c.key_row(c.v, page, key); });
-        hidden = 0;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) hidden |= (unsigned)(pages[g] < 0) << g;
-    };
-    c.find_pages(tiles.start(first), last, pages);
-    issue(tiles.start(first), stage_a);
-    if (first + 1 < end) c.find_pages(tiles.start(first + 1), last, pages);
     wait_lds_dma();
     __syncthreads();
-    auto do_tile = [&](int t, const char *stage, char *next) {
-        const int start = tiles.start(t);
+    auto do_tile = [&](int n, const char *stage, char *next) {
+        const int start = tiles.start(n);
         const unsigned hid = hidden;
-        if (t + 1 < end) issue(tiles.start(t + 1), next);
-        if (t + 2 < end) c.find_pages(tiles.start(t + 2), last, pages);
-        if (rows > 0 && start <= highest && (start + BN > lowest + 1 - a.mask.window || start < a.mask.sinks)) {
+        if (n + 1 < end) issue(tiles.start(n + 1), next);
+        if (n + 2 < end) find_pages(tiles.start(n + 2));
+        if (rows > 0 && start <= highest && (start + BN > lowest + 1 - mask.window || start < mask.sinks)) {
             f32x4 s[BN / 16][2];
-            r.scores(stage, lo, a.mask, start, lowest, highest, hid, c.c2, s);
+            r.scores(stage, lo, mask, start, lowest, highest, hid, c2, s);
             r.values(stage + TILE, lo, s);
         }
         wait_lds_dma();
         __syncthreads();
     };
-    for (int t = first; t < end; t += 2) {
-        do_tile(t, stage_a, stage_b);
-        if (t + 1 < end) do_tile(t + 1, stage_b, stage_a);
+    for (int n = first; n < end; n += 2) {
+        do_tile(n, stage_a, stage_b);
+        if (n + 1 < end) do_tile(n + 1, stage_b, stage_a);
     }
     if (rows <= 0) return;
+    const PagedArgs &e = arguments();
     float l[2], scale[2];
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
         l[qb] = sum_over_groups<16>(r.l[qb]);
         scale[qb] = l[qb] == 0.f ? 0.f : 1.f / l[qb];
     }
-    if (a.parts > 1) {
-        const int64_t all = (int64_t)a.p.n_tokens * a.p.n_q_heads;
+    if (e.parts > 1) {
+        const int64_t all = (int64_t)e.p.n_tokens * e.p.n_q_heads;
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
             const int x = 16 * qb + col;
             if (x >= rows) continue;
-            const int64_t flat = c.flat(x0 + x);
-            float *o = a.part_o + (part * all + flat) * D + 4 * group;
+            const int64_t flat = t.flat(e, x0 + x);
+            float *o = e.part_o + (part * all + flat) * D + 4 * group;
 #pragma unroll
             for (int db = 0; db < D / 16; ++db) *(f32x4 *)(o + 16 * db) = r.o[db][qb];
-            if (group == 0) a.part_ml[flat * a.parts + part] = make_float2(r.m[qb], l[qb]);
+            if (group == 0) e.part_ml[flat * e.parts + part] = make_float2(r.m[qb], l[qb]);
         }
     } else {
         char *scratch = (wave < 2 ? stage_a : stage_b) + (wave & 1) * RowScratch<D>::bytes;
-        store_rows_bf16<D, 16>(r.o, scale, scratch, rows, [&](int x) { return c.out(x0 + x); });
+        store_rows_bf16<D, 16>(r.o, scale, scratch, rows, [&](int x) { return t.out(e, x0 + x); });
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb)
-            if (group == 0 && 16 * qb + col < rows && a.p.lse)
-                *c.lse(x0 + 16 * qb + col) = l[qb] == 0.f ? -INFINITY : __builtin_fmaf(r.m[qb], kLn2, __logf(l[qb]));
+            if (group == 0 && 16 * qb + col < rows)
+                t.put_lse(e, x0 + 16 * qb + col, l[qb] == 0.f ? -INFINITY : __builtin_fmaf(r.m[qb], kLn2, __logf(l[qb])));
     }
-    for_rows_not_finite<D, 16>(r.o, scale, rows, [&](int x) { c.put_again(x0 + x, c.again(x0 + x, tiles, first, end), part); });
+    for_rows_not_finite<D, 16>(r.o, scale, rows, [&](int x) { row_again<D>(e, t, x0 + x, tiles, first, end, part); });
 }
 
 // Few rows: all of them in every wavefront, which has blocks of 32 keys of its own.
-template <int D, int QB>
-__device__ __forceinline__ void few_rows(const Setup<D> &c, const KeyTiles<BN, WindowMask> &tiles, int first, int end, int last, int part, char *k_stage,
-                                         char *v_stage)
+template <int D, int QB, bool WHOLE>
+__device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, const KeyTiles<BN, WindowMask> &tiles, int first, int end, int keys,
+                                         int part, char *k_stage, char *v_stage)
 {
     constexpr int TILE = FEW * 2 * D, COPIES = TILE / 1024;       // copy instructions of a block's keys
-    const PagedArgs &a = c.a;
-    const int wave = wave_id(), lane = threadIdx.x & 63, col = F::column(), group = F::group();
+    const int wave = wave_id(), col = F::column(), group = F::group();
     char *k_tile = k_stage + wave * TILE, *v_tile = v_stage + wave * TILE;
-    Rows<D, FEW / 16, QB> r;
-    r.clear();
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int x = min(16 * qb + col, c.t.rows - 1);
-        r.pos[qb] = c.position(x);
-#pragma unroll
-        for (int ks = 0; ks < D / F::K; ++ks) r.q[qb][ks] = c.query(x, ks * F::K + group * 8);
-    }
-    const int lowest = c.position(0), highest = c.position(c.t.rows - 1);
-    const LaneOffsets<D, 16> lo = lane_offsets<D, 16>();
-    PagedDma<FEW, D, 1> dma;
-    dma.init(c.key_row_bytes, 0);
+    const KeySource src(a, t, keys);
+    GroupDma<D, 32, 1> dma;
+    dma.init(src.row_bytes, 0);
+    GroupDma<D, 16, 1> half_dma;
+    half_dma.init(src.row_bytes, 0);
     // block u of the part: half u % 2 of its key tile u / 2
     auto start_of = [&](int u) { return tiles.start(first + u / 2) + FEW * (u & 1); };
     const int blocks = 2 * (end - first);
-    int k_pages[2], v_pages[2], next_pages[2];
-    auto issue_k = [&](int u) { dma.issue(start_of(u), last, k_pages, k_tile, [&](int page, int key) { return c.key_row(c.k, page, key); }); };
-    auto issue_v = [&](int u) { dma.issue(start_of(u), last, v_pages, v_tile, [&](int page, int key) { return c.key_row(c.v, page, key); }); };
+    int pages[2], next_pages[2];                     // of the two halves
+    auto find_pages = [&](int start, int (&p)[2]) {
+        p[0] = src.page_of(start);
+        p[1] = WHOLE ? p[0] : src.page_of(start + 16);
+    };
+    // (the same number of copies whatever the pages are: they are counted)
+    auto issue = [&](const char *base, int start, const int (&p)[2], char *tile) {
+        if constexpr (WHOLE) {
+            const bool none = p[0] < 0;
+            dma.issue(uniform(none ? (const char *)zeros : base + src.offset(p[0], start)), none ? 0 : src.last - start, tile);
+        } else {
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const bool none = p[g] < 0;
+                half_dma.issue(uniform(none ? (const char *)zeros : base + src.offset(p[g], start + 16 * g)), none ? 0 : src.last - start - 16 * g,
+                               tile + g * (16 * 2 * D));
+            }
+        }
+    };
     // vmcnt(COPIES): all but the copies issued last have landed
     auto wait_older = [] {
         __builtin_amdgcn_s_waitcnt(0x0F70 | COPIES);
@@ -449,23 +510,35 @@ __device__ __forceinline__ void few_rows(const Setup<D> &c, const KeyTiles<BN, W
     };
     int u = wave;
     if (u < blocks) {
-        c.find_pages(start_of(u), last, k_pages);
-        v_pages[0] = k_pages[0], v_pages[1] = k_pages[1];
-        issue_k(u);
-        issue_v(u);
+        find_pages(start_of(u), pages);
+        issue(src.k, start_of(u), pages, k_tile);
+        issue(src.v, start_of(u), pages, v_tile);
     }
+    Rows<D, FEW / 16, QB> r;
+    r.clear();
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int x = min(16 * qb + col, t.rows - 1);
+        r.pos[qb] = t.position(x);
+#pragma unroll
+        for (int ks = 0; ks < D / F::K; ++ks) r.q[qb][ks] = query(a, t, x, ks * F::K + group * 8);
+    }
+    const int lowest = t.position(0), highest = t.position(t.rows - 1);
+    const float c2 = score_factor(a);
+    const WindowMask mask = a.mask;
+    const LaneOffsets<D, 16> lo = lane_offsets<D, 16>();
     for (; u < blocks; u += 4) {
         const int start = start_of(u), next = u + 4;
         const bool more = next < blocks;
-        unsigned hidden = (unsigned)(v_pages[0] < 0) | (unsigned)(v_pages[1] < 0) << 1;
-        if (more) c.find_pages(start_of(next), last, next_pages);
+        // (keys behind the last one are those of later rows, or behind the table's last column, where groups end)
+        const unsigned hidden = (unsigned)(pages[0] < 0 || start > src.last) | (unsigned)(pages[1] < 0 || start + 16 > src.last) << 1;
+        if (more) find_pages(start_of(next), next_pages);
         f32x4 s[FEW / 16][QB];
         wait_older();                                // K is there
-        r.scores(k_tile, lo, a.mask, start, lowest, highest, hidden, c.c2, s);
+        r.scores(k_tile, lo, mask, start, lowest, highest, hidden, c2, s);
         if (more) {
             reads_done();
-            k_pages[0] = next_pages[0], k_pages[1] = next_pages[1];
-            issue_k(next);
+            issue(src.k, start_of(next), next_pages, k_tile);
             wait_older();                            // V is there
         } else {
             wait_lds_dma();
@@ -474,10 +547,11 @@ __device__ __forceinline__ void few_rows(const Setup<D> &c, const KeyTiles<BN, W
         r.values(v_tile, lo, s);
         if (more) {
             reads_done();
-            v_pages[0] = k_pages[0], v_pages[1] = k_pages[1];
-            issue_v(next);
+            issue(src.v, start_of(next), next_pages, v_tile);
+            pages[0] = next_pages[0], pages[1] = next_pages[1];
         }
     }
+    const PagedArgs &e = arguments();
     // The wavefronts meet: maximum and sum of each row, then its result, in the order of the wavefronts.
     __shared__ float m_s[4][16 * QB], l_s[4][16 * QB];
 #pragma unroll
@@ -497,10 +571,10 @@ __device__ __forceinline__ void few_rows(const Setup<D> &c, const KeyTiles<BN, W
     __syncthreads();
     constexpr int PIECES = D / 4, STEP = 256 / PIECES;        // lanes of a row, rows of a step
     const int piece = threadIdx.x % PIECES;
-    const int64_t all = (int64_t)a.p.n_tokens * a.p.n_q_heads;
-    for (int x0 = 0; x0 < c.t.rows; x0 += STEP) {
+    const int64_t all = (int64_t)e.p.n_tokens * e.p.n_q_heads;
+    for (int x0 = 0; x0 < t.rows; x0 += STEP) {
         const int x = x0 + threadIdx.x / PIECES;
-        const bool mine = x < c.t.rows;
+        const bool mine = x < t.rows;
         bool bad = false;
         if (mine) {
             float M = m_s[0][x];
@@ -517,17 +591,17 @@ __device__ __forceinline__ void few_rows(const Setup<D> &c, const KeyTiles<BN, W
             }
             const float total = (sum[0] + sum[1]) + (sum[2] + sum[3]);
             bad = !(fabsf(total) < INFINITY) || !(L < INFINITY);
-            if (a.parts > 1) {
-                const int64_t flat = c.flat(x);
-                *(f32x4 *)(a.part_o + (part * all + flat) * D + 4 * piece) = sum;
-                if (piece == 0) a.part_ml[flat * a.parts + part] = make_float2(M, L);
+            if (e.parts > 1) {
+                const int64_t flat = t.flat(e, x);
+                *(f32x4 *)(e.part_o + (part * all + flat) * D + 4 * piece) = sum;
+                if (piece == 0) e.part_ml[flat * e.parts + part] = make_float2(M, L);
             } else {
                 const float inv = L == 0.f ? 0.f : 1.f / L;
                 bf16x4 w;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = (__bf16)(sum[e] * inv);
-                *(bf16x4 *)(c.out(x) + piece * 8) = w;
-                if (piece == 0 && a.p.lse) *c.lse(x) = L == 0.f ? -INFINITY : __builtin_fmaf(M, kLn2, __logf(L));
+                for (int i = 0; i < 4; ++i) w[i] = (__bf16)(sum[i] * inv);
+                *(bf16x4 *)(t.out(e, x) + piece * 8) = w;
+                if (piece == 0) t.put_lse(e, x, L == 0.f ? -INFINITY : __builtin_fmaf(M, kLn2, __logf(L)));
             }
         }
         // (a wavefront holds whole rows)
@@ -535,47 +609,64 @@ __device__ __forceinline__ void few_rows(const Setup<D> &c, const KeyTiles<BN, W
             const int at = (__ffsll((long long)left) - 1) / PIECES;
             left &= ~(((PIECES == 64 ? 0ull : 1ull << PIECES) - 1) << (at * PIECES));
             const int row = x0 + wave * (64 / PIECES) + at;
-            c.put_again(row, c.again(row, tiles, first, end), part);
+            row_again<D>(e, t, row, tiles, first, end, part);
         }
     }
 }
 
-template <int D>
+// MODE: FEW rows to a tile, all by few_rows; BM rows, all by many_rows; BOTH: BM rows, by what a tile holds.
+enum Mode { kFew, kMany, kBoth };
+template <int D, Mode MODE, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void mfma_paged_kernel(PagedArgs a)
 {
     // Separate arrays: the compiler must see that copies into one do not touch what is read from the other.
     __shared__ __attribute__((aligned(16))) char stage_a[2 * BN * 2 * D];
     __shared__ __attribute__((aligned(16))) char stage_b[2 * BN * 2 * D];
-    const int G = a.p.n_q_heads / a.p.n_kv_heads;
+    TileRows t;
+    t.G = a.p.n_q_heads / a.p.n_kv_heads;
     int id = blockIdx.x;
-    const int kh = id % a.p.n_kv_heads;              // (fastest: an XCD keeps reading the same heads; attn_mfma_fwd.hip)
+    t.kh = id % a.p.n_kv_heads;                      // (fastest: an XCD keeps reading the same heads; attn_mfma_fwd.hip)
     id /= a.p.n_kv_heads;
     const int part = id % a.parts;
-    TileRows t;
-    if (!find_tile(a, G, id / a.parts, t)) return;
-    const Setup<D> c(a, t, G, kh);
-    const int lowest = c.position(0), highest = c.position(t.rows - 1);
-    const int keys = at_most(highest + 1, c.table.capacity());
+    if (!find_tile<MODE == kFew ? FEW : BM>(a, id / a.parts, t)) return;
+    const int lowest = t.position(0), highest = t.position(t.rows - 1);
+    const int keys = at_most(highest + 1, a.p.pages_per_seq << a.shift);
     const KeyTiles<BN, WindowMask> tiles(a.mask, lowest, keys);
     const int n = at_least(0, tiles.n), first = at_most(n, a.parts > 1 ? part * a.tiles_per_part : 0);
     const int end = a.parts > 1 && part + 1 < a.parts ? at_most(n, first + a.tiles_per_part) : n;
     if (first >= end) {                              // no keys: what is left of the rows
-        for (int x = threadIdx.x; x < t.rows && a.parts > 1; x += 256) a.part_ml[c.flat(x) * a.parts + part] = make_float2(-INFINITY, 0.f);
-        if (a.parts > 1) return;
+        const PagedArgs &e = arguments();
+        for (int x = threadIdx.x; x < t.rows && e.parts > 1; x += 256) e.part_ml[t.flat(e, x) * e.parts + part] = make_float2(-INFINITY, 0.f);
+        if (e.parts > 1) return;
         for (int x = threadIdx.x / (D / 8); x < t.rows; x += 256 / (D / 8)) {
-            *(uint4 *)(c.out(x) + threadIdx.x % (D / 8) * 16) = uint4{0, 0, 0, 0};
-            if (threadIdx.x % (D / 8) == 0 && a.p.lse) *c.lse(x) = -INFINITY;
+            *(uint4 *)(t.out(e, x) + threadIdx.x % (D / 8) * 16) = uint4{0, 0, 0, 0};
+            if (threadIdx.x % (D / 8) == 0) t.put_lse(e, x, -INFINITY);
         }
         return;
     }
-    if (t.rows > FEW) many_rows<D>(c, tiles, first, end, keys - 1, part, stage_a, stage_b);
-    else if (t.rows > 16) few_rows<D, 2>(c, tiles, first, end, keys - 1, part, stage_a, stage_b);
-    else few_rows<D, 1>(c, tiles, first, end, keys - 1, part, stage_a, stage_b);
+    if (MODE == kMany || (MODE == kBoth && t.rows > FEW)) {
+        many_rows<D, WHOLE>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
+    } else if constexpr (MODE != kMany) {
+        if (t.rows > 16) few_rows<D, 2, WHOLE>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
+        else few_rows<D, 1, WHOLE>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
+    }
 }
 
-int64_t tiles_most(const cf_attn_paged_params &p) { return (int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads) / BM + p.n_seqs; }
+// Tiles of single tokens and short runs only, of chunks only, or of both?  By the mean number of token-head rows of a sequence; every kernel
+// takes any of them.
+Mode mode_of(const cf_attn_paged_params &p)
+{
+    const int64_t rows = (int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads);
+    return rows <= (int64_t)FEW * p.n_seqs ? kFew : p.n_seqs == 1 || rows >= 512 * (int64_t)p.n_seqs ? kMany : kBoth;
+}
+int64_t tiles_most(const cf_attn_paged_params &p)
+{
+    return (int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads) / (mode_of(p) == kFew ? FEW : BM) + p.n_seqs;
+}
 
 }  // namespace
+
+int64_t paged_mfma_launch_size(const PagedArgs &a) { return tiles_most(a.p) * a.p.n_kv_heads * a.parts * 256; }
 
 // Parts: so many that the chip's 512 workgroup slots each get several, of two key tiles at least.
 void cut_paged_mfma(PagedArgs &a)
@@ -591,12 +682,22 @@ void cut_paged_mfma(PagedArgs &a)
     a.tiles_per_part = (int)((tiles + a.parts - 1) / a.parts);
 }
 
-hipError_t launch_paged_mfma(const PagedArgs &a, hipStream_t s)
+template <int D, bool WHOLE>
+static hipError_t launch(const PagedArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)(tiles_most(a.p) * a.p.n_kv_heads * a.parts));
-    if (a.p.head_dim == 64) mfma_paged_kernel<64><<<grid, 256, 0, s>>>(a);
-    else mfma_paged_kernel<128><<<grid, 256, 0, s>>>(a);
+    switch (mode_of(a.p)) {
+        case kFew: mfma_paged_kernel<D, kFew, WHOLE><<<grid, 256, 0, s>>>(a); break;
+        case kMany: mfma_paged_kernel<D, kMany, WHOLE><<<grid, 256, 0, s>>>(a); break;
+        default: mfma_paged_kernel<D, kBoth, WHOLE><<<grid, 256, 0, s>>>(a);
+    }
     return hipGetLastError();
+}
+hipError_t launch_paged_mfma(const PagedArgs &a, hipStream_t s)
+{
+    const bool whole = a.p.page_size >= BN;
+    if (a.p.head_dim == 64) return whole ? launch<64, true>(a, s) : launch<64, false>(a, s);
+    return whole ? launch<128, true>(a, s) : launch<128, false>(a, s);
 }
 
 }  // namespace cf

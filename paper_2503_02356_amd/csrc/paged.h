@@ -71,6 +71,7 @@ __device__ inline RowSums<T, D> paged_row(const PagedArgs &a, const PageTable &t
 constexpr int kMostParts = 64;       // (a lane of the joining wavefront to a part)
 // bf16 matrix kernel (attn_paged_mfma.hip).
 hipError_t launch_paged_mfma(const PagedArgs &a, hipStream_t s);
+int64_t paged_mfma_launch_size(const PagedArgs &a);      // work-items
 // Cuts a call's keys into parts: sets parts and tiles_per_part.
 void cut_paged_mfma(PagedArgs &a);
 // Joins the parts of every row (one call's parts > 1).
