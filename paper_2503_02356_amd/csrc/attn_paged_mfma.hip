@@ -108,22 +108,25 @@ __device__ __forceinline__ bool find_tile(const PagedArgs &a, int rank, TileRows
 
 // Where a workgroup's keys stand.
 struct KeySource {
-    const int32_t *table;        // the sequence's row
+    const CF_CONSTANT int32_t *table;        // the sequence's row (nothing writes it meanwhile: scalar loads, which no copy in flight holds up)
     int shift, n_pages, last;    // last: the last key that may be read
     unsigned row_bytes;
     int64_t page_bytes;
     const char *k, *v;           // of this head
     __device__ __forceinline__ KeySource(const PagedArgs &a, const TileRows &t, int keys)
-        : table(a.p.block_table + (int64_t)t.seq * a.p.table_stride), shift(a.shift), n_pages(a.p.n_pages), last(keys - 1),
+        : table((const CF_CONSTANT int32_t *)a.p.block_table + (int64_t)t.seq * a.p.table_stride), shift(a.shift), n_pages(a.p.n_pages), last(keys - 1),
           row_bytes((unsigned)(a.p.kv_stride_tok * 2)), page_bytes(a.p.page_stride * 2),
           k((const char *)a.p.k_pages + (int64_t)t.kh * a.p.kv_stride_head * 2), v((const char *)a.p.v_pages + (int64_t)t.kh * a.p.kv_stride_head * 2)
     {
     }
-    // The page of keys key .. (a group that lies in one page), -1: none, or behind the last key.
+    // The table's entry for keys key .. (a group that lies in one page).  Looked at (is_page) only where the page is used, a tile later: the
+    // load has come by then.
+    __device__ __forceinline__ int entry(int key) const { return table[min(key, last) >> shift]; }
+    __device__ __forceinline__ bool is_page(int entry) const { return (unsigned)entry < (unsigned)n_pages; }
     __device__ __forceinline__ int page_of(int key) const
     {
-        const int page = table[min(key, last) >> shift];
-        return page >= 0 && page < n_pages && key <= last ? page : -1;
+        const int page = entry(key);
+        return is_page(page) && key <= last ? page : -1;
     }
     __device__ __forceinline__ int64_t offset(int page, int key) const
     {
@@ -342,6 +345,8 @@ struct Rows {
     }
 };
 
+__device__ __forceinline__ void scalar_loads_done() { __builtin_amdgcn_s_waitcnt(0xC07F); }      // lgkmcnt(0)
+
 // Many rows: 32 to a wavefront, key tiles shared.
 // WHOLE: a page holds 64 keys or more, so that a key tile has one base, else one for each 16 keys.  A tile that is not full, or that has a
 // group of no page, is copied group by group.
@@ -359,14 +364,14 @@ __device__ __forceinline__ void many_rows(const PagedArgs &a, const TileRows &t,
     group_dma.init(src.row_bytes, wave % WAVES);
     int pages[WHOLE ? 1 : 4];
     unsigned hidden = 0;
-    auto find_pages = [&](int start) {
+    auto find_pages = [&](int start, int (&p)[WHOLE ? 1 : 4]) {
 #pragma unroll
-        for (int g = 0; g < (WHOLE ? 1 : 4); ++g) pages[g] = src.page_of(start + 16 * g);
+        for (int g = 0; g < (WHOLE ? 1 : 4); ++g) p[g] = src.entry(start + 16 * g);
     };
     auto issue = [&](int start, char *stage) {
         bool plain = start + BN - 1 <= src.last;
 #pragma unroll
-        for (int g = 0; g < (WHOLE ? 1 : 4); ++g) plain = plain && pages[g] >= 0;
+        for (int g = 0; g < (WHOLE ? 1 : 4); ++g) plain = plain && src.is_page(pages[g]);
         hidden = 0;
         if (plain) {
             if constexpr (WHOLE) {
@@ -395,9 +400,9 @@ __device__ __forceinline__ void many_rows(const PagedArgs &a, const TileRows &t,
             }
         }
     };
-    find_pages(tiles.start(first));
+    find_pages(tiles.start(first), pages);
     issue(tiles.start(first), stage_a);
-    if (first + 1 < end) find_pages(tiles.start(first + 1));
+    if (first + 1 < end) find_pages(tiles.start(first + 1), pages);
 
     Rows<D, BN / 16, 2> r;
     r.clear();
@@ -417,8 +422,14 @@ __device__ __forceinline__ void many_rows(const PagedArgs &a, const TileRows &t,
     auto do_tile = [&](int n, const char *stage, char *next) {
         const int start = tiles.start(n);
         const unsigned hid = hidden;
+        // (The table's entries are asked for before the copies are issued and waited for behind that: with scalar loads in flight no LDS read
+        // can be waited for but all of them.)
+        int coming[WHOLE ? 1 : 4] = {};
+        if (n + 2 < end) find_pages(tiles.start(n + 2), coming);
         if (n + 1 < end) issue(tiles.start(n + 1), next);
-        if (n + 2 < end) find_pages(tiles.start(n + 2));
+        scalar_loads_done();
+#pragma unroll
+        for (int g = 0; g < (WHOLE ? 1 : 4); ++g) pages[g] = coming[g];
         if (rows > 0 && start <= highest && (start + BN > lowest + 1 - mask.window || start < mask.sinks)) {
             f32x4 s[BN / 16][2];
             r.scores(stage, lo, mask, start, lowest, highest, hid, c2, s);
@@ -480,18 +491,18 @@ __device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, 
     const int blocks = 2 * (end - first);
     int pages[2], next_pages[2];                     // of the two halves
     auto find_pages = [&](int start, int (&p)[2]) {
-        p[0] = src.page_of(start);
-        p[1] = WHOLE ? p[0] : src.page_of(start + 16);
+        p[0] = src.entry(start);
+        p[1] = WHOLE ? p[0] : src.entry(start + 16);
     };
     // (the same number of copies whatever the pages are: they are counted)
     auto issue = [&](const char *base, int start, const int (&p)[2], char *tile) {
         if constexpr (WHOLE) {
-            const bool none = p[0] < 0;
+            const bool none = !src.is_page(p[0]) || start > src.last;
             dma.issue(uniform(none ? (const char *)zeros : base + src.offset(p[0], start)), none ? 0 : src.last - start, tile);
         } else {
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-                const bool none = p[g] < 0;
+                const bool none = !src.is_page(p[g]) || start + 16 * g > src.last;
                 half_dma.issue(uniform(none ? (const char *)zeros : base + src.offset(p[g], start + 16 * g)), none ? 0 : src.last - start - 16 * g,
                                tile + g * (16 * 2 * D));
             }
@@ -506,7 +517,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, 
     // lgkmcnt(0): what was read of a stage has been read, before copies into it are issued
     auto reads_done = [] {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_s_waitcnt(0xC07F);
+        scalar_loads_done();
     };
     int u = wave;
     if (u < blocks) {
@@ -531,10 +542,11 @@ __device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, 
         const int start = start_of(u), next = u + 4;
         const bool more = next < blocks;
         // (keys behind the last one are those of later rows, or behind the table's last column, where groups end)
-        const unsigned hidden = (unsigned)(pages[0] < 0 || start > src.last) | (unsigned)(pages[1] < 0 || start + 16 > src.last) << 1;
+        const unsigned hidden = (unsigned)(!src.is_page(pages[0]) || start > src.last) | (unsigned)(!src.is_page(pages[1]) || start + 16 > src.last) << 1;
         if (more) find_pages(start_of(next), next_pages);
         f32x4 s[FEW / 16][QB];
         wait_older();                                // K is there
+        scalar_loads_done();
         r.scores(k_tile, lo, mask, start, lowest, highest, hidden, c2, s);
         if (more) {
             reads_done();
