@@ -394,7 +394,7 @@ typedef struct {
     const int32_t *kv_lens;             /* device, [n_seqs]                                      */
     const int32_t *block_table;         /* device, [n_seqs][pages_per_seq]                       */
     int64_t table_stride;               /* elements from row to row, >= pages_per_seq            */
-    int32_t pages_per_seq;              /* >= 1; pages_per_seq * page_size < 2^31                */
+    int32_t pages_per_seq;              /* >= 1; pages_per_seq * page_size <= 2^30               */
     int32_t page_size;                  /* a power of two, 16 .. 65536                           */
     int32_t n_pages;                    /* >= 1                                                  */
     int32_t max_kv_len;                 /* >= 0                                                  */

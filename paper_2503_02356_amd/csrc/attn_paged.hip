@@ -30,7 +30,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(PagedArgs a)
     for (int t = 0; t < D / 64; ++t) sq[wave][lane + 64 * t] = ld(q + lane + 64 * t);
     __builtin_amdgcn_wave_barrier();
     const KeyTiles<64, WindowMask> tiles(a.mask, position, at_most(position + 1, table.capacity()));
-    const RowSums<T, D> r = paged_row<T, D, 0>(a, table, position, h / (p.n_q_heads / p.n_kv_heads), tiles, 0, tiles.n, [&](int x) { return sq[wave][x]; });
+    const RowSums<T, D> r = paged_row<T, D, 0, 64>(a, table, position, h / (p.n_q_heads / p.n_kv_heads), tiles, 0, tiles.n, [&](int x) { return sq[wave][x]; });
     T *o = (T *)p.o + row * p.o_stride_tok + (int64_t)h * p.o_stride_head;
     const bool none = r.m == -INFINITY && r.z == 0.f;
     for (int t = 0; t < D / 64; ++t) st(o + lane + 64 * t, none ? 0.f : r.acc[t] / r.z);
@@ -121,8 +121,8 @@ int check_common(const char *who, int dtype, int D, int n_tokens, int n_seqs, co
     if (n_tokens < 1 || n_seqs < 1) return fail(CF_EINVAL, "%s: need n_tokens >= 1 and n_seqs >= 1 (got %d, %d)", who, n_tokens, n_seqs);
     if (page_size < 16 || page_size > 65536 || (page_size & (page_size - 1)))
         return fail(CF_EINVAL, "%s: page_size %d must be a power of two from 16 to 65536", who, page_size);
-    if (n_pages < 1 || pages < 1 || (int64_t)pages * page_size > 0x7fffffffLL || table_stride < pages)
-        return fail(CF_EINVAL, "%s: need n_pages >= 1, 1 <= pages_per_seq <= table_stride, pages_per_seq * page_size < 2^31 (got %d, %d, %lld)", who,
+    if (n_pages < 1 || pages < 1 || (int64_t)pages * page_size > (1 << 30) || table_stride < pages)
+        return fail(CF_EINVAL, "%s: need n_pages >= 1, 1 <= pages_per_seq <= table_stride, pages_per_seq * page_size <= 2^30 (got %d, %d, %lld)", who,
                     n_pages, pages, (long long)table_stride);
     if (!cu || !lens || !table) return fail(CF_EINVAL, "%s: NULL device pointer", who);
     if (!aligned(cu, 4) || !aligned(lens, 4) || !aligned(table, 4)) return fail(CF_EINVAL, "%s: misaligned descriptor", who);
@@ -169,16 +169,22 @@ int check_paged(const cf_attn_paged_params *p, const char *who, bool sizes_only,
     return CF_OK;
 }
 
-// The matrix kernel's offsets inside a group of 16 keys have 32 bits.  (Wider rows and calls beyond one launch: a wavefront to a row.)
-bool use_mfma(const PagedArgs &a)
+// The matrix kernels' offsets inside a group of 16 keys have 32 bits, and a HIP launch holds fewer than 2^32 work-items.  (Wider rows and
+// larger calls: a wavefront to a row.)
+enum Path { kRows, kMfma, kF32 };
+Path path_of(const PagedArgs &a)
 {
-    return a.p.dtype == CF_BF16 && !(a.p.flags & CF_FLAG_SCALAR_KERNELS) && a.p.kv_stride_tok < (1 << 25) && paged_mfma_launch_size(a) <= 0xffffffffLL;
+    if ((a.p.flags & CF_FLAG_SCALAR_KERNELS) || a.p.kv_stride_tok >= (1 << 25)) return kRows;
+    if (a.p.dtype == CF_BF16) return paged_mfma_launch_size(a) <= 0xffffffffLL ? kMfma : kRows;
+    return paged_f32_launch_size(a) <= 0xffffffffLL ? kF32 : kRows;
 }
 // Chooses the parts; bytes of workspace.
 int64_t cut(PagedArgs &a)
 {
     a.parts = 1, a.tiles_per_part = 0x7fffffff, a.part_o = nullptr, a.part_ml = nullptr;
-    if (a.p.dtype == CF_BF16 && !(a.p.flags & CF_FLAG_SCALAR_KERNELS)) cut_paged_mfma(a);
+    if (a.p.dtype == CF_BF16) cut_paged_mfma(a);
+    else cut_paged_f32(a);
+    if (path_of(a) == kRows) a.parts = 1;
     if (a.parts == 1) return 0;
     const int64_t rows = (int64_t)a.p.n_tokens * a.p.n_q_heads;
     return a.parts * rows * (a.p.head_dim * 4 + 8);
@@ -215,12 +221,13 @@ extern "C" int cf_attn_paged_fwd(const cf_attn_paged_params *p, void *hip_stream
         a.part_ml = reinterpret_cast<float2 *>(a.part_o + (int64_t)a.parts * p->n_tokens * p->n_q_heads * p->head_dim);
     }
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const cf::Path path = cf::path_of(a);
     hipError_t e;
-    if (cf::use_mfma(a)) {
-        e = cf::launch_paged_mfma(a, s);
-        if (e == hipSuccess && a.parts > 1) e = cf::launch_paged_join(a, s);
-    } else if (p->dtype == CF_FP32) e = p->head_dim == 64 ? cf::run_rows<float, 64>(a, s) : cf::run_rows<float, 128>(a, s);
+    if (path == cf::kMfma) e = cf::launch_paged_mfma(a, s);
+    else if (path == cf::kF32) e = cf::launch_paged_f32(a, s);
+    else if (p->dtype == CF_FP32) e = p->head_dim == 64 ? cf::run_rows<float, 64>(a, s) : cf::run_rows<float, 128>(a, s);
     else e = p->head_dim == 64 ? cf::run_rows<unsigned short, 64>(a, s) : cf::run_rows<unsigned short, 128>(a, s);
+    if (e == hipSuccess && a.parts > 1) e = cf::launch_paged_join(a, s);
     return e == hipSuccess ? CF_OK : cf::fail(CF_EHIP, "%s: %s", who, hipGetErrorString(e));
 }
 

@@ -17,8 +17,7 @@
 
 #include <algorithm>
 
-#include "mfma_common.h"
-#include "paged.h"
+#include "paged_tiles.h"
 
 namespace cf {
 namespace {
@@ -30,109 +29,6 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 constexpr float kLazy = 8.f;                 // log2 units a row maximum may exceed the running reference (attn_mfma_fwd.hip)
 
 __device__ __align__(16) unsigned zeros[64];                 // a row of zeros
-
-// The call's arguments, loaded (again) where this is called.  What a workgroup needs only at its end would stand in scalar registers all the
-// way, and there are too few of them: those of the loops over keys would go to and fro instead.
-__device__ __forceinline__ const PagedArgs &arguments()
-{
-    auto p = (const CF_CONSTANT PagedArgs *)__builtin_amdgcn_kernarg_segment_ptr();
-    asm volatile("" : "+s"(p));
-    return *(const PagedArgs *)p;
-}
-
-// A tile: up to BM token-head rows of a sequence and a key/value head.
-struct TileRows {
-    int seq, q0;                 // sequence, its first row of q
-    int row0, rows;              // first row of the tile among the sequence's token-head rows, and how many it has
-    int first_position;
-    int G, kh;                   // query heads of a key/value head, key/value head
-
-    __device__ __forceinline__ int token(int x) const { return (row0 + x) / G; }
-    __device__ __forceinline__ int position(int x) const { return at_least(-1, first_position + token(x)); }
-    // row of q and head of the tile's row x
-    __device__ __forceinline__ void find(int x, int64_t &row, int &head) const
-    {
-        const int i = token(x);
-        row = q0 + i, head = kh * G + (row0 + x - i * G);
-    }
-    __device__ __forceinline__ int64_t flat(const PagedArgs &a, int x) const
-    {
-        int64_t row;
-        int h;
-        find(x, row, h);
-        return row * a.p.n_q_heads + h;
-    }
-    __device__ __forceinline__ char *out(const PagedArgs &a, int x) const
-    {
-        int64_t row;
-        int h;
-        find(x, row, h);
-        return (char *)a.p.o + (row * a.p.o_stride_tok + (int64_t)h * a.p.o_stride_head) * 2;
-    }
-    __device__ __forceinline__ void put_lse(const PagedArgs &a, int x, float lse) const
-    {
-        int64_t row;
-        int h;
-        find(x, row, h);
-        if (a.p.lse) a.p.lse[(int64_t)h * a.p.n_tokens + row] = lse;
-    }
-};
-
-// Tile `rank`, counted from the last one of the last sequence: sequence g has the ranks from cu[g] * G / BM + g on.
-template <int BM>
-__device__ __forceinline__ bool find_tile(const PagedArgs &a, int rank, TileRows &t)
-{
-    const cf_attn_paged_params &p = a.p;
-    const int32_t *cu = p.cu_seqlens_q;
-    const int lane = threadIdx.x & 63, G = t.G;
-    const int place = (int)((int64_t)p.n_tokens * G / BM) + p.n_seqs - 1 - rank;
-    int lo = 0, hi = p.n_seqs;
-    while (hi - lo > 64) {
-        const int step = (hi - lo + 63) / 64, g = lo + lane * step;
-        const unsigned long long before = __ballot(g < hi && cu[min(g, hi - 1)] * G / BM + g <= place);
-        lo += (63 - __clzll((long long)before)) * step;      // (lane 0 always says yes)
-        hi = min(hi, lo + step);
-    }
-    const int g = min(lo + lane, hi - 1);
-    const int begin = cu[g], end = cu[g + 1], keys = p.kv_lens[g];
-    const int last = 63 - __clzll((long long)__ballot(lo + lane < hi && begin * G / BM + g <= place));
-    t.seq = uniform(lo + last);
-    const int q0 = __builtin_amdgcn_readlane(begin, last), q1 = __builtin_amdgcn_readlane(end, last);
-    const NewRows rows(q0, q1, __builtin_amdgcn_readlane(keys, last));
-    t.q0 = q0;
-    t.row0 = (place - q0 * G / BM - t.seq) * BM;
-    t.rows = at_most(BM, rows.lq * G - t.row0);
-    t.first_position = rows.first_position;
-    return t.rows > 0;
-}
-
-// Where a workgroup's keys stand.
-struct KeySource {
-    const CF_CONSTANT int32_t *table;        // the sequence's row (nothing writes it meanwhile: scalar loads, which no copy in flight holds up)
-    int shift, n_pages, last;    // last: the last key that may be read
-    unsigned row_bytes;
-    int64_t page_bytes;
-    const char *k, *v;           // of this head
-    __device__ __forceinline__ KeySource(const PagedArgs &a, const TileRows &t, int keys)
-        : table((const CF_CONSTANT int32_t *)a.p.block_table + (int64_t)t.seq * a.p.table_stride), shift(a.shift), n_pages(a.p.n_pages), last(keys - 1),
-          row_bytes((unsigned)(a.p.kv_stride_tok * 2)), page_bytes(a.p.page_stride * 2),
-          k((const char *)a.p.k_pages + (int64_t)t.kh * a.p.kv_stride_head * 2), v((const char *)a.p.v_pages + (int64_t)t.kh * a.p.kv_stride_head * 2)
-    {
-    }
-    // The table's entry for keys key .. (a group that lies in one page).  Looked at (is_page) only where the page is used, a tile later: the
-    // load has come by then.
-    __device__ __forceinline__ int entry(int key) const { return table[min(key, last) >> shift]; }
-    __device__ __forceinline__ bool is_page(int entry) const { return (unsigned)entry < (unsigned)n_pages; }
-    __device__ __forceinline__ int page_of(int key) const
-    {
-        const int page = entry(key);
-        return is_page(page) && key <= last ? page : -1;
-    }
-    __device__ __forceinline__ int64_t offset(int page, int key) const
-    {
-        return page * page_bytes + (int64_t)(key & ((1 << shift) - 1)) * row_bytes;
-    }
-};
 
 // Copies a group of GROUP consecutive keys of one page into its place in a swizzled LDS tile, WAVES wavefronts together (an instruction of
 // one of them: RPI rows).
@@ -199,7 +95,7 @@ __device__ __forceinline__ void row_again(const PagedArgs &a, const TileRows &t,
     int h;
     t.find(x, row, h);
     const unsigned short *q = row_of<unsigned short>(a.p.q, (int)row, a.p.q_stride_tok, h, a.p.q_stride_head);
-    const RowSums<unsigned short, D> r = paged_row<unsigned short, D, 4>(a, a.table(t.seq), t.position(x), t.kh, tiles, first, end, [&](int e) { return ld(q + e); });
+    const RowSums<unsigned short, D> r = paged_row<unsigned short, D, 4, BN>(a, a.table(t.seq), t.position(x), t.kh, tiles, first, end, [&](int e) { return ld(q + e); });
     const bool none = r.m == -INFINITY && r.z == 0.f;
     if (a.parts > 1) {
         const int64_t flat = t.flat(a, x);
@@ -357,7 +253,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs &a, const TileRows &t,
     constexpr int TILE = BN * 2 * D, GROUP = 16 * 2 * D, WAVES = D == 128 ? 4 : 2;      // (wavefronts that a group's rows take)
     const int wave = wave_id(), col = F::column(), group = F::group();
     const int x0 = 32 * wave, rows = at_most(32, t.rows - x0);           // this wavefront's rows of the tile (rows <= 0: none)
-    const KeySource src(a, t, keys);
+    const KeySource<2> src(a, t, keys);
     TileDma<BN, D> tile_dma;
     tile_dma.init(src.row_bytes);
     GroupDma<D, 16, WAVES> group_dma;
@@ -481,7 +377,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, 
     constexpr int TILE = FEW * 2 * D, COPIES = TILE / 1024;       // copy instructions of a block's keys
     const int wave = wave_id(), col = F::column(), group = F::group();
     char *k_tile = k_stage + wave * TILE, *v_tile = v_stage + wave * TILE;
-    const KeySource src(a, t, keys);
+    const KeySource<2> src(a, t, keys);
     GroupDma<D, 32, 1> dma;
     dma.init(src.row_bytes, 0);
     GroupDma<D, 16, 1> half_dma;
@@ -689,8 +585,11 @@ void cut_paged_mfma(PagedArgs &a)
     int64_t tiles = (keys + BN - 1) / BN;
     if (p.window > 0) tiles = std::min(tiles, ((int64_t)p.window + BM / G) / BN + 2 + ((int64_t)a.mask.sinks + BN - 1) / BN);
     const int64_t groups = tiles_most(p) * p.n_kv_heads, slots = 512;
-    const int64_t parts = std::min<int64_t>({(8 * slots + groups - 1) / groups, (tiles + 1) / 2, kMostParts});
-    a.parts = groups >= 4 * slots ? 1 : (int)std::max<int64_t>(1, parts);
+    // Workgroup slots' rounds, and from how many on a call is left whole.  Parts of many rows leave and read again 128 KB of results each.
+    const Mode mode = mode_of(p);
+    const int64_t rounds = mode == kMany ? 1 : mode == kFew ? 4 : 8, enough = mode == kMany ? 1 : 4;
+    const int64_t parts = std::min<int64_t>({(rounds * slots + groups - 1) / groups, (tiles + 1) / 2, kMostParts});
+    a.parts = groups >= enough * slots ? 1 : (int)std::max<int64_t>(1, parts);
     a.tiles_per_part = (int)((tiles + a.parts - 1) / a.parts);
 }
 

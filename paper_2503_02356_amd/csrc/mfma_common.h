@@ -301,7 +301,7 @@ __device__ __forceinline__ bool crosses_window(const WindowMask &m, int position
 
 // Keys between a row's sinks and its window: key j is hidden iff (unsigned)(j - sinks) is less (one compare, whose result needs no scalar
 // registers: two of them and an "and" for each of a tile's elements did not fit these).
-__device__ __forceinline__ unsigned hidden_keys(const WindowMask &m, int position) { return (unsigned)max(0, position + 1 - m.window - m.sinks); }
+__device__ __forceinline__ unsigned hidden_keys(const WindowMask &m, int position) { return (unsigned)max(0, max(0, position + 1 - m.window) - m.sinks); }
 
 // Makes a pointer / an int that is the same in every lane known as such to the compiler.
 template <typename T>

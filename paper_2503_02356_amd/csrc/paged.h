@@ -25,14 +25,14 @@ struct PagedArgs {
     __device__ __forceinline__ NewRows rows(int seq) const { return NewRows(p.cu_seqlens_q[seq], p.cu_seqlens_q[seq + 1], p.kv_lens[seq]); }
 };
 
-// One row's softmax over the visible keys of tiles [first, end) of `tiles`: maximum (natural units), sum and unnormalised result, element
+// One row's softmax over the visible keys of tiles [first, end) of `tiles` (TILE <= 64 keys, a lane to a key): maximum (natural units), sum and unnormalised result, element
 // lane + 64 t.
 template <typename T, int D>
 struct RowSums {
     float m = -INFINITY, z = 0.f, acc[D / 64] = {};
 };
-template <typename T, int D, int UNROLL, typename Q>
-__device__ inline RowSums<T, D> paged_row(const PagedArgs &a, const PageTable &table, int position, int kh, const KeyTiles<64, WindowMask> &tiles,
+template <typename T, int D, int UNROLL, int TILE, typename Q>
+__device__ inline RowSums<T, D> paged_row(const PagedArgs &a, const PageTable &table, int position, int kh, const KeyTiles<TILE, WindowMask> &tiles,
                                           int first, int end, Q q)
 {
     const cf_attn_paged_params &p = a.p;
@@ -40,7 +40,7 @@ __device__ inline RowSums<T, D> paged_row(const PagedArgs &a, const PageTable &t
     RowSums<T, D> r;
     for (int t = first; t < end; ++t) {
         const int j = tiles.start(t) + lane;
-        const bool seen = j <= position && (j > position - a.mask.window || j < a.mask.sinks);
+        const bool seen = lane < TILE && j <= position && (j > position - a.mask.window || j < a.mask.sinks);
         const int page = seen ? table.page_of(j) : -1;
         const int64_t at = (int64_t)max(page, 0) * p.page_stride + (int64_t)table.row_in_page(j) * p.kv_stride_tok + (int64_t)kh * p.kv_stride_head;
         float s = -INFINITY;
@@ -74,6 +74,10 @@ hipError_t launch_paged_mfma(const PagedArgs &a, hipStream_t s);
 int64_t paged_mfma_launch_size(const PagedArgs &a);      // work-items
 // Cuts a call's keys into parts: sets parts and tiles_per_part.
 void cut_paged_mfma(PagedArgs &a);
+// fp32 matrix kernel (attn_paged_f32.hip): the same.
+hipError_t launch_paged_f32(const PagedArgs &a, hipStream_t s);
+int64_t paged_f32_launch_size(const PagedArgs &a);
+void cut_paged_f32(PagedArgs &a);
 // Joins the parts of every row (one call's parts > 1).
 hipError_t launch_paged_join(const PagedArgs &a, hipStream_t s);
 

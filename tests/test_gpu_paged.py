@@ -123,7 +123,7 @@ def test_against_the_definition(dtype, D, flags, s):
 @pytest.mark.parametrize("dtype,D,flags", KINDS)
 def test_windows_and_pages_that_were_given_back(dtype, D, flags):
     """Pages behind the windows of all rows are marked, and their content is gone."""
-    for n, (window, sinks, page) in enumerate([(1, 0, 16), (64, 4, 16), (65, 64, 32), (500, 1, 128), (2000, 0, 16), (40, 200, 64)]):
+    for n, (window, sinks, page) in enumerate([(1, 0, 16), (64, 4, 16), (65, 64, 32), (500, 1, 128), (2000, 0, 16), (40, 200, 64), (2**31 - 1, 1000, 16)]):
         seqs = [(1, 1500), (33, 900), (1, 30), (200, 200), (2, 130)]
         hidden = {(i, c): -1 for i, (a, m) in enumerate(seqs) for c in range(-(-m // page)) if (c + 1) * page <= m - a - window + 1 and c * page >= sinks}
         assert n not in (1, 3) or len(hidden) > 5
