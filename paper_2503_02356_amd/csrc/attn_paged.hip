@@ -37,38 +37,78 @@ __global__ __launch_bounds__(kWaves * 64) void paged_rows_kernel(PagedArgs a)
     if (lane == 0 && p.lse) p.lse[(int64_t)h * p.n_tokens + row] = none ? -INFINITY : r.m + logf(r.z);
 }
 
-// O and LSE of the rows from their parts: a wavefront to a row, a lane to a part's maximum and sum, then to some elements of the result.
-// Reads each part once; the parts' order is fixed, so are the bits.
-template <typename T, int D>
+// O and LSE of the rows from their parts: WAVES wavefronts to a row, a lane to a part's maximum and sum, then to some elements of every
+// WAVES-th part's result.  The order of the sums is fixed, so are the bits.  Bound by latency where there are few rows, else by the parts'
+// bytes.  More than 16 parts: four wavefronts, 16 parts in flight each, the first ones before the weights are known (one token behind 8192
+// keys, 32/8 heads, 64 parts: the whole call 13.9 us, with one wavefront and 8 in flight 17.4).  Fewer: one, 8 in flight, and only parts that
+// had keys are read (256 tokens of 16 heads, 5 parts: 68 us, 75 with four wavefronts).
+template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(kWaves * 64) void paged_join_kernel(PagedArgs a)
 {
     const cf_attn_paged_params &p = a.p;
-    const int lane = threadIdx.x & 63;
-    const int64_t rows = (int64_t)min(p.n_tokens, p.cu_seqlens_q[p.n_seqs]) * p.n_q_heads, all = (int64_t)p.n_tokens * p.n_q_heads;
-    const int64_t r = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    if (r >= rows) return;
+    constexpr int E = D / 64, AT_ONCE = WAVES == 1 ? 8 : 16;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = wave % WAVES;
+    const int64_t all = (int64_t)p.n_tokens * p.n_q_heads, r = (int64_t)blockIdx.x * (kWaves / WAVES) + wave / WAVES;
+    const bool inside = r < all;                     // (part_o and part_ml hold all rows, also those of a padded batch that nobody wrote)
+    const float *o_parts = a.part_o + (inside ? r : 0) * D + lane * E;
+    float v[AT_ONCE][E], acc[E] = {};
+    auto fetch = [&](int x, int part) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[x][e] = o_parts[(int64_t)part * all * D + e];
+    };
+    auto add = [&](int x, float w) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += w == 0.f ? 0.f : w * v[x][e];      // (a part without keys holds anything)
+    };
+    auto fetch_every = [&](int x0) {
+#pragma unroll
+        for (int x = 0; x < AT_ONCE; ++x) fetch(x, min(x0 + WAVES * x, a.parts - 1));
+    };
+    if (WAVES > 1) fetch_every(sub);
     float2 ml = {-INFINITY, 0.f};
-    if (lane < a.parts) ml = a.part_ml[r * a.parts + lane];
+    if (inside && lane < a.parts) ml = a.part_ml[r * a.parts + lane];
+    const int64_t rows = (int64_t)min(p.n_tokens, p.cu_seqlens_q[p.n_seqs]) * p.n_q_heads;
     const float M = wave_max(ml.x), ref = M == -INFINITY ? 0.f : M;
     const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - ref);
     const float L = wave_sum(w * ml.y);
-    // (parts without keys hold anything, and count 0 times: whatever it is, it is left out.  Eight at a time: a latency for eight)
-    constexpr int E = D / 64, AT_ONCE = 8;
-    float acc[E] = {};
-    const float *o_parts = a.part_o + r * D + lane * E;
-    for (int x0 = 0; x0 < a.parts; x0 += AT_ONCE) {
-        float v[AT_ONCE][E];
+    if constexpr (WAVES == 1) {
+        for (unsigned long long left = __ballot(ml.x != -INFINITY); left != 0;) {
+            int at[AT_ONCE], n = 0;
 #pragma unroll
-        for (int x = 0; x < AT_ONCE; ++x)
+            for (int x = 0; x < AT_ONCE; ++x) {      // (the last one again where there are no more)
+                at[x] = left != 0 ? __ffsll((long long)left) - 1 : at[x > 0 ? x - 1 : 0];
+                n += left != 0;
+                left &= left - 1;
+                fetch(x, at[x]);
+            }
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[x][e] = o_parts[(int64_t)min(x0 + x, a.parts - 1) * all * D + e];
-#pragma unroll
-        for (int x = 0; x < AT_ONCE; ++x) {
-            const float wx = x0 + x < a.parts ? __shfl(w, x0 + x) : 0.f;
-#pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] += wx == 0.f ? 0.f : wx * v[x][e];
+            for (int x = 0; x < AT_ONCE; ++x) {
+                const float wx = __shfl(w, at[x]);
+                add(x, x < n ? wx : 0.f);
+            }
         }
+    } else {
+        for (int x0 = sub;;) {
+#pragma unroll
+            for (int x = 0; x < AT_ONCE; ++x) {
+                const int at = x0 + WAVES * x;
+                const float wx = __shfl(w, at & 63);
+                add(x, at < a.parts ? wx : 0.f);
+            }
+            x0 += WAVES * AT_ONCE;
+            if (x0 >= a.parts) break;
+            fetch_every(x0);
+        }
+        __shared__ float sums[kWaves][E][64];
+#pragma unroll
+        for (int e = 0; e < E; ++e) sums[wave][e][lane] = acc[e];
+        __syncthreads();
+        if (sub != 0) return;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            for (int x = 1; x < WAVES; ++x) acc[e] += sums[wave + x][e][lane];
     }
+    if (r >= rows) return;
     const int64_t row = r / p.n_q_heads, h = r - row * p.n_q_heads;
     T *o = (T *)p.o + row * p.o_stride_tok + h * p.o_stride_head;
     const float inv = M == -INFINITY ? 0.f : 1.f / L;
@@ -85,7 +125,17 @@ __global__ __launch_bounds__(256) void kv_append_kernel(cf_kv_append_params p, i
     const int64_t row = id / per_row;
     if (row >= min(p.n_tokens, p.cu_seqlens_q[p.n_seqs])) return;
     const int rest = (int)(id - row * per_row), h = rest / units, unit = rest - h * units;
-    const int seq = find_segment(p.cu_seqlens_q, p.n_seqs, (int)row);
+    // The sequence of the wavefront's first row, 64 bounds at a time; the others' are that or one of the next.
+    const int lane = threadIdx.x & 63, first = __builtin_amdgcn_readfirstlane((int)row);
+    int lo = 0, hi = p.n_seqs;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64, g = lo + lane * step;
+        const unsigned long long before = __ballot(g < hi && p.cu_seqlens_q[min(g, hi - 1)] <= first);
+        lo += (63 - __clzll((long long)before)) * step;      // (lane 0 is in it, and always says yes)
+        hi = min(hi, lo + step);
+    }
+    int seq = lo;
+    while (p.cu_seqlens_q[seq + 1] <= row) ++seq;
     const NewRows rows(p.cu_seqlens_q[seq], p.cu_seqlens_q[seq + 1], p.kv_lens[seq]);
     const PageTable table{p.block_table + (int64_t)seq * p.table_stride, p.pages_per_seq, shift, p.n_pages};
     const int position = rows.position((int)row - rows.q0), page = table.page_of(position);
@@ -107,7 +157,9 @@ hipError_t run_rows(const PagedArgs &a, hipStream_t s)
 template <typename T, int D>
 hipError_t run_join(const PagedArgs &a, hipStream_t s)
 {
-    paged_join_kernel<T, D><<<dim3((unsigned)(((int64_t)a.p.n_tokens * a.p.n_q_heads + kWaves - 1) / kWaves)), kWaves * 64, 0, s>>>(a);
+    const int64_t rows = (int64_t)a.p.n_tokens * a.p.n_q_heads;
+    if (a.parts > 16 && rows <= 0x7fffffffLL / (kWaves * 64)) paged_join_kernel<T, D, 4><<<dim3((unsigned)rows), kWaves * 64, 0, s>>>(a);
+    else paged_join_kernel<T, D, 1><<<dim3((unsigned)((rows + kWaves - 1) / kWaves)), kWaves * 64, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -540,8 +540,10 @@ __global__ __launch_bounds__(256, 2) void mfma_paged_kernel(PagedArgs a)
     const int lowest = t.position(0), highest = t.position(t.rows - 1);
     const int keys = at_most(highest + 1, a.p.pages_per_seq << a.shift);
     const KeyTiles<BN, WindowMask> tiles(a.mask, lowest, keys);
-    const int n = at_least(0, tiles.n), first = at_most(n, a.parts > 1 ? part * a.tiles_per_part : 0);
-    const int end = a.parts > 1 && part + 1 < a.parts ? at_most(n, first + a.tiles_per_part) : n;
+    // (BOTH: tiles of many rows are cut a third as often, for a part of them leaves four times as much to be joined)
+    const int thirds = MODE == kBoth && t.rows > FEW ? 3 : 1, per_part = a.tiles_per_part * thirds, last_part = (a.parts - 1) / thirds;
+    const int n = at_least(0, tiles.n), first = at_most(n, a.parts == 1 ? 0 : part > last_part ? n : part * per_part);
+    const int end = a.parts > 1 && part < last_part ? at_most(n, first + per_part) : n;
     if (first >= end) {                              // no keys: what is left of the rows
         const PagedArgs &e = arguments();
         for (int x = threadIdx.x; x < t.rows && e.parts > 1; x += 256) e.part_ml[t.flat(e, x) * e.parts + part] = make_float2(-INFINITY, 0.f);
@@ -576,7 +578,10 @@ int64_t tiles_most(const cf_attn_paged_params &p)
 
 int64_t paged_mfma_launch_size(const PagedArgs &a) { return tiles_most(a.p) * a.p.n_kv_heads * a.parts * 256; }
 
-// Parts: so many that the chip's 512 workgroup slots each get several, of two key tiles at least.
+// Parts: so many that the chip's 512 workgroup slots each get several, of four key tiles at least (two blocks of 32 keys to a wavefront; 32/8
+// heads, us, parts of at least 2 / 4 / 6 tiles: one token behind 2000 keys 10.2 / 10.3 / 11.0, 8192 13.9 / 13.6 / 13.7, 4 behind up to 8192
+// 24.7 / 21.9 / 18.9).  Rounds of slots, tokens: 64 behind up to 16384 keys 486 us with 4, 442 with 5, 459 with 8, 443 with 12; 128 behind up
+// to 2048 138 / 131 / 149 / 141.
 void cut_paged_mfma(PagedArgs &a)
 {
     const cf_attn_paged_params &p = a.p;
@@ -587,8 +592,8 @@ void cut_paged_mfma(PagedArgs &a)
     const int64_t groups = tiles_most(p) * p.n_kv_heads, slots = 512;
     // Workgroup slots' rounds, and from how many on a call is left whole.  Parts of many rows leave and read again 128 KB of results each.
     const Mode mode = mode_of(p);
-    const int64_t rounds = mode == kMany ? 1 : mode == kFew ? 4 : 8, enough = mode == kMany ? 1 : 4;
-    const int64_t parts = std::min<int64_t>({(rounds * slots + groups - 1) / groups, (tiles + 1) / 2, kMostParts});
+    const int64_t rounds = mode == kMany ? 1 : mode == kFew ? 5 : 8, enough = mode == kMany ? 1 : 4;
+    const int64_t parts = std::min<int64_t>({(rounds * slots + groups - 1) / groups, (tiles + 3) / 4, kMostParts});
     a.parts = groups >= enough * slots ? 1 : (int)std::max<int64_t>(1, parts);
     a.tiles_per_part = (int)((tiles + a.parts - 1) / a.parts);
 }
