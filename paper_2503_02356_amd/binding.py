@@ -414,6 +414,30 @@ def _window(window, n_sinks):
     return C.byref(AttnWindow(int(window), int(n_sinks)))
 
 
+class Attention:
+    """The calls of one kind of attention over a chunk: causal, or with a window (keys that a query sees, itself among them) and sinks."""
+
+    def __init__(self, window=None, n_sinks=0):
+        if window is None and n_sinks:
+            raise ValueError("n_sinks needs a window")
+        self.window, self.n_sinks = window, int(n_sinks)
+        if window is not None and (int(window) < 1 or int(n_sinks) < 0):
+            raise ValueError(f"need window >= 1 and n_sinks >= 0 (got {window}, {n_sinks})")
+
+    def fwd(self, params, stream=None):
+        cf_attn_fwd(params, stream) if self.window is None else cf_attn_window_fwd(params, self.window, self.n_sinks, stream)
+
+    def bwd(self, params, stream=None):
+        cf_attn_bwd(params, stream) if self.window is None else cf_attn_window_bwd(params, self.window, self.n_sinks, stream)
+
+    def bwd_workspace_bytes(self, params):
+        return (cf_attn_bwd_workspace_bytes(params) if self.window is None else
+                cf_attn_window_bwd_workspace_bytes(params, self.window, self.n_sinks))
+
+    def count_pairs(self, cu_q, cu_k):
+        return cf_count_pairs(cu_q, cu_k) if self.window is None else cf_count_window_pairs(cu_q, cu_k, self.window, self.n_sinks)
+
+
 def cf_attn_window_fwd(params, window, n_sinks=0, stream=None):
     """cf_attn_fwd's call with a sliding window: a query sees its last `window` keys and its sequence's first n_sinks."""
     _check(lib().cf_attn_window_fwd(C.byref(params), _window(window, n_sinks), stream if stream is not None else _stream()))

@@ -44,7 +44,8 @@ class _Slot:
 
 
 class SlotExecutor:
-    def __init__(self, plan, n_q_heads, n_kv_heads, head_dim, dtype, K, scale=None, device="cuda:0", flags=0):
+    def __init__(self, plan, n_q_heads, n_kv_heads, head_dim, dtype, K, scale=None, device="cuda:0", flags=0, window=None, n_sinks=0):
+        self.attn = B.Attention(window, n_sinks)      # (as in runner.ChunkAttention)
         self.plan, self.Hq, self.Hkv, self.D, self.K = plan, n_q_heads, n_kv_heads, head_dim, int(K)
         self.tdtype = torch.bfloat16 if dtype == "bf16" else torch.float32
         self.scale = float(scale) if scale is not None else 1.0 / float(np.sqrt(head_dim))
@@ -118,7 +119,7 @@ class SlotExecutor:
         self.state = None       # (group, k, v, dk, dv) of the split sequence being processed
 
     def _ensure_workspace(self, fp):
-        need = B.cf_attn_bwd_workspace_bytes(fp)
+        need = self.attn.bwd_workspace_bytes(fp)
         if need > self._ws_bytes:
             self.workspace = torch.empty(need, dtype=torch.uint8, device=self.dev)
             self._ws_bytes = need
@@ -176,7 +177,7 @@ class SlotExecutor:
             self.kv[0][:T].copy_(h["k"], non_blocking=True)
             self.kv[1][:T].copy_(h["v"], non_blocking=True)
         fp = self._params(c, slot)
-        B.cf_attn_fwd(fp)
+        self.attn.fwd(fp)
         self.n_forward += 1
         h["o"].copy_(slot.o[:T], non_blocking=True)          # what the next layer consumes
         h["lse"].copy_(slot.lse[:self.Hq * T].view(self.Hq, T), non_blocking=True)
@@ -200,7 +201,7 @@ class SlotExecutor:
         else:
             self.dkv[:, :T].zero_()
             dk, dv = self.dkv[0][:T], self.dkv[1][:T]
-        B.cf_attn_bwd(B.make_bwd_params(fp, self.d_o[:T], self.d_q[:T], dk, dv, self.workspace))
+        self.attn.bwd(B.make_bwd_params(fp, self.d_o[:T], self.d_q[:T], dk, dv, self.workspace))
         self.n_backward += 1
         h["d_q"].copy_(self.d_q[:T], non_blocking=True)
         if "dk" in h:

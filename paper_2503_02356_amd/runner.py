@@ -34,10 +34,15 @@ def calls_together(ws_bytes):
 
 class ChunkAttention:
     def __init__(self, plan, n_q_heads, n_kv_heads, head_dim, dtype, scale=None, device="cuda:0", flags=0,
-                 n_streams=1, fused_launch=False, only_groups=None, tile_tables=True):
+                 n_streams=1, fused_launch=False, only_groups=None, tile_tables=True, window=None, n_sinks=0):
         """n_streams > 1: dependency groups are dealt over that many HIP streams (default priority), so that
         the last, partly filled wave of workgroups of one chunk's kernel overlaps with the next group's
-        kernels.  The chunks of one group stay on one stream, in the order of section 4.2."""
+        kernels.  The chunks of one group stay on one stream, in the order of section 4.2.
+        window, n_sinks: every query sees its last `window` keys and its sequence's first n_sinks (None: all keys before it); a call per
+        chunk then, without fused_launch."""
+        self.attn = B.Attention(window, n_sinks)
+        if window is not None and fused_launch:
+            raise ValueError("a window goes by a call per chunk: fused_launch takes none")
         self.plan, self.Hq, self.Hkv, self.D = plan, n_q_heads, n_kv_heads, head_dim
         self.n_streams = max(1, int(n_streams))
         # fused_launch: run_forward / run_backward hand the whole plan to cf_attn_fwd_batch / cf_attn_bwd_batch
@@ -171,12 +176,12 @@ class ChunkAttention:
                     ch["v"][a:b].copy_(up(vals["v"]))
                 ch["cu_k_host"] = cu.copy()
             ch["cu_k"] = torch.from_numpy(ch["cu_k_host"].copy()).to(dev)
-            ch["pairs"] = B.cf_count_pairs(ch["cu_q_host"], ch["cu_k_host"])
+            ch["pairs"] = self.attn.count_pairs(ch["cu_q_host"], ch["cu_k_host"])
             if self.tile_tables:
                 ch["q_tiles"] = torch.from_numpy(B.cf_attn_q_tiles(ch["cu_q_host"], ch["cu_k_host"])).to(dev)
             ch["fwd"] = B.make_fwd_params(ch["q"], ch["k"], ch["v"], ch["o"], ch["lse"], ch["cu_q"], ch["cu_k"],
                                           self.scale, self.flags, q_tiles=ch.get("q_tiles"))
-            ws_bytes = max(ws_bytes, B.cf_attn_bwd_workspace_bytes(ch["fwd"]))
+            ws_bytes = max(ws_bytes, self.attn.bwd_workspace_bytes(ch["fwd"]))
             self.chunks.append(ch)
         # Calls in flight together need a backward workspace each: one per stream, and on a single stream as many in turn
         # as backward calls share a launch.
@@ -233,7 +238,7 @@ class ChunkAttention:
         for bwd, c in ops:
             ch = self.chunks[c]
             handle = B.C.c_void_p(self.streams[ch["lane"]].cuda_stream)
-            (B.cf_attn_bwd if bwd else B.cf_attn_fwd)(ch["bwd" if bwd else "fwd"], handle)
+            (self.attn.bwd if bwd else self.attn.fwd)(ch["bwd" if bwd else "fwd"], handle)
         for st in self.streams:
             done = torch.cuda.Event()
             done.record(st)
@@ -244,6 +249,12 @@ class ChunkAttention:
         stream, one cf_attn_fwd / cf_attn_bwd call per op, in a list that is laid out once, like the plan."""
         if self.streams:
             self._launch(make_ops())
+            return
+        if self.attn.window is not None:
+            if key not in self._calls:
+                self._calls[key] = [(self.attn.bwd, self.chunks[c]["bwd"]) if bwd else (self.attn.fwd, self.chunks[c]["fwd"]) for bwd, c in make_ops()]
+            for call, params in self._calls[key]:
+                call(params)
             return
         if key not in self._calls:
             self._calls[key] = B.make_calls((bwd, self.chunks[c]["bwd" if bwd else "fwd"]) for bwd, c in make_ops())
