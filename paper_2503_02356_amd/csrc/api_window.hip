@@ -22,7 +22,8 @@ bool use_window_mfma(const cf_attn_bwd_params &b, const cf::WindowMask &mask)
 }
 int64_t window_scratch(const cf_attn_fwd_params &p, const cf::WindowMask &mask)
 {
-    return delta_bytes(p) + (mfma_shape(p) ? 256 + cf::window_worklist_capacity(p, mask) * 16 : 0);
+    // (the scalar kernels' delta, whatever runs; behind it the list of the bf16 kernels or the sums of the fp32 one)
+    return delta_bytes(p) + (mfma_shape(p) ? 256 + cf::window_worklist_capacity(p, mask) * 16 : p.dtype == CF_FP32 ? cf::window_f32_scratch(p, mask) : 0);
 }
 
 }  // namespace
@@ -34,7 +35,7 @@ extern "C" int cf_attn_window_fwd(const cf_attn_fwd_params *p, const cf_attn_win
     if (int rc = check_fwd(p, who, false)) return rc;
     if (int rc = check_window(w, p->n_kv_tokens, who, &mask)) return rc;
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    const hipError_t e = use_window_mfma(*p) ? cf::launch_window_mfma_fwd(*p, mask, s)
+    const hipError_t e = use_window_mfma(*p) ? (cf::window_few(*p) ? cf::launch_window_few(*p, mask, s) : cf::launch_window_mfma_fwd(*p, mask, s))
                          : use_f32(*p)       ? cf::launch_window_f32_fwd(*p, mask, s)
                                              : cf::launch_window_simple_fwd(*p, mask, s);
     return e == hipSuccess ? CF_OK : hip_fail(who, e);
@@ -67,7 +68,7 @@ extern "C" int cf_attn_window_bwd(const cf_attn_bwd_params *b, const cf_attn_win
     }
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const hipError_t e = use_window_mfma(*b, mask) ? cf::launch_window_mfma_bwd(*b, ws, mask, s)
-                         : use_f32(*b)             ? cf::launch_window_f32_bwd(*b, mask, s)
+                         : use_f32(*b)             ? cf::launch_window_f32_bwd(*b, ws.delta + delta_bytes(b->f) / 4, mask, s)
                                                    : cf::launch_window_simple_bwd(*b, ws, mask, s);
     return e == hipSuccess ? CF_OK : hip_fail(who, e);
 }

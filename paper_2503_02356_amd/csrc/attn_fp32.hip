@@ -277,10 +277,37 @@ __device__ __forceinline__ void f32_dq_body(const BwdArgs &b, int id, char *smem
     });
 }
 
+// The far rows of a window's sinks, those that see a sink behind their window, are most of a long slice's rows, and its first key blocks would
+// be the work of one workgroup each.  FAR: they are cut into pieces of kFarRows rows, each with a workgroup of its own that leaves its
+// sums in the workspace (place of the piece: cu_q / kFarRows + segment + number in the segment); a small kernel behind adds these up in order,
+// so that the gradients stay reproducible.  NEAR: a key block without its far rows.  1000 rows behind 300 keys, 6/2 heads, D = 128, window 200,
+// 2 sinks, forward and backward: 171 us with ALL, 84 so (without sinks 69).
+enum RowsOf { kAllRows, kNearRows, kFarPieces };
+constexpr int kFarRows = 256;
+struct FarSums {
+    float *sums;                 // [place][kv head][sink block][dV, dK][16 keys][D]
+    int blocks;                  // blocks of 16 keys that hold sinks
+};
+// Query blocks of key block k0 that are near ones, and where its far ones begin.
+template <typename Mask>
+__device__ __forceinline__ QueryTiles<RB> near_blocks(const Mask &mask, int k0, int rows, int off, int lq) { return QueryTiles<RB>(mask, k0, k0 + rows, off, lq); }
+__device__ __forceinline__ QueryTiles<RB> near_blocks(const WindowMask &mask, int k0, int rows, int off, int lq)
+{
+    QueryTiles<RB> t(WindowMask{mask.window, 0}, k0, k0 + rows, off, lq);
+    t.end = max(t.first, t.end);
+    return t;
+}
+
+template <int D>
+__device__ __forceinline__ float *far_sums(const FarSums &far, const BwdArgs::Fwd &p, int place, int kh, int block, int which)
+{
+    return far.sums + ((((int64_t)place * p.n_kv_heads + kh) * far.blocks + block) * 2 + which) * (RB * D);
+}
+
 // dK, dV of 16 key rows of one key/value head: (query head of the group, 16-row query block) pairs dealt over the
 // wavefronts.
-template <int D, bool CHAINS, typename Mask>
-__device__ __forceinline__ void f32_dkv_body(const BwdArgs &b, int id, char *smem, float (*stat)[2 * RB], const Mask &mask)
+template <int D, bool CHAINS, typename Mask, RowsOf ROWS = kAllRows>
+__device__ __forceinline__ void f32_dkv_body(const BwdArgs &b, int id, char *smem, float (*stat)[2 * RB], const Mask &mask, const FarSums &far = FarSums())
 {
     using S = Shape<D>;
     // In D = 128's kernel of chains dK/dV fills the 128 registers, and what the compiler keeps of the lane from one use to the next, or over
@@ -293,12 +320,30 @@ __device__ __forceinline__ void f32_dkv_body(const BwdArgs &b, int id, char *sme
     const int lane = threadIdx.x & 63, wave = wave_id(), quarter = lane >> 4, col = lane & 15;
     const int G = p.n_q_heads / p.n_kv_heads, kh = id % p.n_kv_heads;
     TileLocation loc;
-    if (!locate_tile<ANEW>(p.cu_seqlens_k, p.cu_seqlens_q, p.n_segments, p.n_kv_tokens, RB, id / p.n_kv_heads, loc)) return;
+    int far_place = 0, far_block = 0;
+    if constexpr (ROWS == kFarPieces) {
+        far_block = id / p.n_kv_heads % far.blocks;
+        TileLocation q;
+        if (!locate_tile<ANEW>(p.cu_seqlens_q, p.cu_seqlens_k, p.n_segments, p.n_tokens, kFarRows, id / p.n_kv_heads / far.blocks, q)) return;
+        far_place = uniform(q.begin / kFarRows + q.seg + q.tile_in_seg);
+        loc = TileLocation{q.seg, q.tile_in_seg, q.other_begin, q.other_len, q.begin, q.len};
+    } else if (!locate_tile<ANEW>(p.cu_seqlens_k, p.cu_seqlens_q, p.n_segments, p.n_kv_tokens, RB, id / p.n_kv_heads, loc)) return;
     const int lk = uniform(loc.len), lq = uniform(loc.other_len), off = lk - lq;
     // (tiles are numbered from a segment's end; its FIRST key tiles are seen by the most rows: start with those)
-    const int k0 = ((lk + RB - 1) / RB - 1 - uniform(loc.tile_in_seg)) * RB, rows = min(RB, lk - k0);
+    const int k0 = ROWS == kFarPieces ? far_block * RB : ((lk + RB - 1) / RB - 1 - uniform(loc.tile_in_seg)) * RB, rows = min(RB, lk - k0);
+    if (ROWS == kFarPieces && rows <= 0) return;
     const QueryTiles<RB> seen_by(mask, k0, k0 + rows, off, lq);
-    const int qb_first = seen_by.first, n_qb = seen_by.end - qb_first;
+    int qb_first = seen_by.first, qb_end = seen_by.end;
+    if constexpr (ROWS != kAllRows) {
+        const int near_end = near_blocks(mask, k0, rows, off, lq).end;
+        if (ROWS == kNearRows) {
+            qb_end = min(qb_end, near_end);
+        } else {
+            const int piece = uniform(loc.tile_in_seg) * (kFarRows / RB);
+            qb_first = max(max(qb_first, near_end), piece), qb_end = min(qb_end, piece + kFarRows / RB);
+        }
+    }
+    const int n_qb = qb_end - qb_first;
     if (n_qb <= 0) return;
     const int n_items = G * n_qb;
     stage_rows<D, ANEW>((const float *)p.k + (int64_t)loc.begin * p.kv_stride_tok + (int64_t)kh * p.kv_stride_head, p.kv_stride_tok, k0, lk - 1, ks);
@@ -370,8 +415,9 @@ __device__ __forceinline__ void f32_dkv_body(const BwdArgs &b, int id, char *sme
         const int which = TOGETHER == 1 ? first : t / (rows * (D / 4));
         const bool mine = t < TOGETHER * rows * (D / 4);
         f32x4 *to = (f32x4 *)((which ? b.d_k : b.d_v) + (int64_t)(loc.begin + k0 + r) * b.dkv_stride_tok + (int64_t)kh * b.dkv_stride_head + c * 4);
+        if constexpr (ROWS == kFarPieces) to = (f32x4 *)(far_sums<D>(far, p, far_place, kh, far_block, which) + r * D + c * 4);
         f32x4 held = {0.f, 0.f, 0.f, 0.f}, a = held;
-        if (mine) held = *to;
+        if (mine && ROWS != kFarPieces) held = *to;
         if (first == 0) lds_turn();
         else __syncthreads();
         if (wave < n_items) {
@@ -391,11 +437,23 @@ __device__ __forceinline__ void f32_dkv_body(const BwdArgs &b, int id, char *sme
             const SegmentRows g{loc.other_begin, lq, loc.begin, lk};
             const float *kr = row_of<float>(p.k, krow, p.kv_stride_tok, kh, p.kv_stride_head), *vr = row_of<float>(p.v, krow, p.kv_stride_tok, kh, p.kv_stride_head);
             float gk[D / 64], gv[D / 64];
-            scalar_dkv_row<float, D, 4>(b, g, krow, kh, [&](int x) { return kr[x]; }, [&](int x) { return vr[x]; },
-                                        [&](int row, int h) { return scalar_delta<float, D>(b, g, row, h, mask); }, gk, gv, mask);
-            float *dst = (is_k ? b.d_k : b.d_v) + (int64_t)krow * b.dkv_stride_tok + (int64_t)kh * b.dkv_stride_head;
+            if constexpr (ROWS == kAllRows) {
+                scalar_dkv_row<float, D, 4>(b, g, krow, kh, [&](int x) { return kr[x]; }, [&](int x) { return vr[x]; },
+                                            [&](int row, int h) { return scalar_delta<float, D>(b, g, row, h, mask); }, gk, gv, mask);
+            } else {
 #pragma unroll
-            for (int x = 0; x < D / 64; ++x) dst[end_lane + 64 * x] += is_k ? gk[x] * p.softmax_scale : gv[x];
+                for (int x = 0; x < D / 64; ++x) gk[x] = gv[x] = 0.f;
+                for (int h = kh * G; h < (kh + 1) * G; ++h)
+                    scalar_dkv_rows<float, D, 4>(b, g, krow, h, qb_first * RB, min(qb_end * RB, lq), [&](int x) { return kr[x]; }, [&](int x) { return vr[x]; },
+                                                 [&](int row, int h) { return scalar_delta<float, D>(b, g, row, h, mask); }, gk, gv, mask);
+            }
+            float *dst = (is_k ? b.d_k : b.d_v) + (int64_t)krow * b.dkv_stride_tok + (int64_t)kh * b.dkv_stride_head;
+            if constexpr (ROWS == kFarPieces) dst = far_sums<D>(far, p, far_place, kh, far_block, is_k) + (first / (D / 4) % rows) * D;
+#pragma unroll
+            for (int x = 0; x < D / 64; ++x) {
+                const float add = is_k ? gk[x] * p.softmax_scale : gv[x];
+                dst[end_lane + 64 * x] = ROWS == kFarPieces ? add : dst[end_lane + 64 * x] + add;
+            }
         });
 }
 
@@ -421,6 +479,40 @@ __global__ __launch_bounds__(NW * 64) void f32_window_bwd_kernel(BwdArgs b, int 
     const int id = blockIdx.x;
     if (id < dkv_blocks) f32_dkv_body<D, false>(b, id, smem, stat, mask);
     else f32_dq_body<D>(b, id - dkv_blocks, smem, mask);
+}
+// With far rows in pieces: the pieces first, their workgroups have the longest way to the gradients.
+template <int D>
+__global__ __launch_bounds__(NW * 64) void f32_far_bwd_kernel(BwdArgs b, int far_blocks, int dkv_blocks, FarSums far, WindowMask mask)
+{
+    __shared__ __attribute__((aligned(16))) char smem[BwdLds<D>::bytes];
+    __shared__ __attribute__((aligned(16))) float stat[NW][2 * RB];
+    const int id = blockIdx.x;
+    if (id < far_blocks) f32_dkv_body<D, false, WindowMask, kFarPieces>(b, id, smem, stat, mask, far);
+    else if (id < far_blocks + dkv_blocks) f32_dkv_body<D, false, WindowMask, kNearRows>(b, id - far_blocks, smem, stat, mask);
+    else f32_dq_body<D>(b, id - far_blocks - dkv_blocks, smem, mask);
+}
+// Adds the pieces' sums of a segment's key block (blockIdx.x: block, key/value head; y: segment) to its gradients, in their order.
+template <int D>
+__global__ __launch_bounds__(256) void f32_far_add_kernel(BwdArgs b, FarSums far, WindowMask mask)
+{
+    const BwdArgs::Fwd &p = b.f;
+    const int kh = blockIdx.x % p.n_kv_heads, block = blockIdx.x / p.n_kv_heads, seg = blockIdx.y, k0 = block * RB;
+    const int q0 = p.cu_seqlens_q[seg], lq = p.cu_seqlens_q[seg + 1] - q0, key0 = p.cu_seqlens_k[seg], lk = p.cu_seqlens_k[seg + 1] - key0;
+    const int rows = min(RB, lk - k0);
+    if (rows <= 0) return;
+    const int first = near_blocks(mask, k0, rows, lk - lq, lq).end / (kFarRows / RB), end = (lq + kFarRows - 1) / kFarRows;
+    // (of the first piece every block may be a near one: it has left nothing)
+    const int from = near_blocks(mask, k0, rows, lk - lq, lq).end >= min((lq + RB - 1) / RB, (first + 1) * (kFarRows / RB)) ? first + 1 : first;
+    if (from >= end) return;
+    const int64_t stride = (int64_t)p.n_kv_heads * far.blocks * 2 * RB * D, place = q0 / kFarRows + seg;
+    for (int t = threadIdx.x; t < 2 * rows * (D / 4); t += 256) {
+        const int which = t / (rows * (D / 4)), r = t / (D / 4) % rows, c = t % (D / 4);
+        const float *sums = far.sums + (place + from) * stride + (((int64_t)kh * far.blocks + block) * 2 + which) * RB * D + r * D + c * 4;
+        f32x4 a = {0.f, 0.f, 0.f, 0.f};
+        for (int x = from; x < end; ++x, sums += stride) a += *(const f32x4 *)sums;
+        f32x4 *to = (f32x4 *)((which ? b.d_k : b.d_v) + (int64_t)(key0 + k0 + r) * b.dkv_stride_tok + (int64_t)kh * b.dkv_stride_head + c * 4);
+        *to += a;
+    }
 }
 // Slices of one sequence add to the same dK/dV rows.  One workgroup adds to 16 of them for all slices of the launch, slice by
 // slice as the calls would, so that a split sequence does not take a launch per slice, each ending with one
@@ -525,8 +617,32 @@ hipError_t launch_window_f32_fwd(const cf_attn_fwd_params &p, const WindowMask &
     else f32_window_fwd_kernel<128><<<grid, NW * 64, 0, s>>>(p, mask);
     return hipGetLastError();
 }
-hipError_t launch_window_f32_bwd(const cf_attn_bwd_params &b, const WindowMask &mask, hipStream_t s)
+// Far rows in pieces?  Where an average segment has far rows enough that its first key blocks would be twice the work of others, and the
+// pieces' sums are not many.
+int64_t far_places(const cf_attn_fwd_params &p) { return (int64_t)p.n_tokens / kFarRows + p.n_segments; }
+int64_t far_blocks(const cf_attn_fwd_params &p, const WindowMask &mask) { return far_places(p) * p.n_kv_heads * ((mask.sinks + RB - 1) / RB); }
+int64_t window_f32_scratch(const cf_attn_fwd_params &p, const WindowMask &mask)
 {
+    if (mask.sinks == 0 || p.n_tokens <= p.n_segments * ((int64_t)mask.window + kFarRows)) return 0;
+    const int64_t bytes = far_blocks(p, mask) * 2 * RB * p.head_dim * 4;
+    return bytes <= (256 << 20) && launch_blocks(p, true) + far_blocks(p, mask) <= 0x3fffff ? bytes : 0;
+}
+
+template <int D>
+static hipError_t run_far_bwd(const cf_attn_bwd_params &b, float *sums, const WindowMask &mask, hipStream_t s)
+{
+    const FarSums far = {sums, (mask.sinks + RB - 1) / RB};
+    const int pieces = (int)far_blocks(b.f, mask), dkv = (int)key_blocks(b.f);
+    f32_far_bwd_kernel<D><<<dim3((unsigned)(pieces + launch_blocks(b.f, true))), NW * 64, 0, s>>>(b, pieces, dkv, far, mask);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    f32_far_add_kernel<D><<<dim3((unsigned)(far.blocks * b.f.n_kv_heads), (unsigned)b.f.n_segments), 256, 0, s>>>(b, far, mask);
+    return hipGetLastError();
+}
+
+hipError_t launch_window_f32_bwd(const cf_attn_bwd_params &b, float *far_sums, const WindowMask &mask, hipStream_t s)
+{
+    if (window_f32_scratch(b.f, mask) > 0) return b.f.head_dim == 64 ? run_far_bwd<64>(b, far_sums, mask, s) : run_far_bwd<128>(b, far_sums, mask, s);
     if (launch_blocks(b.f, true) > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const int dkv = (int)key_blocks(b.f);
     const dim3 grid((unsigned)launch_blocks(b.f, true));

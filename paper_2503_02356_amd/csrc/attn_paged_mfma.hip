@@ -24,6 +24,10 @@ namespace {
 
 constexpr int BM = 128, BN = 64;             // rows of a tile, keys of a key tile
 constexpr int FEW = 32;                      // rows that the wavefronts share, keys of their blocks
+// Tiles of FEW rows of a windowed chunk that goes this way: one round of workgroups.  Forward, 28/4 heads, window 256, us, its rows to the
+// wavefronts / its keys: 1 row behind 500 keys 11.5 / 7.0, 33 behind 500 13.5 / 11.3, 250 behind 5000 14.3 / 11.7, 500 behind 8000 14.4 / 13.7;
+// 32/8 heads, window 4000: 100 behind 2000 41.5 / 27.0, 250 behind 5000 81.4 / 46.9, 500 behind 8000 81.7 / 64.3.
+constexpr int64_t kWindowFewTiles = 512;
 using F = Mfma<16>;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLazy = 8.f;                 // log2 units a row maximum may exceed the running reference (attn_mfma_fwd.hip)
@@ -87,7 +91,7 @@ __device__ __forceinline__ bf16x8 query(const PagedArgs &a, const TileRows &t, i
 __device__ __forceinline__ float score_factor(const PagedArgs &a) { return a.p.softmax_scale == 0.f ? 1.f : fabsf(a.p.softmax_scale) * kLog2e; }
 
 // One row over the key tiles [first, end), pair by pair, into the call's tensors or as a part (a row whose result is not finite).
-template <int D>
+template <int D, bool CHUNK = false>
 __device__ __forceinline__ void row_again(const PagedArgs &a, const TileRows &t, int x, const KeyTiles<BN, WindowMask> &tiles, int first, int end, int part)
 {
     const int lane = threadIdx.x & 63;
@@ -95,7 +99,8 @@ __device__ __forceinline__ void row_again(const PagedArgs &a, const TileRows &t,
     int h;
     t.find(x, row, h);
     const unsigned short *q = row_of<unsigned short>(a.p.q, (int)row, a.p.q_stride_tok, h, a.p.q_stride_head);
-    const RowSums<unsigned short, D> r = paged_row<unsigned short, D, 4, BN>(a, a.table(t.seq), t.position(x), t.kh, tiles, first, end, [&](int e) { return ld(q + e); });
+    const RowSums<unsigned short, D> r = paged_row<unsigned short, D, 4, BN>(
+        a, CHUNK ? PageTable{(const int32_t *)zeros, 1, 30, 1} : a.table(t.seq), t.position(x), t.kh, tiles, first, end, [&](int e) { return ld(q + e); }, t.key0);
     const bool none = r.m == -INFINITY && r.z == 0.f;
     if (a.parts > 1) {
         const int64_t flat = t.flat(a, x);
@@ -110,7 +115,9 @@ __device__ __forceinline__ void row_again(const PagedArgs &a, const TileRows &t,
 }
 
 // One block of KB x 16 keys, for QB x 16 rows: scores of a K tile, masks, the running softmax, P.
-template <int D, int KB, int QB>
+// RESIDUAL: P enters the second product with the bf16 rounding of what its own rounding leaves (16 bits and more), as a chunk's kernels have
+// it at head_dim 64 and for a sequence's first rows; the wavefronts of few rows have time for it.
+template <int D, int KB, int QB, bool RESIDUAL = false>
 struct Rows {
     static constexpr int KS = D / F::K, DB = D / 16, NS = KB * F::R;
     bf16x8 q[QB][KS];
@@ -219,13 +226,18 @@ struct Rows {
     {
 #pragma unroll
         for (int t = 0; t < KB * 16 / F::K; ++t) {
-            bf16x8 pb[QB];
+            bf16x8 pb[QB], rest[QB];
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
                 float f[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] = s[(8 * t + e) / F::R][qb][(8 * t + e) % F::R];
                 pb[qb] = pack8(f);
+                if (RESIDUAL) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e] -= (float)pb[qb][e];
+                    rest[qb] = pack8(f);
+                }
             }
             const char *va = v_tile + t * (F::K * 2 * D);
 #pragma unroll
@@ -235,6 +247,7 @@ struct Rows {
                 for (int y = 0; y < QB; ++y) {
                     const int qb = db & 1 ? QB - 1 - y : y;
                     o[db][qb] = F::mul(x, pb[qb], o[db][qb]);
+                    if (RESIDUAL) o[db][qb] = F::mul(x, rest[qb], o[db][qb]);
                 }
             }
         }
@@ -370,14 +383,14 @@ __device__ __forceinline__ void many_rows(const PagedArgs &a, const TileRows &t,
 }
 
 // Few rows: all of them in every wavefront, which has blocks of 32 keys of its own.
-template <int D, int QB, bool WHOLE>
+template <int D, int QB, bool WHOLE, bool CHUNK>
 __device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, const KeyTiles<BN, WindowMask> &tiles, int first, int end, int keys,
                                          int part, char *k_stage, char *v_stage)
 {
     constexpr int TILE = FEW * 2 * D, COPIES = TILE / 1024;       // copy instructions of a block's keys
     const int wave = wave_id(), col = F::column(), group = F::group();
     char *k_tile = k_stage + wave * TILE, *v_tile = v_stage + wave * TILE;
-    const KeySource<2> src(a, t, keys);
+    const KeySource<2, CHUNK> src(a, t, keys);
     GroupDma<D, 32, 1> dma;
     dma.init(src.row_bytes, 0);
     GroupDma<D, 16, 1> half_dma;
@@ -421,7 +434,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, 
         issue(src.k, start_of(u), pages, k_tile);
         issue(src.v, start_of(u), pages, v_tile);
     }
-    Rows<D, FEW / 16, QB> r;
+    Rows<D, FEW / 16, QB, CHUNK> r;
     r.clear();
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
@@ -517,13 +530,13 @@ __device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, 
             const int at = (__ffsll((long long)left) - 1) / PIECES;
             left &= ~(((PIECES == 64 ? 0ull : 1ull << PIECES) - 1) << (at * PIECES));
             const int row = x0 + wave * (64 / PIECES) + at;
-            row_again<D>(e, t, row, tiles, first, end, part);
+            row_again<D, CHUNK>(e, t, row, tiles, first, end, part);
         }
     }
 }
 
-// MODE: FEW rows to a tile, all by few_rows; BM rows, all by many_rows; BOTH: BM rows, by what a tile holds.
-enum Mode { kFew, kMany, kBoth };
+// MODE: FEW rows to a tile, all by few_rows; BM rows, all by many_rows; BOTH: BM rows, by what a tile holds; CHUNK: as FEW, keys in one piece.
+enum Mode { kFew, kMany, kBoth, kChunk };
 template <int D, Mode MODE, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void mfma_paged_kernel(PagedArgs a)
 {
@@ -536,9 +549,9 @@ __global__ __launch_bounds__(256, 2) void mfma_paged_kernel(PagedArgs a)
     t.kh = id % a.p.n_kv_heads;                      // (fastest: an XCD keeps reading the same heads; attn_mfma_fwd.hip)
     id /= a.p.n_kv_heads;
     const int part = id % a.parts;
-    if (!find_tile<MODE == kFew ? FEW : BM>(a, id / a.parts, t)) return;
+    if (!find_tile<MODE == kFew || MODE == kChunk ? FEW : BM, MODE == kChunk>(a, id / a.parts, t)) return;
     const int lowest = t.position(0), highest = t.position(t.rows - 1);
-    const int keys = at_most(highest + 1, a.p.pages_per_seq << a.shift);
+    const int keys = MODE == kChunk ? highest + 1 : at_most(highest + 1, a.p.pages_per_seq << a.shift);
     const KeyTiles<BN, WindowMask> tiles(a.mask, lowest, keys);
     // (BOTH: tiles of many rows are cut a third as often, for a part of them leaves four times as much to be joined)
     const int thirds = MODE == kBoth && t.rows > FEW ? 3 : 1, per_part = a.tiles_per_part * thirds, last_part = (a.parts - 1) / thirds;
@@ -557,8 +570,8 @@ __global__ __launch_bounds__(256, 2) void mfma_paged_kernel(PagedArgs a)
     if (MODE == kMany || (MODE == kBoth && t.rows > FEW)) {
         many_rows<D, WHOLE>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
     } else if constexpr (MODE != kMany) {
-        if (t.rows > 16) few_rows<D, 2, WHOLE>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
-        else few_rows<D, 1, WHOLE>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
+        if (t.rows > 16) few_rows<D, 2, WHOLE, MODE == kChunk>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
+        else few_rows<D, 1, WHOLE, MODE == kChunk>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
     }
 }
 
@@ -609,6 +622,27 @@ static hipError_t launch(const PagedArgs &a, hipStream_t s)
     }
     return hipGetLastError();
 }
+// A windowed chunk of few rows: its wavefronts share the keys instead of the rows.
+bool window_few(const cf_attn_fwd_params &p)
+{
+    return ((int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads) / FEW + p.n_segments) * p.n_kv_heads <= kWindowFewTiles && (int64_t)p.n_tokens * p.n_q_heads < 0x7fffffffLL &&
+           p.n_kv_tokens < (1 << 30);
+}
+hipError_t launch_window_few(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s)
+{
+    PagedArgs a{};
+    a.p.dtype = p.dtype, a.p.n_q_heads = p.n_q_heads, a.p.n_kv_heads = p.n_kv_heads, a.p.head_dim = p.head_dim, a.p.softmax_scale = p.softmax_scale;
+    a.p.n_tokens = p.n_tokens, a.p.n_seqs = p.n_segments, a.p.cu_seqlens_q = p.cu_seqlens_q, a.p.kv_lens = p.cu_seqlens_k;
+    a.p.q = p.q, a.p.q_stride_tok = p.q_stride_tok, a.p.q_stride_head = p.q_stride_head;
+    a.p.k_pages = p.k, a.p.v_pages = p.v, a.p.kv_stride_tok = p.kv_stride_tok, a.p.kv_stride_head = p.kv_stride_head;
+    a.p.o = p.o, a.p.o_stride_tok = p.o_stride_tok, a.p.o_stride_head = p.o_stride_head, a.p.lse = p.lse;
+    a.mask = mask, a.parts = 1, a.tiles_per_part = 0x7fffffff, a.shift = 30;
+    const dim3 grid((unsigned)(((int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads) / FEW + p.n_segments) * p.n_kv_heads));
+    if (p.head_dim == 64) mfma_paged_kernel<64, kChunk, true><<<grid, 256, 0, s>>>(a);
+    else mfma_paged_kernel<128, kChunk, true><<<grid, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
 hipError_t launch_paged_mfma(const PagedArgs &a, hipStream_t s)
 {
     const bool whole = a.p.page_size >= BN;

@@ -195,12 +195,16 @@ hipError_t launch_delta(const cf_attn_bwd_params &p, const BwdWorkspace &ws, hip
 // The same with a window and sinks (attn_window.hip).
 hipError_t launch_window_simple_fwd(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s);
 hipError_t launch_window_simple_bwd(const cf_attn_bwd_params &b, const BwdWorkspace &ws, const WindowMask &mask, hipStream_t s);
+// A chunk of so few rows that they leave most of the chip idle (attn_paged_mfma.hip).
+bool window_few(const cf_attn_fwd_params &p);
+hipError_t launch_window_few(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s);
 hipError_t launch_window_mfma_fwd(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s);
 hipError_t launch_window_mfma_bwd(const cf_attn_bwd_params &b, const BwdWorkspace &ws, const WindowMask &mask, hipStream_t s);
 int64_t window_launch_size(const cf_attn_fwd_params &p, const WindowMask &mask);      // work-items of the backward's larger launch
 int64_t window_worklist_capacity(const cf_attn_fwd_params &p, const WindowMask &mask);
 hipError_t launch_window_f32_fwd(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s);
-hipError_t launch_window_f32_bwd(const cf_attn_bwd_params &b, const WindowMask &mask, hipStream_t s);
+hipError_t launch_window_f32_bwd(const cf_attn_bwd_params &b, float *far_sums, const WindowMask &mask, hipStream_t s);
+int64_t window_f32_scratch(const cf_attn_fwd_params &p, const WindowMask &mask);      // bytes of far_sums (0: not needed)
 
 // head_dim 128, forward and dQ: 32x32x16 MFMAs instead of 16x16x32 (mfma_common.h)?  A launch that fills the chip is limited by power and
 // gains 2-7 % from the smaller ones.  On a chip that is mostly empty a wavefront is alone on its SIMD, and the time to issue twice as many

@@ -31,9 +31,10 @@ template <typename T, int D>
 struct RowSums {
     float m = -INFINITY, z = 0.f, acc[D / 64] = {};
 };
+// key0: row of the pages that the table counts from (0 but for keys in one piece).
 template <typename T, int D, int UNROLL, int TILE, typename Q>
 __device__ inline RowSums<T, D> paged_row(const PagedArgs &a, const PageTable &table, int position, int kh, const KeyTiles<TILE, WindowMask> &tiles,
-                                          int first, int end, Q q)
+                                          int first, int end, Q q, int key0 = 0)
 {
     const cf_attn_paged_params &p = a.p;
     const int lane = threadIdx.x & 63;
@@ -42,7 +43,7 @@ __device__ inline RowSums<T, D> paged_row(const PagedArgs &a, const PageTable &t
         const int j = tiles.start(t) + lane;
         const bool seen = lane < TILE && j <= position && (j > position - a.mask.window || j < a.mask.sinks);
         const int page = seen ? table.page_of(j) : -1;
-        const int64_t at = (int64_t)max(page, 0) * p.page_stride + (int64_t)table.row_in_page(j) * p.kv_stride_tok + (int64_t)kh * p.kv_stride_head;
+        const int64_t at = (int64_t)max(page, 0) * p.page_stride + (int64_t)(key0 + table.row_in_page(j)) * p.kv_stride_tok + (int64_t)kh * p.kv_stride_head;
         float s = -INFINITY;
         if (page >= 0) {
             const T *k = (const T *)p.k_pages + at;
@@ -69,7 +70,7 @@ __device__ inline RowSums<T, D> paged_row(const PagedArgs &a, const PageTable &t
 }
 
 constexpr int kMostParts = 64;       // (a lane of the joining wavefront to a part)
-// bf16 matrix kernel (attn_paged_mfma.hip).
+// bf16 matrix kernel (attn_paged_mfma.hip).  A windowed chunk of few rows goes by it too, as a cache of one page (launch_window_few).
 hipError_t launch_paged_mfma(const PagedArgs &a, hipStream_t s);
 int64_t paged_mfma_launch_size(const PagedArgs &a);      // work-items
 // Cuts a call's keys into parts: sets parts and tiles_per_part.

@@ -21,6 +21,7 @@ struct TileRows {
     int row0, rows;              // first row of the tile among the sequence's token-head rows, and how many it has
     int first_position;
     int G, kh;                   // query heads of a key/value head, key/value head
+    int key0;                    // keys in one piece: the sequence's first row of them
 
     __device__ __forceinline__ int token(int x) const { return (row0 + x) / G; }
     __device__ __forceinline__ int position(int x) const { return at_least(-1, first_position + token(x)); }
@@ -54,7 +55,8 @@ struct TileRows {
 };
 
 // Tile `rank`, counted from the last one of the last sequence: sequence g has the ranks from cu[g] * G / BM + g on.
-template <int BM>
+// CHUNK: kv_lens holds the bounds of the sequences' keys, which stand in one piece.
+template <int BM, bool CHUNK = false>
 __device__ __forceinline__ bool find_tile(const PagedArgs &a, int rank, TileRows &t)
 {
     const cf_attn_paged_params &p = a.p;
@@ -69,20 +71,21 @@ __device__ __forceinline__ bool find_tile(const PagedArgs &a, int rank, TileRows
         hi = min(hi, lo + step);
     }
     const int g = min(lo + lane, hi - 1);
-    const int begin = cu[g], end = cu[g + 1], keys = p.kv_lens[g];
+    const int begin = cu[g], end = cu[g + 1], key0 = p.kv_lens[g], keys = CHUNK ? p.kv_lens[g + 1] - key0 : key0;
     const int last = 63 - __clzll((long long)__ballot(lo + lane < hi && begin * G / BM + g <= place));
     t.seq = uniform(lo + last);
     const int q0 = __builtin_amdgcn_readlane(begin, last), q1 = __builtin_amdgcn_readlane(end, last);
     const NewRows rows(q0, q1, __builtin_amdgcn_readlane(keys, last));
     t.q0 = q0;
+    t.key0 = CHUNK ? __builtin_amdgcn_readlane(key0, last) : 0;
     t.row0 = (place - q0 * G / BM - t.seq) * BM;
     t.rows = at_most(BM, rows.lq * G - t.row0);
     t.first_position = rows.first_position;
     return t.rows > 0;
 }
 
-// Where a workgroup's keys stand.  SIZE: bytes of an element.
-template <int SIZE>
+// Where a workgroup's keys stand.  SIZE: bytes of an element.  CHUNK: in one piece, one page without end.
+template <int SIZE, bool CHUNK = false>
 struct KeySource {
     const CF_CONSTANT int32_t *table;        // the sequence's row (nothing writes it meanwhile: scalar loads, which no copy in flight holds up)
     int shift, n_pages, last;    // last: the last key that may be read
@@ -92,13 +95,14 @@ struct KeySource {
     __device__ __forceinline__ KeySource(const PagedArgs &a, const TileRows &t, int keys)
         : table((const CF_CONSTANT int32_t *)a.p.block_table + (int64_t)t.seq * a.p.table_stride), shift(a.shift), n_pages(a.p.n_pages), last(keys - 1),
           row_bytes((unsigned)(a.p.kv_stride_tok * SIZE)), page_bytes(a.p.page_stride * SIZE),
-          k((const char *)a.p.k_pages + (int64_t)t.kh * a.p.kv_stride_head * SIZE), v((const char *)a.p.v_pages + (int64_t)t.kh * a.p.kv_stride_head * SIZE)
+          k((const char *)a.p.k_pages + ((int64_t)t.key0 * a.p.kv_stride_tok + (int64_t)t.kh * a.p.kv_stride_head) * SIZE),
+          v((const char *)a.p.v_pages + ((int64_t)t.key0 * a.p.kv_stride_tok + (int64_t)t.kh * a.p.kv_stride_head) * SIZE)
     {
     }
     // The table's entry for keys key .. (a group that lies in one page).  Looked at (is_page) only where the page is used, a tile later: the
     // load has come by then.
-    __device__ __forceinline__ int entry(int key) const { return table[min(key, last) >> shift]; }
-    __device__ __forceinline__ bool is_page(int entry) const { return (unsigned)entry < (unsigned)n_pages; }
+    __device__ __forceinline__ int entry(int key) const { return CHUNK ? 0 : table[min(key, last) >> shift]; }
+    __device__ __forceinline__ bool is_page(int entry) const { return CHUNK || (unsigned)entry < (unsigned)n_pages; }
     __device__ __forceinline__ int page_of(int key) const
     {
         const int page = entry(key);
@@ -106,6 +110,7 @@ struct KeySource {
     }
     __device__ __forceinline__ int64_t offset(int page, int key) const
     {
+        if (CHUNK) return (int64_t)key * row_bytes;
         return page * page_bytes + (int64_t)(key & ((1 << shift) - 1)) * row_bytes;
     }
 };
