@@ -99,7 +99,7 @@ inline int64_t key_tiles_most(const cf_attn_fwd_params &p, const WindowMask &m)
 template <typename Mask = CausalMask>
 __host__ __device__ inline int64_t dkv_items_most(const cf_attn_fwd_params &p, const Mask &mask = Mask())
 {
-    const int64_t tiles = key_tiles_most(p, mask), G = p.n_q_heads / p.n_kv_heads, cuts = kSlots * 10 / 16 / p.n_kv_heads + 1;
+    const int64_t tiles = key_tiles_most(p, mask), G = p.n_q_heads / p.n_kv_heads, cuts = (Mask::windowed ? kSlots * 10 / 13 : kSlots * 10 / 16) / p.n_kv_heads + 1;
     return tiles * G > tiles + cuts ? tiles * G : tiles + cuts;
 }
 
@@ -108,12 +108,15 @@ struct ListCuts {
     float average;                                   // pairs per slot
     int fair, target;
     bool large, small, even_heads;
-    __host__ __device__ ListCuts(int total, int n_tiles, int n_q_heads, int slots)
+    // averages: of a fine item.  Windowed calls: 1.3, their key tiles having about the same pairs each (28/4 heads, forward and backward, us,
+    // 1.6 / 1.3 / 1.0: 16384 rows, window 1024 1290 / 1221 / 1215, 8192 packed around 600, window 512 344 / 330 / 383, 2048 behind 8000, window 1024
+    // 237 / 233 / 237; 32/8, 4096 packed around 300, window 128 171 / 175 / 195).
+    __host__ __device__ ListCuts(int total, int n_tiles, int n_q_heads, int slots, float averages = 1.6f)
     {
         const int64_t all_pairs = (int64_t)total * n_q_heads;
         // (in floating point: a rounding moves a cut, and no more; 64-bit divisions would take longer than the rest of the list)
         average = (float)all_pairs / (float)slots;
-        const int fine = share(average, 1.6f);
+        const int fine = share(average, averages);
         large = fine > kFineMost, small = slots == kSlots && average <= kSmallMost;
         fair = small ? max(3, share(average, 2.2f)) : fine;
         const int64_t head_items = (int64_t)n_tiles * n_q_heads;
@@ -170,7 +173,7 @@ __device__ __forceinline__ void build_dkv_worklist(const BwdArgs::Fwd &p, int *w
     atomicAdd(&total, mine);
     atomicAdd(&n_tiles, my_tiles);
     __syncthreads();
-    const ListCuts cuts(total, n_tiles, p.n_q_heads, slots);
+    const ListCuts cuts(total, n_tiles, p.n_q_heads, slots, Mask::windowed ? 1.3f : 1.6f);
     bool cut_heads = true;
     auto for_each_item = [&](auto &&visit) {
         for_each_tile([&](int seg, int kt0, int n_qt) {
