@@ -546,10 +546,10 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
                     float f[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f[e] = value(x, (8 * (g % 2) + e) % NS, 0);
-                    split_exact(f, ws);
+                    split<LIST ? 2 : 3>(f, ws);
                 }
 #pragma unroll
-                for (int t = 0; t < 3; ++t) accumulate_in_place<D>(x ? dk[j] : dv[j], ring[n % RING], ws[t]);
+                for (int t = 0; t < (LIST ? 2 : 3); ++t) accumulate_in_place<D>(x ? dk[j] : dv[j], ring[n % RING], ws[t]);
             } else {
                 accumulate_in_place<D>(x ? dk[j] : dv[j], ring[n % RING], w);
             }
@@ -985,11 +985,11 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
                         for (int qb = 0; qb < N; ++qb) {
 #pragma unroll
                             for (int e = 0; e < 8; ++e) f[qb][e] = dp[(8 * tq + e) / F::R][qb][(8 * tq + e) % F::R];
-                            if (D == 64) split_exact(f[qb], dsb[qb]);
+                            if (D == 64) split<Mask::windowed ? 2 : 3>(f[qb], dsb[qb]);
                             else dsb[qb][0] = pack8(f[qb]);
                         }
 #pragma unroll
-                        for (int x = 0; x < (D == 64 ? 3 : 1); ++x)
+                        for (int x = 0; x < (D != 64 ? 1 : Mask::windowed ? 2 : 3); ++x)
 #pragma unroll
                             for (int j = 0; j < DB; ++j)
 #pragma unroll

@@ -29,6 +29,10 @@ constexpr int BN = 64;         // key rows per tile
 template <int D>
 constexpr float kLazy = D == 64 ? 0.f : 8.f;
 
+// Operands that P enters the second product as.
+template <int D, typename Mask>
+constexpr int kWords = D != 64 ? 1 : Mask::windowed ? 2 : 3;
+
 template <int D>
 struct Stage {
     static constexpr int tile_bytes = BN * 2 * D;    // one swizzled K or V tile (see mfma_common.h)
@@ -238,7 +242,7 @@ __device__ __forceinline__ void fwd_body(const cf_attn_fwd_params &p, int id, ch
                     float f[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f[e] = s[(8 * t + e) / F::R][qb][(8 * t + e) % F::R];
-                    if (D == 64) split_exact(f, pb[qb]);
+                    if (D == 64) split<kWords<D, Mask>>(f, pb[qb]);
                     else pb[qb][0] = pack8(f);
                 }
                 const char *va = vst + t * (TILE_BYTES / (BN / F::K));
@@ -249,7 +253,7 @@ __device__ __forceinline__ void fwd_body(const cf_attn_fwd_params &p, int id, ch
                     for (int x = 0; x < QB; ++x) {
                         const int qb = db & 1 ? QB - 1 - x : x;
 #pragma unroll
-                        for (int w = 0; w < (D == 64 ? 3 : 1); ++w) o_acc[db][qb] = F::mul(a, pb[qb][w], o_acc[db][qb]);
+                        for (int w = 0; w < kWords<D, Mask>; ++w) o_acc[db][qb] = F::mul(a, pb[qb][w], o_acc[db][qb]);
                     }
                 }
             }
