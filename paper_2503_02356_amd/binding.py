@@ -410,8 +410,25 @@ def cf_attn_bwd_static(params, stream=None):
     _check(lib().cf_attn_bwd_static(C.byref(params), stream if stream is not None else _stream()))
 
 
+def _stream_for(params, stream):
+    """The given stream, or the current one: of the device that the call's tensors are on, or the kernels would not reach them."""
+    if stream is not None:
+        return stream
+    import torch
+    t = params._keepalive[0] if hasattr(params, "_keepalive") else None
+    t = t._keepalive[0] if isinstance(t, AttnFwdParams) else t
+    if t is not None and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{t.device.index}, the current device is cuda:{torch.cuda.current_device()}")
+    return _stream()
+
+
+def _int32(x):
+    """ctypes drops what an int32 field does not hold: a window of 2**32 keys would be one of 0."""
+    return max(-1 << 31, min((1 << 31) - 1, int(x)))
+
+
 def _window(window, n_sinks):
-    return C.byref(AttnWindow(int(window), int(n_sinks)))
+    return C.byref(AttnWindow(_int32(window), _int32(n_sinks)))
 
 
 class Attention:
@@ -440,7 +457,7 @@ class Attention:
 
 def cf_attn_window_fwd(params, window, n_sinks=0, stream=None):
     """cf_attn_fwd's call with a sliding window: a query sees its last `window` keys and its sequence's first n_sinks."""
-    _check(lib().cf_attn_window_fwd(C.byref(params), _window(window, n_sinks), stream if stream is not None else _stream()))
+    _check(lib().cf_attn_window_fwd(C.byref(params), _window(window, n_sinks), _stream_for(params, stream)))
 
 
 def cf_attn_window_bwd_workspace_bytes(params, window, n_sinks=0):
@@ -448,15 +465,16 @@ def cf_attn_window_bwd_workspace_bytes(params, window, n_sinks=0):
 
 
 def cf_attn_window_bwd(params, window, n_sinks=0, stream=None):
-    _check(lib().cf_attn_window_bwd(C.byref(params), _window(window, n_sinks), stream if stream is not None else _stream()))
+    _check(lib().cf_attn_window_bwd(C.byref(params), _window(window, n_sinks), _stream_for(params, stream)))
 
 
-def _check_paged(cu_q, kv_lens, block_table, k_pages, v_pages):
+def _check_paged(cu_q, kv_lens, block_table, k_pages, v_pages, *others):
     for t in (cu_q, kv_lens, block_table):
         assert t.is_cuda and t.element_size() == 4 and not t.is_floating_point()
     assert cu_q.is_contiguous() and kv_lens.is_contiguous() and block_table.stride(1) == 1
     assert block_table.shape[0] == kv_lens.numel() == cu_q.numel() - 1
     assert k_pages.is_cuda and k_pages.stride(3) == 1 and k_pages.stride() == v_pages.stride() and k_pages.shape == v_pages.shape
+    assert all(t.device == k_pages.device for t in (cu_q, kv_lens, block_table, v_pages) + others)
 
 
 def make_paged_params(q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, scale, max_kv_len=0, window=0, n_sinks=0, flags=0,
@@ -466,7 +484,7 @@ def make_paged_params(q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, s
     kept with the parameters."""
     import torch
     T, Hq, D = q.shape
-    _check_paged(cu_q, kv_lens, block_table, k_pages, v_pages)
+    _check_paged(cu_q, kv_lens, block_table, k_pages, v_pages, q, o, *(t for t in (lse, workspace) if t is not None))
     assert q.is_cuda and q.stride(2) == 1 and o.stride(2) == 1 and q.dtype == k_pages.dtype == v_pages.dtype == o.dtype
     assert o.shape == q.shape and k_pages.shape[3] == D
     assert lse is None or (lse.is_contiguous() and tuple(lse.shape) == (Hq, T) and lse.dtype == torch.float32)
@@ -475,8 +493,8 @@ def make_paged_params(q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, s
     p.softmax_scale, p.n_tokens, p.n_seqs = float(scale), T, kv_lens.numel()
     p.cu_seqlens_q, p.kv_lens, p.block_table = cu_q.data_ptr(), kv_lens.data_ptr(), block_table.data_ptr()
     p.table_stride, p.pages_per_seq = block_table.stride(0) if block_table.shape[0] > 1 else block_table.shape[1], block_table.shape[1]
-    p.page_size, p.n_pages, p.max_kv_len = k_pages.shape[1], k_pages.shape[0], int(max_kv_len)
-    p.window, p.n_sinks = int(window), int(n_sinks)
+    p.page_size, p.n_pages, p.max_kv_len = k_pages.shape[1], k_pages.shape[0], _int32(max_kv_len)
+    p.window, p.n_sinks = _int32(window), _int32(n_sinks)
     p.q, p.q_stride_tok, p.q_stride_head = q.data_ptr(), q.stride(0), q.stride(1)
     p.k_pages, p.v_pages = k_pages.data_ptr(), v_pages.data_ptr()
     p.page_stride, p.kv_stride_tok, p.kv_stride_head = k_pages.stride(0), k_pages.stride(1), k_pages.stride(2)
@@ -486,6 +504,7 @@ def make_paged_params(q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, s
         need = cf_attn_paged_workspace_bytes(p)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     if workspace is not None:
+        assert workspace.is_contiguous()
         p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     p._keepalive = (q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, workspace)      # see make_fwd_params
     return p
@@ -496,12 +515,12 @@ def cf_attn_paged_workspace_bytes(params):
 
 
 def cf_attn_paged_fwd(params, stream=None):
-    _check(lib().cf_attn_paged_fwd(C.byref(params), stream if stream is not None else _stream()))
+    _check(lib().cf_attn_paged_fwd(C.byref(params), _stream_for(params, stream)))
 
 
 def make_kv_append_params(k, v, k_pages, v_pages, cu_q, kv_lens, block_table):
     """k, v [T,Hkv,D] (views with the same strides); the rest as in make_paged_params."""
-    _check_paged(cu_q, kv_lens, block_table, k_pages, v_pages)
+    _check_paged(cu_q, kv_lens, block_table, k_pages, v_pages, k, v)
     assert k.is_cuda and k.stride(2) == 1 and k.stride() == v.stride() and k.shape == v.shape
     assert k.dtype == v.dtype == k_pages.dtype == v_pages.dtype and tuple(k.shape[1:]) == tuple(k_pages.shape[2:])
     p = KvAppendParams()
@@ -517,4 +536,4 @@ def make_kv_append_params(k, v, k_pages, v_pages, cu_q, kv_lens, block_table):
 
 
 def cf_kv_append(params, stream=None):
-    _check(lib().cf_kv_append(C.byref(params), stream if stream is not None else _stream()))
+    _check(lib().cf_kv_append(C.byref(params), _stream_for(params, stream)))

@@ -5,6 +5,7 @@ import itertools
 import os
 import re
 import subprocess
+import types
 
 import numpy as np
 import pytest
@@ -81,6 +82,31 @@ def test_what_the_calls_without_a_window_refuse_is_refused():
 def test_workspace_does_not_grow_with_a_prefix_that_nobody_sees():
     near, far = (B.cf_attn_window_bwd_workspace_bytes(params(Tk=n), 64, 4) for n in (5000, 1 << 30))
     assert near == far
+
+
+def test_workspace_of_the_largest_calls():
+    """Sizes whose products leave 63 bits: the far rows' sums are not asked for (delta is: 2^30 rows of 2^15 heads)."""
+    p = params(dtype=B.CF_FP32, Hq=1 << 15, Hkv=1 << 15, D=64, T=1 << 30, Tk=1 << 30)
+    p.n_segments = 512
+    assert B.cf_attn_window_bwd_workspace_bytes(p, 1, 1 << 30) == 1 << 47
+
+
+def test_windows_longer_than_the_field():
+    """2^32 + 3 keys are all of them, not 3."""
+    assert B.cf_count_window_pairs([0, 100], [0, 100], (1 << 32) + 3) == B.cf_count_pairs([0, 100], [0, 100]) == 5050
+    assert B.cf_count_window_pairs([0, 100], [0, 100], 1, 1 << 40) == 5050
+    refused(B.CF_EINVAL, "window >= 1", lambda: B.cf_count_window_pairs([0, 1], [0, 1], -(1 << 32) + 5))
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    there = types.SimpleNamespace(device=types.SimpleNamespace(index=1))
+    p, paged, append = params(), B.AttnPagedParams(), B.KvAppendParams()
+    b = bwd(p)
+    b._keepalive, p._keepalive, paged._keepalive, append._keepalive = (p,), (there,), (there,), (there,)
+    for call in (lambda: B.cf_attn_window_fwd(p, 8), lambda: B.cf_attn_window_bwd(b, 8), lambda: B.cf_attn_paged_fwd(paged), lambda: B.cf_kv_append(append)):
+        with pytest.raises(ValueError, match="cuda:1, the current device is cuda:0"):
+            call()
 
 
 def test_pairs_are_counted():
