@@ -64,11 +64,30 @@ class PagedCache:
         """counts[i] new tokens of sequence names[i] (new names begin a sequence), their rows one behind the other in q [T,Hq,D] and k, v
         [T,Hkv,D]: their keys and values are written into pages, then they attend to all that their sequences hold.  -> o [T,Hq,D] (rows
         behind the last sequence's, of a padded batch, 0), in the order of the current stream; lse: [Hq,T] fp32 tensor to be written, or
-        None.  Raises MemoryError, with nothing changed, where pages are missing."""
-        counts = [int(n) for n in counts]
+        None.  Raises MemoryError where pages are missing; whatever it raises, the sequences are what they were."""
+        names, counts = list(names), [int(n) for n in counts]
+        if not names or len(names) != len(counts):
+            raise ValueError(f"{len(names)} sequences and {len(counts)} numbers of new tokens")
         if sum(counts) > q.shape[0] or q.shape[0] != k.shape[0]:
             raise ValueError(f"{sum(counts)} new tokens in {q.shape[0]} rows of q and {k.shape[0]} of k")
+        before = {name: (self.seqs[name][0], len(self.seqs[name][1])) for name in names if name in self.seqs}
         self._grow(names, counts)
+        try:
+            o = self._append_and_attend(names, counts, q, k, v, scale, lse)
+        except Exception:
+            for name in reversed(names):             # (arguments that the calls refuse)
+                length, n = before.get(name, (0, 0))
+                pages = self.seqs[name][1]
+                self.free += reversed(pages[n:])
+                self.seqs[name] = [length, pages[:n]]
+                if name not in before:
+                    del self.seqs[name]
+            raise
+        if self.window:
+            self._give_back(names)
+        return o
+
+    def _append_and_attend(self, names, counts, q, k, v, scale, lse):
         held = [self.seqs[name] for name in names]
         table = np.full((len(names), max(1, max(len(pages) for _, pages in held))), -1, dtype=np.int32)
         for i, (_, pages) in enumerate(held):
@@ -79,12 +98,12 @@ class PagedCache:
         n = len(names)
         cu, kv_lens, block_table = desc[:n + 1], desc[n + 1:2 * n + 1], desc[2 * n + 1:].view(table.shape)
         o = torch.empty_like(q) if sum(counts) == q.shape[0] else torch.zeros_like(q)
-        B.cf_kv_append(B.make_kv_append_params(k, v, self.k_pages, self.v_pages, cu, kv_lens, block_table))
-        B.cf_attn_paged_fwd(B.make_paged_params(q, self.k_pages, self.v_pages, o, lse, cu, kv_lens, block_table,
-                                                scale if scale is not None else q.shape[2] ** -0.5, max_kv_len=int(lens.max()), window=self.window,
-                                                n_sinks=self.n_sinks))
-        if self.window:
-            self._give_back(names)
+        append = B.make_kv_append_params(k, v, self.k_pages, self.v_pages, cu, kv_lens, block_table)
+        attention = B.make_paged_params(q, self.k_pages, self.v_pages, o, lse, cu, kv_lens, block_table,
+                                        scale if scale is not None else q.shape[2] ** -0.5, max_kv_len=int(lens.max()), window=self.window,
+                                        n_sinks=self.n_sinks)
+        B.cf_kv_append(append)
+        B.cf_attn_paged_fwd(attention)
         return o
 
 
