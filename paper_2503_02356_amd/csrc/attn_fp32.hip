@@ -624,6 +624,7 @@ int64_t far_blocks(const cf_attn_fwd_params &p, const WindowMask &mask) { return
 int64_t window_f32_scratch(const cf_attn_fwd_params &p, const WindowMask &mask)
 {
     if (mask.sinks == 0 || p.n_tokens <= p.n_segments * ((int64_t)mask.window + kFarRows)) return 0;
+    if (launch_blocks(p, true) > 0x3fffff) return 0;         // (what follows has 63 bits below that)
     const int64_t bytes = far_blocks(p, mask) * 2 * RB * p.head_dim * 4;
     return bytes <= (256 << 20) && launch_blocks(p, true) + far_blocks(p, mask) <= 0x3fffff ? bytes : 0;
 }

@@ -233,7 +233,7 @@ Path path_of(const PagedArgs &a)
 // Chooses the parts; bytes of workspace.
 int64_t cut(PagedArgs &a)
 {
-    a.parts = 1, a.tiles_per_part = 0x7fffffff, a.part_o = nullptr, a.part_ml = nullptr;
+    a.parts = 1, a.tiles_per_part = 1 << 28, a.part_o = nullptr, a.part_ml = nullptr;
     if (a.p.dtype == CF_BF16) cut_paged_mfma(a);
     else cut_paged_f32(a);
     if (path_of(a) == kRows) a.parts = 1;

@@ -636,7 +636,7 @@ hipError_t launch_window_few(const cf_attn_fwd_params &p, const WindowMask &mask
     a.p.q = p.q, a.p.q_stride_tok = p.q_stride_tok, a.p.q_stride_head = p.q_stride_head;
     a.p.k_pages = p.k, a.p.v_pages = p.v, a.p.kv_stride_tok = p.kv_stride_tok, a.p.kv_stride_head = p.kv_stride_head;
     a.p.o = p.o, a.p.o_stride_tok = p.o_stride_tok, a.p.o_stride_head = p.o_stride_head, a.p.lse = p.lse;
-    a.mask = mask, a.parts = 1, a.tiles_per_part = 0x7fffffff, a.shift = 30;
+    a.mask = mask, a.parts = 1, a.tiles_per_part = 1 << 28, a.shift = 30;
     const dim3 grid((unsigned)(((int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads) / FEW + p.n_segments) * p.n_kv_heads));
     if (p.head_dim == 64) mfma_paged_kernel<64, kChunk, true><<<grid, 256, 0, s>>>(a);
     else mfma_paged_kernel<128, kChunk, true><<<grid, 256, 0, s>>>(a);
