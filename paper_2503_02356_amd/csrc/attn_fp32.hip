@@ -43,13 +43,13 @@ namespace {
 __device__ __forceinline__ bool out_of_window(const CausalMask &, int, int) { return false; }
 __device__ __forceinline__ bool out_of_window(const WindowMask &m, int position, int key) { return key <= position - m.window && key >= m.sinks; }
 
-template <int D, typename Mask>
+template <int D, typename Mask, int W = NW>
 __device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id, const Mask &mask)
 {
     using S = Shape<D>;
     __shared__ f32x4 qs[S::J * 64];
-    __shared__ __attribute__((aligned(16))) float parts[NW * S::PART];
-    __shared__ float m_s[NW][RB], l_s[NW][RB];
+    __shared__ __attribute__((aligned(16))) float parts[W * S::PART];
+    __shared__ float m_s[W][RB], l_s[W][RB];
     const int lane = threadIdx.x & 63, wave = wave_id(), quarter = lane >> 4, col = lane & 15;
     const int G = p.n_q_heads / p.n_kv_heads, kh = id % p.n_kv_heads, h = kh * G + id / p.n_kv_heads % G;
     TileLocation loc;
@@ -74,7 +74,7 @@ __device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    for (int kb = wave; kb < n_kb; kb += NW) {
+    for (int kb = wave; kb < n_kb; kb += W) {
         const int k0 = key_blocks.start(kb);
         f32x4 x[4][S::NC];
         auto load_v = [&] { load_columns<D>(v + (int64_t)k0 * p.kv_stride_tok, kv_row_bytes, lk - 1 - k0, lane, x); };
@@ -84,7 +84,7 @@ __device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id
             __builtin_amdgcn_sched_barrier(0);       // V takes the registers of K: with both held D = 128 spills
             load_v();
         }
-        if (kb + NW < n_kb) load_row<D>(k + (int64_t)min(key_blocks.start(kb + NW) + col, lk - 1) * p.kv_stride_tok, quarter, kf);
+        if (kb + W < n_kb) load_row<D>(k + (int64_t)min(key_blocks.start(kb + W) + col, lk - 1) * p.kv_stride_tok, quarter, kf);
         const int lim = amax - k0 - 4 * quarter;         // key 4 * quarter + i of the block is masked iff i > lim
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[i] = i > lim || out_of_window(mask, amax, k0 + 4 * quarter + i) ? -INFINITY : s[i] * c2;
@@ -108,7 +108,7 @@ __device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id
     __syncthreads();
 
     // O = sum_w 2^(m_w - M) O_w / sum_w 2^(m_w - M) l_w over the wavefronts that had a block
-    const int n = min(NW, n_kb), r = threadIdx.x / (D / 4), c = threadIdx.x % (D / 4);
+    const int n = min(W, n_kb), r = threadIdx.x / (D / 4), c = threadIdx.x % (D / 4);
     bool bad = false;
     if (r < rows) {
         float M = m_s[0][r], L = 0.f;
@@ -134,8 +134,8 @@ __device__ __forceinline__ void f32_fwd_body(const cf_attn_fwd_params &p, int id
 
 template <int D>
 __global__ __launch_bounds__(NW * 64) void f32_fwd_kernel(cf_attn_fwd_params p) { f32_fwd_body<D>(p, blockIdx.x, CausalMask()); }
-template <int D>
-__global__ __launch_bounds__(NW * 64) void f32_window_fwd_kernel(cf_attn_fwd_params p, WindowMask mask) { f32_fwd_body<D>(p, blockIdx.x, mask); }
+template <int D, int W>
+__global__ __launch_bounds__(W * 64, 4) void f32_window_fwd_kernel(cf_attn_fwd_params p, WindowMask mask) { f32_fwd_body<D, WindowMask, W>(p, blockIdx.x, mask); }
 
 // Several chunks in one launch; of a chunk's workgroups the first dkv_blocks[c] belong to its key rows and those of the chunks chained behind
 // it.
@@ -281,7 +281,7 @@ __device__ __forceinline__ void f32_dq_body(const BwdArgs &b, int id, char *smem
 // be the work of one workgroup each.  FAR: they are cut into pieces of kFarRows rows, each with a workgroup of its own that leaves its
 // sums in the workspace (place of the piece: cu_q / kFarRows + segment + number in the segment); a small kernel behind adds these up in order,
 // so that the gradients stay reproducible.  NEAR: a key block without its far rows.  1000 rows behind 300 keys, 6/2 heads, D = 128, window 200,
-// 2 sinks, forward and backward: 171 us with ALL, 84 so (without sinks 69).
+// 2 sinks, forward and backward: 171 us with ALL, 76 so.
 enum RowsOf { kAllRows, kNearRows, kFarPieces };
 constexpr int kFarRows = 256;
 struct FarSums {
@@ -493,7 +493,7 @@ __global__ __launch_bounds__(NW * 64) void f32_far_bwd_kernel(BwdArgs b, int far
 }
 // Adds the pieces' sums of a segment's key block (blockIdx.x: block, key/value head; y: segment) to its gradients, in their order.
 template <int D>
-__global__ __launch_bounds__(256) void f32_far_add_kernel(BwdArgs b, FarSums far, WindowMask mask)
+__global__ __launch_bounds__(2 * RB * (D / 4)) void f32_far_add_kernel(BwdArgs b, FarSums far, WindowMask mask)
 {
     const BwdArgs::Fwd &p = b.f;
     const int kh = blockIdx.x % p.n_kv_heads, block = blockIdx.x / p.n_kv_heads, seg = blockIdx.y, k0 = block * RB;
@@ -505,13 +505,21 @@ __global__ __launch_bounds__(256) void f32_far_add_kernel(BwdArgs b, FarSums far
     const int from = near_blocks(mask, k0, rows, lk - lq, lq).end >= min((lq + RB - 1) / RB, (first + 1) * (kFarRows / RB)) ? first + 1 : first;
     if (from >= end) return;
     const int64_t stride = (int64_t)p.n_kv_heads * far.blocks * 2 * RB * D, place = q0 / kFarRows + seg;
-    for (int t = threadIdx.x; t < 2 * rows * (D / 4); t += 256) {
+    if (const int t = threadIdx.x; t < 2 * rows * (D / 4)) {
         const int which = t / (rows * (D / 4)), r = t / (D / 4) % rows, c = t % (D / 4);
         const float *sums = far.sums + (place + from) * stride + (((int64_t)kh * far.blocks + block) * 2 + which) * RB * D + r * D + c * 4;
-        f32x4 a = {0.f, 0.f, 0.f, 0.f};
-        for (int x = from; x < end; ++x, sums += stride) a += *(const f32x4 *)sums;
         f32x4 *to = (f32x4 *)((which ? b.d_k : b.d_v) + (int64_t)(key0 + k0 + r) * b.dkv_stride_tok + (int64_t)kh * b.dkv_stride_head + c * 4);
-        *to += a;
+        const f32x4 held = *to;
+        f32x4 a = {0.f, 0.f, 0.f, 0.f};
+        for (int x = from; x < end; x += 8, sums += 8 * stride) {        // (eight loads in flight)
+            f32x4 piece[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) piece[y] = *(const f32x4 *)(sums + min(y, end - 1 - x) * stride);
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+                if (x + y < end) a += piece[y];
+        }
+        *to = held + a;
     }
 }
 // Slices of one sequence add to the same dK/dV rows.  One workgroup adds to 16 of them for all slices of the launch, slice by
@@ -608,14 +616,22 @@ hipError_t launch_f32_bwd_batch(const cf_attn_bwd_params *const *chunks, int n, 
     return hipGetLastError();
 }
 
+// More workgroups than compute units: 8 wavefronts each, two workgroups to a compute unit (77 KB of LDS at D = 128), one of which multiplies
+// while the other loads or joins its results (forward, us, 16 / 8 wavefronts: 6/2 heads, D = 128, 700 rows behind 300, window 200 19.9 / 16.2, 3000
+// rows, window 1000 94.8 / 84.8; 4/2 heads, D = 64, 2000 rows, window 64 9.3 / 7.8; with fewer workgroups 10.9 either way).  The backward keeps
+// 16: its longest workgroups, those of key blocks, would be twice as long (1000 rows: 80 us, with 7 that fit twice 87).
+template <int D>
+static hipError_t run_window_fwd(const cf_attn_fwd_params &p, const WindowMask &mask, unsigned blocks, hipStream_t s)
+{
+    if (blocks > 256) f32_window_fwd_kernel<D, 8><<<dim3(blocks), 8 * 64, 0, s>>>(p, mask);
+    else f32_window_fwd_kernel<D, NW><<<dim3(blocks), NW * 64, 0, s>>>(p, mask);
+    return hipGetLastError();
+}
 hipError_t launch_window_f32_fwd(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s)
 {
     const int64_t blocks = launch_blocks(p, false);
     if (blocks > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-    const dim3 grid((unsigned)blocks);
-    if (p.head_dim == 64) f32_window_fwd_kernel<64><<<grid, NW * 64, 0, s>>>(p, mask);
-    else f32_window_fwd_kernel<128><<<grid, NW * 64, 0, s>>>(p, mask);
-    return hipGetLastError();
+    return p.head_dim == 64 ? run_window_fwd<64>(p, mask, (unsigned)blocks, s) : run_window_fwd<128>(p, mask, (unsigned)blocks, s);
 }
 // Far rows in pieces?  Where an average segment has far rows enough that its first key blocks would be twice the work of others, and the
 // pieces' sums are not many.
@@ -637,7 +653,7 @@ static hipError_t run_far_bwd(const cf_attn_bwd_params &b, float *sums, const Wi
     f32_far_bwd_kernel<D><<<dim3((unsigned)(pieces + launch_blocks(b.f, true))), NW * 64, 0, s>>>(b, pieces, dkv, far, mask);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    f32_far_add_kernel<D><<<dim3((unsigned)(far.blocks * b.f.n_kv_heads), (unsigned)b.f.n_segments), 256, 0, s>>>(b, far, mask);
+    f32_far_add_kernel<D><<<dim3((unsigned)(far.blocks * b.f.n_kv_heads), (unsigned)b.f.n_segments), 2 * RB * (D / 4), 0, s>>>(b, far, mask);
     return hipGetLastError();
 }
 

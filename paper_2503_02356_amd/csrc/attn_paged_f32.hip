@@ -1,6 +1,6 @@
 // fp32 attention of new tokens over a paged cache, head_dim 64 and 128, any scale: the fp32 forward kernel of a chunk (attn_fp32.hip) over
-// tiles of 16 token-head rows (row r of a sequence: token r / G, head r % G).  A workgroup of 16 wavefronts takes a tile and a part of its
-// keys, its wavefronts every 16th block of 16 keys, straight from the pages into registers (a block lies in one page); their results meet in
+// tiles of 16 token-head rows (row r of a sequence: token r / G, head r % G).  A workgroup of 8 wavefronts takes a tile and a part of its
+// keys, its wavefronts every 8th block of 16 keys, straight from the pages into registers (a block lies in one page); their results meet in
 // LDS in a fixed order, parts in a kernel behind this one.  A block of no page is passed over.
 // Bound by the fp32 matrix rate where there are many rows, by the chain of a wavefront's blocks and the loads' latency where there are few.
 #include <hip/hip_runtime.h>
@@ -13,13 +13,17 @@
 namespace cf {
 namespace {
 
+// Wavefronts of a workgroup.  8: two workgroups to a compute unit, one multiplies while the other loads (append and attention, 6/2 heads, D = 128,
+// us, 16 / 8 / 4 wavefronts: 3 tokens and 2 chunks of 100 behind up to 700 keys 27.9 / 18.7 / 21.0, 64 tokens behind 4000 134 / 103 / 118, a prompt of 2000
+// 83.6 / 76.3 / 103).
+constexpr int W = 8;
 template <int D>
-__global__ __launch_bounds__(NW * 64) void f32_paged_kernel(PagedArgs a)
+__global__ __launch_bounds__(W * 64, 4) void f32_paged_kernel(PagedArgs a)
 {
     using S = Shape<D>;
     __shared__ f32x4 qs[S::J * 64];
-    __shared__ __attribute__((aligned(16))) float parts[NW * S::PART];
-    __shared__ float m_s[NW][RB], l_s[NW][RB];
+    __shared__ __attribute__((aligned(16))) float parts[W * S::PART];
+    __shared__ float m_s[W][RB], l_s[W][RB];
     const int lane = threadIdx.x & 63, wave = wave_id(), quarter = lane >> 4, col = lane & 15;
     TileRows t;
     t.G = a.p.n_q_heads / a.p.n_kv_heads;
@@ -38,7 +42,7 @@ __global__ __launch_bounds__(NW * 64) void f32_paged_kernel(PagedArgs a)
         if (threadIdx.x < t.rows) a.part_ml[t.flat(a, threadIdx.x) * a.parts + part] = make_float2(-INFINITY, 0.f);
         return;
     }
-    for (int i = threadIdx.x; i < RB * D / 4; i += NW * 64) {
+    for (int i = threadIdx.x; i < RB * D / 4; i += W * 64) {
         const int r = i / (D / 4), c = i % (D / 4);
         int64_t row;
         int h;
@@ -54,7 +58,7 @@ __global__ __launch_bounds__(NW * 64) void f32_paged_kernel(PagedArgs a)
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    for (int b = first + wave; b < end; b += NW) {
+    for (int b = first + wave; b < end; b += W) {
         const int k0 = blocks.start(b), page = src.page_of(k0);
         if (page < 0) continue;
         const int64_t at = src.offset(page, k0);
@@ -90,7 +94,7 @@ __global__ __launch_bounds__(NW * 64) void f32_paged_kernel(PagedArgs a)
         m_s[wave][col] = m;
         l_s[wave][col] = l;
     }
-    const int used = at_most(NW, end - first);       // wavefronts that had a block
+    const int used = at_most(W, end - first);       // wavefronts that had a block
     if (wave < used) write_part<D>(o, parts + wave * S::PART, lane);
     __syncthreads();
 
@@ -140,16 +144,17 @@ int64_t groups_most(const cf_attn_paged_params &p) { return ((int64_t)p.n_tokens
 
 }  // namespace
 
-int64_t paged_f32_launch_size(const PagedArgs &a) { return groups_most(a.p) * a.parts * NW * 64; }
+int64_t paged_f32_launch_size(const PagedArgs &a) { return groups_most(a.p) * a.parts * W * 64; }
 
-// Parts of at least one block for each wavefront, so many that the 256 workgroups that the chip holds get two each.
+// Parts of at least one block for each wavefront, so many that there is a workgroup for each of the chip's 512 places (for 256 / 512 / 1024
+// workgroups: the case above 22.4 / 18.9 / 18.9 us, 64 tokens behind 4000 keys 132 / 102 / 109).
 void cut_paged_f32(PagedArgs &a)
 {
     const cf_attn_paged_params &p = a.p;
     const int64_t capacity = (int64_t)p.pages_per_seq * p.page_size;
     int64_t blocks = ((p.max_kv_len > 0 ? std::min<int64_t>(p.max_kv_len, capacity) : capacity) + RB - 1) / RB;
     if (p.window > 0) blocks = std::min(blocks, ((int64_t)p.window + RB) / RB + 2 + ((int64_t)a.mask.sinks + RB - 1) / RB);
-    const int64_t groups = groups_most(p), parts = std::min<int64_t>({(512 + groups - 1) / groups, (blocks + NW - 1) / NW, kMostParts});
+    const int64_t groups = groups_most(p), parts = std::min<int64_t>({(512 + groups - 1) / groups, (blocks + W - 1) / W, kMostParts});
     a.parts = (int)std::max<int64_t>(1, parts);
     a.tiles_per_part = (int)((blocks + a.parts - 1) / a.parts);
 }
@@ -157,8 +162,8 @@ void cut_paged_f32(PagedArgs &a)
 hipError_t launch_paged_f32(const PagedArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)(groups_most(a.p) * a.parts));
-    if (a.p.head_dim == 64) f32_paged_kernel<64><<<grid, NW * 64, 0, s>>>(a);
-    else f32_paged_kernel<128><<<grid, NW * 64, 0, s>>>(a);
+    if (a.p.head_dim == 64) f32_paged_kernel<64><<<grid, W * 64, 0, s>>>(a);
+    else f32_paged_kernel<128><<<grid, W * 64, 0, s>>>(a);
     return hipGetLastError();
 }
 
