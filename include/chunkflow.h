@@ -8,7 +8,8 @@
  *      several short sequences packed under a per-sequence causal mask (section 2.2) or one slice
  *      of a long sequence that also attends to the retained key/value state of that sequence's
  *      earlier chunks, the key/value gradients of those earlier rows being accumulated by the
- *      later chunks' backward passes (section 4.2).
+ *      later chunks' backward passes (section 4.2); the same with a sliding window and sinks; and,
+ *      forward only, over a paged key/value cache.
  *
  * Conventions
  *   - Every function returns CF_OK (0) or a negative error code; nothing throws, aborts or prints.

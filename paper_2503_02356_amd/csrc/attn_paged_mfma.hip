@@ -4,10 +4,12 @@
 // they all multiply with the same keys and values.  A tile is 128 of them.  A workgroup (4 wavefronts, 16x16x32 MFMAs, everything
 // transposed as in attn_mfma_fwd.hip: S^T = K Q^T, O^T += V^T P^T, the row on the lane axis) takes a tile and a part of its keys:
 //   many rows  (more than 32)  a wavefront has 32 rows; key tiles of 64 are shared through LDS, double buffered.  Bound by the MFMAs and
-//              the arithmetic between them, like the forward kernel of a chunk.
+//              the arithmetic between them, like the forward kernel of a chunk (8192 rows behind 24576 keys, 28/4 heads, D = 128: 2.96 ms,
+//              1137 TFLOP/s; that kernel on contiguous keys 2.93).
 //   few rows   every wavefront has all of them and takes every fourth block of 32 keys, copied into its own part of LDS: it waits for
 //              nobody.  Bound by the memory that holds the cache: 16 KB of keys and values a wavefront, 8 wavefronts a compute unit, are in
-//              flight or in use.  The four results meet in LDS at the end.
+//              flight or in use.  The four results meet in LDS at the end.  (64 tokens behind up to 16384 keys, 32/8 heads, D = 128, pages of 64:
+//              2.43 GB in 439 us, 5.5 TB/s; 256 with a window of 1024, 16/4, D = 64, pages of 32: 58 us, 4.7 TB/s.)
 // A long cache with few tiles is cut into parts, joined by a kernel behind this one (attn_paged.hip).
 // Pages: 16 consecutive keys lie in one page (a page holds a multiple of 16), so that each copy instruction (512 / D rows of a tile) has one
 // base, found with scalar instructions from a table entry that was loaded a tile ahead.  Keys that are hidden as a whole group (no such page,

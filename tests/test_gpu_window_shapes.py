@@ -1,0 +1,57 @@
+"""Windowed and paged calls at shapes where another path begins: thousands of sequences, wide groups of heads, pages that sequences share, the
+largest pages, more fp32 workgroups than compute units."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2503_02356_amd import binding as B
+from tests.test_gpu_paged import Batch, ints
+from tests.test_gpu_window import HUGE, Chunk
+
+pytestmark = pytest.mark.gpu
+BF16, FP32 = torch.bfloat16, torch.float32
+
+
+@pytest.mark.parametrize("dtype,new", [(BF16, 1), (BF16, 3), (FP32, 2)])
+def test_thousands_of_sequences(dtype, new):
+    """Sequences are found 64 bounds at a time: 4200 of them, runs of empty ones, some without a key."""
+    rng = np.random.default_rng(4)
+    seqs = [(int(rng.integers(0, new + 1)) if i % 700 < 500 else 0, int(rng.integers(0, 40))) for i in range(4200)]
+    b = Batch(seqs, 2, 1, 64, dtype, 16, pad=5, seed=13)
+    b.check(b.run(), new)
+
+
+@pytest.mark.parametrize("dtype,D,flags", [(BF16, 128, 0), (BF16, 64, 0), (FP32, 128, 0), (BF16, 128, B.CF_FLAG_SCALAR_KERNELS)])
+def test_wide_groups_and_shared_pages(dtype, D, flags):
+    """A group's rows are more than a tile of few rows holds; two sequences begin with the same pages."""
+    for Hq, Hkv in ((40, 1), (64, 1), (130, 2)):
+        b = Batch([(1, 700), (1, 300), (2, 40), (9, 320)], Hq, Hkv, D, dtype, 32, window=250, sinks=20, seed=14)
+        for i, columns in ((1, 8), (3, 5)):
+            b.table_host[i, :columns] = b.table_host[0, :columns]
+            for mine, first in zip(b.keys[i], b.keys[0]):
+                mine[:32 * columns] = first[:32 * columns]
+        b.table = ints(b.table_host)
+        b.check(b.run(flags), (Hq, Hkv))
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 64), (BF16, 128), (FP32, 64)])
+def test_the_largest_pages(dtype, D):
+    b = Batch([(1, 70000), (3, 10), (40, 65536)], 2, 1, D, dtype, 65536, seed=15)
+    b.check(b.run(), "largest pages")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_fp32_chunks_of_many_workgroups(D):
+    segs = [(300, 40), (1, 0), (17, 100), (700, 0)]
+    c = Chunk(segs, 8, 2, D, FP32, seed=16)
+    for window, sinks in ((1, 0), (60, 3), (333, 20), (HUGE, 0)):
+        c.check(c.run(window, sinks), c.reference(window, sinks), (window, sinks))
+    # one value of the first segment's key 70 (position 70, rows 30 .. 79 see it)
+    clean = c.run(50, 0, backward=False)
+    c.v[70, 1, 3] = float("nan")
+    got = c.run(50, 0, backward=False)
+    seen = torch.zeros(c.o.shape, dtype=torch.bool, device=c.o.device)
+    seen[30:80, 4:] = True
+    assert bool(torch.equal(got["o"][~seen], clean["o"][~seen])) and bool(torch.equal(got["lse"][:4], clean["lse"][:4]))
+    rows = got["o"][30:80, 4:]
+    assert bool(rows[..., 3].isnan().all()) and bool(torch.cat([rows[..., :3], rows[..., 4:]], -1).isfinite().all())
