@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2503_02356_amd import binding as B
+from tests import plain_window as W
 from tests.test_gpu_paged import Batch, ints
 from tests.test_gpu_window import HUGE, Chunk
 
@@ -46,12 +47,14 @@ def test_fp32_chunks_of_many_workgroups(D):
     c = Chunk(segs, 8, 2, D, FP32, seed=16)
     for window, sinks in ((1, 0), (60, 3), (333, 20), (HUGE, 0)):
         c.check(c.run(window, sinks), c.reference(window, sinks), (window, sinks))
-    # one value of the first segment's key 70 (position 70, rows 30 .. 79 see it)
-    clean = c.run(50, 0, backward=False)
+    # One value of the first segment's key 70 (position 70, rows 30 .. 79 see it).  Other rows of its block are done again pair by pair: they hold
+    # the definition's values, not the same bits.
+    ref = c.reference(50, 0)
+    tol = W.tolerances(ref, FP32, D, False)
     c.v[70, 1, 3] = float("nan")
     got = c.run(50, 0, backward=False)
     seen = torch.zeros(c.o.shape, dtype=torch.bool, device=c.o.device)
     seen[30:80, 4:] = True
-    assert bool(torch.equal(got["o"][~seen], clean["o"][~seen])) and bool(torch.equal(got["lse"][:4], clean["lse"][:4]))
+    W.check(dict(o=got["o"][~seen], lse=got["lse"]), dict(o=ref["o"][~seen], lse=ref["lse"]), dict(o=tol["o"][~seen], lse=tol["lse"]), "rows that do not see it")
     rows = got["o"][30:80, 4:]
     assert bool(rows[..., 3].isnan().all()) and bool(torch.cat([rows[..., :3], rows[..., 4:]], -1).isfinite().all())
