@@ -260,7 +260,7 @@ struct KeyArgs {
 // MFMAs the bf16 values of P and dS AND their bf16 rounding residuals: rows that see few keys have large P and dS, whose
 // rounding would be the largest error in dK/dV.  At D = 64 P and dS enter every product with all their 24 bits instead, as
 // three bf16 operands.
-// RING: operand fragments in flight (below).  wave: of this wavefront.
+// RING: operand fragments in flight (below; up to 3: a kernel that is short of registers, which loads its arguments again where it needs them).  wave: of this wavefront.
 // WindowMask: of a block's pairs those outside the window are hidden as those above the diagonal are; blocks that a wavefront's keys
 // have no part in are passed over; where no row sees more than 128 keys every pair is a RESIDUAL one.
 template <int D, bool FUSED_HEADS, int RING = 4, typename Mask = CausalMask>
@@ -281,8 +281,8 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
     // Block id -> (item, key/value head); the key/value head varies fastest (XCD L2 locality, see forward).
     //   fused mode : item = key tile rank, all G heads of the group
     //   otherwise  : item = entry of the work list
-    const KeyArgs first(b, wl, RING != 3);
-    auto args = [&] { return RING == 3 ? KeyArgs(b, wl, false) : first; };
+    const KeyArgs first(b, wl, RING > 3);
+    auto args = [&] { return RING <= 3 ? KeyArgs(b, wl, false) : first; };
     const int G = args().n_q_heads / args().n_kv_heads;
     const int kh = id % args().n_kv_heads;
     id /= args().n_kv_heads;
@@ -291,7 +291,7 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
     // the compiler: say so, or everything derived from them lives in vector registers.)
     if (FUSED_HEADS) {
         TileLocation loc;
-        if (!locate_tile<RING == 3>(args().cu_k, args().cu_q, p.n_segments, p.n_kv_tokens, BKV, id, loc)) return;
+        if (!locate_tile<RING <= 3>(args().cu_k, args().cu_q, p.n_segments, p.n_kv_tokens, BKV, id, loc)) return;
         q_seg0 = uniform(loc.other_begin), lq = uniform(loc.other_len), k_seg0 = uniform(loc.begin), lk = uniform(loc.len);
         // locate_tile numbers tiles from the end; the FIRST key tiles of a segment are seen by the most rows, so
         // flip the order inside the segment to start the heaviest tiles first.
@@ -709,15 +709,17 @@ __global__ __launch_bounds__(256, 2) void mfma_dkv_kernel(BwdArgs b, const float
     dkv_body<D, FUSED_HEADS>(b, delta, blockIdx.x, wl, st0, st1);
 }
 
-// One call with a window: the keys that some row sees, by a work list at either head_dim.  28/4 heads, D = 128: 8192 rows behind 24576 keys, window
+// One call with a window: the keys that some row sees, by a work list at either head_dim.  D = 64: with two fragments in flight it fits the
+// registers of three workgroups to a compute unit (16/4 heads, forward and backward, us, with four and two workgroups / so: 4096 packed around 300,
+// window 128 76.0 / 75.5, 4096 behind 5000, window 1000 179.9 / 175.3, 16384, window 512 305.5 / 301.6).  28/4 heads, D = 128: 8192 rows behind 24576 keys, window
 // 4096 910-1000 us (1.0 PFLOP/s); packed around 600, window 512 155 us, where the longest slot has 1.4 averages of pairs and an item's 128 KB
 // of atomic adds count (an only writer's rows added with loads and stores instead: 333 us a step against 336, no gain).
 template <int D>
-__global__ __launch_bounds__(256, 2) void mfma_window_dkv_kernel(BwdArgs b, const float *__restrict__ delta, const int *__restrict__ wl, WindowMask mask)
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void mfma_window_dkv_kernel(BwdArgs b, const float *__restrict__ delta, const int *__restrict__ wl, WindowMask mask)
 {
     __shared__ __attribute__((aligned(16))) char st0[DkvStage<D, true>::bytes];
     __shared__ __attribute__((aligned(16))) char st1[DkvStage<D, true>::bytes];
-    dkv_body<D, false, D == 128 ? 3 : 4>(b, delta, blockIdx.x, wl, st0, st1, wave_id(), mask);
+    dkv_body<D, false, D == 64 ? 2 : 3>(b, delta, blockIdx.x, wl, st0, st1, wave_id(), mask);
 }
 
 // Several chunks' backward in one launch.
