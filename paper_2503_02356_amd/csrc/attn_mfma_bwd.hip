@@ -111,14 +111,17 @@ struct ListCuts {
     // averages: of a fine item.  Windowed calls: 1.3, their key tiles having about the same pairs each (28/4 heads, forward and backward, us,
     // 1.6 / 1.3 / 1.0: 16384 rows, window 1024 1290 / 1221 / 1215, 8192 packed around 600, window 512 344 / 330 / 383, 2048 behind 8000, window 1024
     // 237 / 233 / 237; 32/8, 4096 packed around 300, window 128 171 / 175 / 195).
-    __host__ __device__ ListCuts(int total, int n_tiles, int n_q_heads, int slots, float averages = 1.6f)
+    // small_averages: of an item of a small call.  Windowed calls at D = 128: 2.6 (2.2 / 2.6 / 3.0: 16/4 heads, 2000 packed around 400, window 200
+    // 87.8 / 81.8 / 81.9, 4/4, 3000 behind 500, window 300 84.8 / 76.2 / 76.2, 28/4, 1000 packed around 200, window 100 81.7 / 82.3 / 86.8; D = 64,
+    // 2.2 / 3.0: 16/4, 4096 packed around 300, window 128 75.9 / 80.5).
+    __host__ __device__ ListCuts(int total, int n_tiles, int n_q_heads, int slots, float averages = 1.6f, float small_averages = 2.2f)
     {
         const int64_t all_pairs = (int64_t)total * n_q_heads;
         // (in floating point: a rounding moves a cut, and no more; 64-bit divisions would take longer than the rest of the list)
         average = (float)all_pairs / (float)slots;
         const int fine = share(average, averages);
         large = fine > kFineMost, small = slots == kSlots && average <= kSmallMost;
-        fair = small ? max(3, share(average, 2.2f)) : fine;
+        fair = small ? max(3, share(average, small_averages)) : fine;
         const int64_t head_items = (int64_t)n_tiles * n_q_heads;
         even_heads = small ? head_items > kSlots / 4 && head_items <= kSlots / 2
                            : !large && head_items > kSlots && head_items <= kSlots * 3 / 2;
@@ -140,7 +143,8 @@ struct ListCuts {
 // takes every fourth segment, its lanes the key tiles.
 // one_writer: one item to a key tile, however long.
 template <typename Mask = CausalMask>
-__device__ __forceinline__ void build_dkv_worklist(const BwdArgs::Fwd &p, int *wl, int capacity, int slots, const Mask &mask = Mask(), bool one_writer = false)
+__device__ __forceinline__ void build_dkv_worklist(const BwdArgs::Fwd &p, int *wl, int capacity, int slots, const Mask &mask = Mask(), bool one_writer = false,
+                                                   float small_averages = 2.2f)
 {
     __shared__ int bucket[kDurationBuckets];        // items per duration, then the next free slot of each duration
     __shared__ int seg_lq[256], seg_lk[256];
@@ -173,7 +177,7 @@ __device__ __forceinline__ void build_dkv_worklist(const BwdArgs::Fwd &p, int *w
     atomicAdd(&total, mine);
     atomicAdd(&n_tiles, my_tiles);
     __syncthreads();
-    const ListCuts cuts(total, n_tiles, p.n_q_heads, slots, Mask::windowed ? 1.3f : 1.6f);
+    const ListCuts cuts(total, n_tiles, p.n_q_heads, slots, Mask::windowed ? 1.3f : 1.6f, small_averages);
     bool cut_heads = true;
     auto for_each_item = [&](auto &&visit) {
         for_each_tile([&](int seg, int kt0, int n_qt) {
@@ -1076,7 +1080,7 @@ template <int D, int M>
 __global__ __launch_bounds__(256, 2) void mfma_window_dq_kernel(BwdArgs b, float *__restrict__ delta, int *wl, int capacity, int one_writer, WindowMask mask)
 {
     if (blockIdx.x == 0) {
-        build_dkv_worklist(b.f, wl, capacity, kSlots, mask, one_writer != 0);
+        build_dkv_worklist(b.f, wl, capacity, kSlots, mask, one_writer != 0, D == 128 ? 2.6f : 2.2f);
         return;
     }
     __shared__ __attribute__((aligned(16))) char stage_a[KvStage<D>::bytes];
