@@ -20,10 +20,11 @@ bool use_window_mfma(const cf_attn_bwd_params &b, const cf::WindowMask &mask)
 {
     return use_window_mfma(b.f) && b.do_stride_tok < kMostStride && cf::window_launch_size(b.f, mask) <= cf::kMostWorkItems;
 }
+int64_t list_bytes(const cf_attn_fwd_params &p, const cf::WindowMask &mask) { return round_up(256 + cf::window_worklist_capacity(p, mask) * 16, 256); }
 int64_t window_scratch(const cf_attn_fwd_params &p, const cf::WindowMask &mask)
 {
-    // (the scalar kernels' delta, whatever runs; behind it the list of the bf16 kernels or the sums of the fp32 one)
-    return delta_bytes(p) + (mfma_shape(p) ? 256 + cf::window_worklist_capacity(p, mask) * 16 : p.dtype == CF_FP32 ? cf::window_f32_scratch(p, mask) : 0);
+    // (the scalar kernels' delta, whatever runs; behind it the list of the bf16 kernels and dQ's parts, or the sums of the fp32 one)
+    return delta_bytes(p) + (mfma_shape(p) ? list_bytes(p, mask) + cf::window_dq_sums(p, mask) : p.dtype == CF_FP32 ? cf::window_f32_scratch(p, mask) : 0);
 }
 
 }  // namespace
@@ -67,7 +68,7 @@ extern "C" int cf_attn_window_bwd(const cf_attn_bwd_params *b, const cf_attn_win
         ws.worklist_items = cf::window_worklist_capacity(b->f, mask);
     }
     const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-    const hipError_t e = use_window_mfma(*b, mask) ? cf::launch_window_mfma_bwd(*b, ws, mask, s)
+    const hipError_t e = use_window_mfma(*b, mask) ? cf::launch_window_mfma_bwd(*b, ws, ws.delta + (delta_bytes(b->f) + list_bytes(b->f, mask)) / 4, mask, s)
                          : use_f32(*b)             ? cf::launch_window_f32_bwd(*b, ws.delta + delta_bytes(b->f) / 4, mask, s)
                                                    : cf::launch_window_simple_bwd(*b, ws, mask, s);
     return e == hipSuccess ? CF_OK : hip_fail(who, e);

@@ -85,6 +85,7 @@ constexpr int BQ = DkvShape<128>::BQ, BKV = DkvShape<128>::BKV;
 // Workspace layout (ints): [0] = number of items, [64 ...] = the items; an item is int4 {segment, kt0, first pair, pairs}.
 constexpr int kSlots = 512, kSplitTarget = 48, kFineMost = 64, kSmallMost = 8;
 constexpr int kDurationBuckets = 256;
+constexpr int kDqTiles = 6, kDqMost = 8;            // dQ in parts: key tiles of a part at least, parts at most
 
 // sum over segments of ceil(Lk / 128) <= n_kv_tokens / 128 + n_segments
 __host__ __device__ inline int64_t key_tiles_most(const cf_attn_fwd_params &p, const CausalMask & = CausalMask()) { return (int64_t)p.n_kv_tokens / BKV + p.n_segments; }
@@ -782,8 +783,15 @@ struct KvStage {
 // LDS, where the first has left them, and no tile's second half is computed where no row sees it.  Steps of 16 packed chunks, 28 / 4
 // heads: 512 tokens around 37 each 297 -> 269 us, 8192 around 600 9.31 -> 9.05 ms; 16 / 4 heads, D = 64, 16.7k tokens 979 -> 940 us.
 // WindowMask: key tiles as in the forward kernel; where no row sees more than 128 keys every tile is a head tile.
-template <int D, int M, typename Mask = CausalMask>
-__device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ delta, int id, char *stage_a, char *stage_b, const Mask &mask = Mask())
+// PARTS: a workgroup takes a part of the key tiles and leaves its sums, in fp32 and without the scale, for a kernel behind this one to add in
+// order (head tiles: the first part takes all).
+struct DqParts {
+    int parts;
+    float *sums;                                     // [part][row][query head][D]
+};
+template <int D, int M, typename Mask = CausalMask, bool PARTS = false>
+__device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ delta, int id, char *stage_a, char *stage_b, const Mask &mask = Mask(),
+                                        const DqParts &cut = DqParts())
 {
     using F = Mfma<M>;
     constexpr int KS = D / F::K, DB = D / F::M, N = F::N32, KVTILE_BYTES = KvStage<D>::tile_bytes;
@@ -796,6 +804,8 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
     const int G = a.n_q_heads / a.n_kv_heads;
     const int kh = id % a.n_kv_heads;
     id /= a.n_kv_heads;
+    const int part = PARTS ? id % cut.parts : 0;
+    if constexpr (PARTS) id /= cut.parts;
     const int j = id % G;                            // which of the G workgroups of this (tile, key/value head)
     const int rank = id / G;
 
@@ -825,6 +835,8 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
     const int kmax = q_tile0 + min(rows_valid, ((4 * j + 3) / G + 1) * 32) + off;   // keys [0, kmax) are visible to some row of the workgroup
     const KeyTiles<BN, Mask> key_tiles(mask, q_tile0 + (4 * j) / G * 32 + off, kmax);
     const int n_tiles = key_tiles.n;
+    const int per_part = PARTS && !head ? (n_tiles + cut.parts - 1) / cut.parts : n_tiles;
+    const int first_tile = PARTS ? min(n_tiles, part * per_part) : 0, end_tile = PARTS ? min(n_tiles, first_tile + per_part) : n_tiles;      // of this workgroup
     const int wq0 = q_tile0 + blk * 32;
     const int wave_kmax = min(kmax, wq0 + 32 + off);
     const bool wave_active = wq0 < lq;
@@ -864,7 +876,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
                 for (int e = 0; e < 8; ++e) dlt[qb] = __builtin_fmaf((float)of[e], (float)dof[qb][ks][e], dlt[qb]);
             }
             dlt[qb] = sum_over_groups<M>(dlt[qb]);
-            if (iq < lq && group == 0) delta[stat_at(qb)] = -dlt[qb];
+            if (iq < lq && group == 0 && part == 0) delta[stat_at(qb)] = -dlt[qb];
         }
     }
     const float c2 = p.softmax_scale * kLog2e;
@@ -887,7 +899,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
     auto sweep = [&](auto delta_pass_tag, int staged) {
         constexpr bool DELTA_PASS = decltype(delta_pass_tag)::value;
         if (staged == 0) {
-            issue_tile(key_tiles.start(0), stage_a);
+            issue_tile(key_tiles.start(first_tile), stage_a);
             wait_lds_dma();
             __syncthreads();
         }
@@ -895,7 +907,7 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
             const int tile_start = key_tiles.start(t);
             const char *ks_ = stage;
             const char *vs_ = stage + KVTILE_BYTES;
-            if (t + 1 < n_tiles && t + 1 >= staged) issue_tile(key_tiles.next(t, tile_start), next_stage);
+            if (t + 1 < end_tile && t + 1 >= staged) issue_tile(key_tiles.next(t, tile_start), next_stage);
 
             if (wave_active && tile_start < wave_kmax) {
                 bool need_mask = tile_start + BN - 1 > wq0 + off;
@@ -1022,12 +1034,12 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
             wait_lds_dma();
             __syncthreads();
         };
-        for (int t = 0; t < n_tiles; t += 2) {
+        for (int t = first_tile; t < end_tile; t += 2) {
             do_tile(t, stage_a, stage_b);
-            if (t + 1 < n_tiles) do_tile(t + 1, stage_b, stage_a);
+            if (t + 1 < end_tile) do_tile(t + 1, stage_b, stage_a);
         }
     };
-    if (head) {
+    if (head && part == 0) {
         sweep(std::true_type(), 0);
 #pragma unroll
         for (int qb = 0; qb < N; ++qb) {
@@ -1035,7 +1047,20 @@ __device__ __forceinline__ void dq_body(const BwdArgs &b, float *__restrict__ de
             if (row_of_block(qb) < lq && group == 0) delta[stat_at(qb)] = -dlt[qb];
         }
     }
-    sweep(std::false_type(), head && n_tiles <= 2 ? n_tiles : 0);
+    if (!PARTS || first_tile < end_tile) sweep(std::false_type(), head && n_tiles <= 2 ? n_tiles : 0);
+
+    if constexpr (PARTS) {
+#pragma unroll
+        for (int qb = 0; qb < N; ++qb) {
+            if (!wave_active || row_of_block(qb) >= lq) continue;
+            float *to = cut.sums + (((int64_t)part * p.n_tokens + q_seg0 + row_of_block(qb)) * a.n_q_heads + h) * D + 4 * group;
+#pragma unroll
+            for (int i = 0; i < D * F::R / F::M; i += 4)
+                *(f32x4 *)(to + F::place(i)) = f32x4{dq[i / F::R][qb][i % F::R], dq[i / F::R][qb][i % F::R + 1], dq[i / F::R][qb][i % F::R + 2],
+                                                     dq[i / F::R][qb][i % F::R + 3]};
+        }
+        return;
+    }
 
     if (wave_active) {
         // dQ rows leave through this wavefront's part of the (now idle) stage buffers, whole rows per store instruction
@@ -1086,6 +1111,65 @@ __global__ __launch_bounds__(256, 2) void mfma_window_dq_kernel(BwdArgs b, float
     __shared__ __attribute__((aligned(16))) char stage_a[KvStage<D>::bytes];
     __shared__ __attribute__((aligned(16))) char stage_b[KvStage<D>::bytes];
     dq_body<D, M>(b, delta, (int)blockIdx.x - 1, stage_a, stage_b, mask);
+}
+
+// Short slices behind a long window: their key tiles in parts, so many that the chip's 512 workgroup slots are filled, of six tiles at least (of four:
+// 500 rows behind 3000, 28/4 heads, D = 128, window 400 79.6 us for 76.8 with none).  Forward and backward, us, without / with parts: 100 rows behind
+// 30000, 28/4, D = 128, window 4096 265 / 185, 2000 rows, 4/4, window 1500 113.8 / 92.1, 600 behind 5000, 16/4, D = 64, window 2048 118.2 / 100.4, 1000 behind 20000,
+// 28/4, window 4096 (two parts) 367 / 355.
+template <int D, int M>
+__global__ __launch_bounds__(256, 2) void mfma_window_dq_parts_kernel(BwdArgs b, float *__restrict__ delta, int *wl, int capacity, int one_writer, WindowMask mask,
+                                                                      DqParts cut)
+{
+    if (blockIdx.x == 0) {
+        build_dkv_worklist(b.f, wl, capacity, kSlots, mask, one_writer != 0, D == 128 ? 2.6f : 2.2f);
+        return;
+    }
+    __shared__ __attribute__((aligned(16))) char stage_a[KvStage<D>::bytes];
+    __shared__ __attribute__((aligned(16))) char stage_b[KvStage<D>::bytes];
+    dq_body<D, M, WindowMask, true>(b, delta, (int)blockIdx.x - 1, stage_a, stage_b, mask, cut);
+}
+// dQ of the rows from their parts, D / 8 lanes to a row; a row that is not finite once more pair by pair.  Bound by the parts' bytes, at most 32 MB.
+template <int D>
+__global__ __launch_bounds__(256) void window_dq_join_kernel(cf_attn_bwd_params b, const float *__restrict__ delta, WindowMask mask, DqParts cut)
+{
+    const cf_attn_fwd_params &p = b.f;
+    constexpr int LANES = D / 8;
+    const int64_t all = (int64_t)p.n_tokens * p.n_q_heads, at = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES, id = min(at, all - 1);
+    const bool mine = at < (int64_t)min(p.n_tokens, p.cu_seqlens_q[p.n_segments]) * p.n_q_heads;       // (of the other rows there is nothing)
+    const int c = threadIdx.x % LANES;
+    const float *from = cut.sums + id * D + 8 * c;
+    f32x4 sum[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    for (int x = 0; x < cut.parts; x += 4) {         // (four parts in flight)
+        f32x4 v[4][2];
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) v[y][e] = *(const f32x4 *)(from + min(x + y, cut.parts - 1) * all * D + 4 * e);
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (x + y < cut.parts) sum[e] += v[y][e];
+    }
+    const int row = (int)(id / p.n_q_heads), h = (int)(id - (int64_t)row * p.n_q_heads);
+    float f[8];
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        f[e] = sum[e / 4][e % 4] * p.softmax_scale;
+        bad = bad || !finite(f[e]);
+    }
+    if (mine) *(bf16x8 *)((char *)b.d_q + ((int64_t)row * b.dq_stride_tok + (int64_t)h * b.dq_stride_head + 8 * c) * 2) = pack8(f);
+    for (unsigned long long left = __ballot(bad && mine); left != 0;) {
+        const int first = (__ffsll((long long)left) - 1) / LANES * LANES;
+        left &= ~(((1ull << LANES) - 1) << first);
+        const int r = __shfl(row, first), head = __shfl(h, first);
+        const unsigned short *qr = row_of<unsigned short>(p.q, r, p.q_stride_tok, head, p.q_stride_head);
+        const unsigned short *dr = row_of<unsigned short>(b.d_o, r, b.do_stride_tok, head, b.do_stride_head);
+        scalar_dq_row<unsigned short, D, 4>(b, segment_of_query(p, r), r, head, [&](int x) { return ld(qr + x); }, [&](int x) { return ld(dr + x); },
+                                            -delta[(int64_t)head * p.n_tokens + r], mask);
+    }
 }
 
 // Several chunks, heaviest first: dQ and delta of a chunk depend on nothing another chunk's backward writes, so the last,
@@ -1295,30 +1379,56 @@ int64_t mfma_bwd_blocks(const cf_attn_fwd_params &p)
     return std::max(q_tiles_most(p) * p.n_q_heads + 1, std::max(kv_tiles_most(p), items) * p.n_kv_heads);
 }
 
+int window_dq_parts(const cf_attn_fwd_params &p, const WindowMask &mask);
 // Windowed calls: room for the list, and launches.
 int64_t window_worklist_capacity(const cf_attn_fwd_params &p, const WindowMask &mask) { return dkv_items_most(p, mask); }
 int64_t window_launch_size(const cf_attn_fwd_params &p, const WindowMask &mask)
 {
-    return std::max(q_tiles_most(p) * p.n_q_heads + 1, window_worklist_capacity(p, mask) * p.n_kv_heads) * 256;
+    return std::max(q_tiles_most(p) * p.n_q_heads * window_dq_parts(p, mask) + 1, window_worklist_capacity(p, mask) * p.n_kv_heads) * 256;
+}
+
+// Parts of a call's key tiles in dQ, 1: none.
+int window_dq_parts(const cf_attn_fwd_params &p, const WindowMask &mask)
+{
+    if (mask.few(128)) return 1;
+    const int64_t units = ((int64_t)p.n_tokens + 31) / 32 + p.n_segments - 1, active = (units * p.n_q_heads + 3) / 4;
+    const int64_t seen = ((int64_t)mask.window + 31 + BN - 1) / BN + 1 + ((int64_t)mask.sinks + BN - 1) / BN, keys = (int64_t)p.n_kv_tokens / p.n_segments;
+    const int64_t parts = std::min<int64_t>({kSlots / active, std::min(seen, (keys + BN - 1) / BN) / kDqTiles, kDqMost});
+    return (int)std::max<int64_t>(1, parts);
+}
+int64_t window_dq_sums(const cf_attn_fwd_params &p, const WindowMask &mask)
+{
+    const int parts = window_dq_parts(p, mask);
+    return parts > 1 ? (int64_t)parts * p.n_tokens * p.n_q_heads * p.head_dim * 4 : 0;
 }
 
 template <int D>
-static hipError_t run_window_bwd(const cf_attn_bwd_params &b, const BwdWorkspace &ws, const WindowMask &mask, hipStream_t s)
+static hipError_t run_window_bwd(const cf_attn_bwd_params &b, const BwdWorkspace &ws, float *dq_sums, const WindowMask &mask, hipStream_t s)
 {
-    const int64_t dq_blocks = q_tiles_most(b.f) * b.f.n_q_heads + 1, dkv_blocks = ws.worklist_items * b.f.n_kv_heads;
+    const DqParts cut = {window_dq_parts(b.f, mask), dq_sums};
+    const int64_t dq_blocks = q_tiles_most(b.f) * b.f.n_q_heads * cut.parts + 1, dkv_blocks = ws.worklist_items * b.f.n_kv_heads;
     if (dq_blocks > 0x7fffffffLL || dkv_blocks > 0x7fffffffLL || ws.worklist_items > 0x7fffffffLL) return hipErrorInvalidConfiguration;
     const int one_writer = (b.f.flags & CF_FLAG_DKV_SINGLE_WRITER) != 0, capacity = (int)ws.worklist_items;
     const dim3 grid((unsigned)dq_blocks);
-    if (D == 64 || wide_mfma(b.f)) mfma_window_dq_kernel<D, 32><<<grid, 256, 0, s>>>(b, ws.delta, ws.worklist, capacity, one_writer, mask);
-    else if constexpr (D == 128) mfma_window_dq_kernel<D, 16><<<grid, 256, 0, s>>>(b, ws.delta, ws.worklist, capacity, one_writer, mask);
-    const hipError_t e = hipGetLastError();
+    if (D == 64 || wide_mfma(b.f)) {
+        if (cut.parts > 1) mfma_window_dq_parts_kernel<D, 32><<<grid, 256, 0, s>>>(b, ws.delta, ws.worklist, capacity, one_writer, mask, cut);
+        else mfma_window_dq_kernel<D, 32><<<grid, 256, 0, s>>>(b, ws.delta, ws.worklist, capacity, one_writer, mask);
+    } else if constexpr (D == 128) {
+        if (cut.parts > 1) mfma_window_dq_parts_kernel<D, 16><<<grid, 256, 0, s>>>(b, ws.delta, ws.worklist, capacity, one_writer, mask, cut);
+        else mfma_window_dq_kernel<D, 16><<<grid, 256, 0, s>>>(b, ws.delta, ws.worklist, capacity, one_writer, mask);
+    }
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     mfma_window_dkv_kernel<D><<<dim3((unsigned)dkv_blocks), 256, 0, s>>>(b, ws.delta, ws.worklist, mask);
+    e = hipGetLastError();
+    if (e != hipSuccess || cut.parts == 1) return e;
+    constexpr int ROWS = 256 / (D / 8);
+    window_dq_join_kernel<D><<<dim3((unsigned)(((int64_t)b.f.n_tokens * b.f.n_q_heads + ROWS - 1) / ROWS)), 256, 0, s>>>(b, ws.delta, mask, cut);
     return hipGetLastError();
 }
-hipError_t launch_window_mfma_bwd(const cf_attn_bwd_params &b, const BwdWorkspace &ws, const WindowMask &mask, hipStream_t s)
+hipError_t launch_window_mfma_bwd(const cf_attn_bwd_params &b, const BwdWorkspace &ws, float *dq_sums, const WindowMask &mask, hipStream_t s)
 {
-    return b.f.head_dim == 64 ? run_window_bwd<64>(b, ws, mask, s) : run_window_bwd<128>(b, ws, mask, s);
+    return b.f.head_dim == 64 ? run_window_bwd<64>(b, ws, dq_sums, mask, s) : run_window_bwd<128>(b, ws, dq_sums, mask, s);
 }
 
 int64_t dkv_worklist_least(const cf_attn_fwd_params &p) { return key_tiles_most(p) * (p.n_q_heads / p.n_kv_heads); }

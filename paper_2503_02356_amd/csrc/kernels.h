@@ -199,7 +199,8 @@ hipError_t launch_window_simple_bwd(const cf_attn_bwd_params &b, const BwdWorksp
 bool window_few(const cf_attn_fwd_params &p);
 hipError_t launch_window_few(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s);
 hipError_t launch_window_mfma_fwd(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s);
-hipError_t launch_window_mfma_bwd(const cf_attn_bwd_params &b, const BwdWorkspace &ws, const WindowMask &mask, hipStream_t s);
+hipError_t launch_window_mfma_bwd(const cf_attn_bwd_params &b, const BwdWorkspace &ws, float *dq_sums, const WindowMask &mask, hipStream_t s);
+int64_t window_dq_sums(const cf_attn_fwd_params &p, const WindowMask &mask);      // bytes of dq_sums (0: not needed)
 int64_t window_launch_size(const cf_attn_fwd_params &p, const WindowMask &mask);      // work-items of the backward's larger launch
 int64_t window_worklist_capacity(const cf_attn_fwd_params &p, const WindowMask &mask);
 hipError_t launch_window_f32_fwd(const cf_attn_fwd_params &p, const WindowMask &mask, hipStream_t s);

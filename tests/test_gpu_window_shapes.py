@@ -58,3 +58,22 @@ def test_fp32_chunks_of_many_workgroups(D):
     W.check(dict(o=got["o"][~seen], lse=got["lse"]), dict(o=ref["o"][~seen], lse=ref["lse"]), dict(o=tol["o"][~seen], lse=tol["lse"]), "rows that do not see it")
     rows = got["o"][30:80, 4:]
     assert bool(rows[..., 3].isnan().all()) and bool(torch.cat([rows[..., :3], rows[..., 4:]], -1).isfinite().all())
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 64), (BF16, 128)])
+def test_short_slices_behind_long_windows(dtype, D):
+    """dQ from parts of the keys: parts that end inside the sinks' and the window's tiles, rows near the beginning, a segment of one row, results
+    that repeat bit for bit and a value that is not finite in one row's dO."""
+    segs = [(27, 4000), (1, 2500), (40, 10), (65, 700)]
+    for Hq, Hkv in ((7, 1), (4, 4)):
+        c = Chunk(segs, Hq, Hkv, D, dtype, seed=17)
+        for window, sinks in ((3000, 100), (129, 0), (HUGE, 0), (1000, 1500)):
+            got = c.run(window, sinks)
+            c.check(got, c.reference(window, sinks), (Hq, window, sinks))
+            assert bool(torch.equal(got["dq"], c.run(window, sinks)["dq"]))
+    clean = c.run(3000, 100)
+    c.d_o[5, 1, 7] = float("inf")
+    got = c.run(3000, 100)
+    others = torch.ones(clean["dq"].shape[:2], dtype=torch.bool, device=c.o.device)
+    others[5, 1] = False
+    assert bool(torch.equal(got["dq"][others], clean["dq"][others])) and not bool(got["dq"][5, 1].isfinite().all())
