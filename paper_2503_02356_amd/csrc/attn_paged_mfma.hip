@@ -26,9 +26,10 @@ namespace {
 
 constexpr int BM = 128, BN = 64;             // rows of a tile, keys of a key tile
 constexpr int FEW = 32;                      // rows that the wavefronts share, keys of their blocks
-// Tiles of FEW rows of a windowed chunk that goes this way: one round of workgroups.  Forward, 28/4 heads, window 256, us, its rows to the
-// wavefronts / its keys: 1 row behind 500 keys 11.5 / 7.0, 33 behind 500 13.5 / 11.3, 250 behind 5000 14.3 / 11.7, 500 behind 8000 14.4 / 13.7;
-// 32/8 heads, window 4000: 100 behind 2000 41.5 / 27.0, 250 behind 5000 81.4 / 46.9, 500 behind 8000 81.7 / 64.3.
+// Tiles of FEW rows of a windowed chunk that goes this way: one round of workgroups; of half as many rows where that still is one round.  Forward,
+// 28/4 heads, window 256, us, its rows to the wavefronts / its keys, tiles of 32 / of 16: 1 row behind 500 keys 11.5 / 8.0 / 7.9, 33 behind 500
+// 13.5 / 11.3 / 8.1, 250 behind 5000 14.3 / 11.7 / 10.3, 500 behind 8000 14.4 / 13.4 / 16.7 (two rounds); 32/8 heads, window 4000: 100 behind 2000 41.5 /
+// 27.0 / 19.6, 400 behind 2000 with tiles of 32 35.7, of 16 47.1.
 constexpr int64_t kWindowFewTiles = 512;
 using F = Mfma<16>;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -537,8 +538,9 @@ __device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, 
     }
 }
 
-// MODE: FEW rows to a tile, all by few_rows; BM rows, all by many_rows; BOTH: BM rows, by what a tile holds; CHUNK: as FEW, keys in one piece.
-enum Mode { kFew, kMany, kBoth, kChunk };
+// MODE: FEW rows to a tile, all by few_rows; BM rows, all by many_rows; BOTH: BM rows, by what a tile holds; CHUNK: as FEW, keys in one piece;
+// CHUNK_HALF: the same with half the rows.
+enum Mode { kFew, kMany, kBoth, kChunk, kChunkHalf };
 template <int D, Mode MODE, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void mfma_paged_kernel(PagedArgs a)
 {
@@ -551,9 +553,10 @@ __global__ __launch_bounds__(256, 2) void mfma_paged_kernel(PagedArgs a)
     t.kh = id % a.p.n_kv_heads;                      // (fastest: an XCD keeps reading the same heads; attn_mfma_fwd.hip)
     id /= a.p.n_kv_heads;
     const int part = id % a.parts;
-    if (!find_tile<MODE == kFew || MODE == kChunk ? FEW : BM, MODE == kChunk>(a, id / a.parts, t)) return;
+    constexpr bool CHUNK = MODE == kChunk || MODE == kChunkHalf;
+    if (!find_tile<MODE == kChunkHalf ? FEW / 2 : MODE == kFew || MODE == kChunk ? FEW : BM, CHUNK>(a, id / a.parts, t)) return;
     const int lowest = t.position(0), highest = t.position(t.rows - 1);
-    const int keys = MODE == kChunk ? highest + 1 : at_most(highest + 1, a.p.pages_per_seq << a.shift);
+    const int keys = CHUNK ? highest + 1 : at_most(highest + 1, a.p.pages_per_seq << a.shift);
     const KeyTiles<BN, WindowMask> tiles(a.mask, lowest, keys);
     // (BOTH: tiles of many rows are cut a third as often, for a part of them leaves four times as much to be joined)
     const int thirds = MODE == kBoth && t.rows > FEW ? 3 : 1, per_part = a.tiles_per_part * thirds, last_part = (a.parts - 1) / thirds;
@@ -572,8 +575,8 @@ __global__ __launch_bounds__(256, 2) void mfma_paged_kernel(PagedArgs a)
     if (MODE == kMany || (MODE == kBoth && t.rows > FEW)) {
         many_rows<D, WHOLE>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
     } else if constexpr (MODE != kMany) {
-        if (t.rows > 16) few_rows<D, 2, WHOLE, MODE == kChunk>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
-        else few_rows<D, 1, WHOLE, MODE == kChunk>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
+        if (MODE != kChunkHalf && t.rows > 16) few_rows<D, 2, WHOLE, CHUNK>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
+        else few_rows<D, 1, WHOLE, CHUNK>(a, t, tiles, first, end, keys, part, stage_a, stage_b);
     }
 }
 
@@ -639,9 +642,14 @@ hipError_t launch_window_few(const cf_attn_fwd_params &p, const WindowMask &mask
     a.p.k_pages = p.k, a.p.v_pages = p.v, a.p.kv_stride_tok = p.kv_stride_tok, a.p.kv_stride_head = p.kv_stride_head;
     a.p.o = p.o, a.p.o_stride_tok = p.o_stride_tok, a.p.o_stride_head = p.o_stride_head, a.p.lse = p.lse;
     a.mask = mask, a.parts = 1, a.tiles_per_part = 1 << 28, a.shift = 30;
-    const dim3 grid((unsigned)(((int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads) / FEW + p.n_segments) * p.n_kv_heads));
-    if (p.head_dim == 64) mfma_paged_kernel<64, kChunk, true><<<grid, 256, 0, s>>>(a);
-    else mfma_paged_kernel<128, kChunk, true><<<grid, 256, 0, s>>>(a);
+    auto grid = [&](int rows) { return dim3((unsigned)(((int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads) / rows + p.n_segments) * p.n_kv_heads)); };
+    if (((int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads) / (FEW / 2) + p.n_segments) * p.n_kv_heads <= kWindowFewTiles) {
+        if (p.head_dim == 64) mfma_paged_kernel<64, kChunkHalf, true><<<grid(FEW / 2), 256, 0, s>>>(a);
+        else mfma_paged_kernel<128, kChunkHalf, true><<<grid(FEW / 2), 256, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    if (p.head_dim == 64) mfma_paged_kernel<64, kChunk, true><<<grid(FEW), 256, 0, s>>>(a);
+    else mfma_paged_kernel<128, kChunk, true><<<grid(FEW), 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
