@@ -77,3 +77,35 @@ def test_short_slices_behind_long_windows(dtype, D):
     others = torch.ones(clean["dq"].shape[:2], dtype=torch.bool, device=c.o.device)
     others[5, 1] = False
     assert bool(torch.equal(got["dq"][others], clean["dq"][others])) and not bool(got["dq"][5, 1].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 64), (BF16, 128)])
+@pytest.mark.parametrize("segs", [[(400, 50), (1, 0), (180, 300)], [(900, 50), (1, 0), (300, 700), (129, 0)]])
+def test_chunks_of_more_rows(dtype, D, segs):
+    """Too many rows for tiles of 16, and for the wavefronts to share keys at all; then one value of the first segment's key 70."""
+    c = Chunk(segs, 16, 2, D, dtype, seed=18)
+    for window, sinks in ((1, 0), (100, 4), (130, 70), (700, 129), (HUGE, 0)):
+        c.check(c.run(window, sinks, tiles=window == 100), c.reference(window, sinks), (window, sinks))
+    ref = c.reference(50, 0)
+    tol = W.tolerances(ref, dtype, D, True)
+    c.v[70, 1, 3] = float("inf")
+    got = c.run(50, 0, backward=False)
+    seen = torch.zeros(c.o.shape, dtype=torch.bool, device=c.o.device)
+    seen[20:70, 8:] = True                           # (position 70, behind 50: rows 20 .. 69 see it)
+    W.check(dict(o=got["o"][~seen], lse=got["lse"]), dict(o=ref["o"][~seen], lse=ref["lse"]), dict(o=tol["o"][~seen], lse=tol["lse"]), "rows that do not see it")
+    rows = got["o"][20:70, 8:]
+    assert bool((rows[..., 3] == float("inf")).all()) and bool(torch.cat([rows[..., :3], rows[..., 4:]], -1).isfinite().all())
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_longer_slices_behind_long_windows(D):
+    """dQ from parts with the matrix instruction of larger calls; a value that nobody sees changes nothing."""
+    c = Chunk([(600, 2500), (300, 20)], 16, 2, D, BF16, seed=19)
+    for window, sinks in ((2000, 4), (HUGE, 0), (700, 900)):
+        got = c.run(window, sinks)
+        c.check(got, c.reference(window, sinks), (window, sinks))
+        assert bool(torch.equal(got["dq"], c.run(window, sinks)["dq"]))
+    clean = c.run(1500, 0)
+    c.k[100, 1, 5] = float("inf")                    # (position 100: no row of the first segment sees it, whose rows begin at 2500)
+    got = c.run(1500, 0)
+    assert bool(torch.equal(got["o"], clean["o"])) and bool(torch.equal(got["dq"], clean["dq"]))
