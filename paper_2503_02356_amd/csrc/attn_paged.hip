@@ -57,9 +57,10 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join_kernel(PagedArgs a)
 #pragma unroll
         for (int e = 0; e < E; ++e) v[x][e] = o_parts[(int64_t)part * all * D + e];
     };
-    auto add = [&](int x, float w) {
+    // held: of a part that had keys.  (One without holds anything.  A weight of 0 takes an infinity or a NaN along, as it does in one piece.)
+    auto add = [&](int x, float w, bool held) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] += w == 0.f ? 0.f : w * v[x][e];      // (a part without keys holds anything)
+        for (int e = 0; e < E; ++e) acc[e] += held ? w * v[x][e] : 0.f;
     };
     auto fetch_every = [&](int x0) {
 #pragma unroll
@@ -69,11 +70,13 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join_kernel(PagedArgs a)
     float2 ml = {-INFINITY, 0.f};
     if (inside && lane < a.parts) ml = a.part_ml[r * a.parts + lane];
     const int64_t rows = (int64_t)min(p.n_tokens, p.cu_seqlens_q[p.n_seqs]) * p.n_q_heads;
+    // A part without keys is (-infinity, 0); (-infinity, NaN) is one whose scores are NaN (a maximum takes none), and so is its row.
+    const unsigned long long with_keys = __ballot(!(ml.x == -INFINITY && ml.y == 0.f));
     const float M = wave_max(ml.x), ref = M == -INFINITY ? 0.f : M;
-    const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - ref);
+    const float w = __builtin_amdgcn_exp2f(ml.x - ref);
     const float L = wave_sum(w * ml.y);
     if constexpr (WAVES == 1) {
-        for (unsigned long long left = __ballot(ml.x != -INFINITY); left != 0;) {
+        for (unsigned long long left = with_keys; left != 0;) {
             int at[AT_ONCE], n = 0;
 #pragma unroll
             for (int x = 0; x < AT_ONCE; ++x) {      // (the last one again where there are no more)
@@ -85,7 +88,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join_kernel(PagedArgs a)
 #pragma unroll
             for (int x = 0; x < AT_ONCE; ++x) {
                 const float wx = __shfl(w, at[x]);
-                add(x, x < n ? wx : 0.f);
+                add(x, wx, x < n);
             }
         }
     } else {
@@ -94,7 +97,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join_kernel(PagedArgs a)
             for (int x = 0; x < AT_ONCE; ++x) {
                 const int at = x0 + WAVES * x;
                 const float wx = __shfl(w, at & 63);
-                add(x, at < a.parts ? wx : 0.f);
+                add(x, wx, at < a.parts && (with_keys >> (at & 63) & 1));
             }
             x0 += WAVES * AT_ONCE;
             if (x0 >= a.parts) break;
@@ -112,10 +115,11 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join_kernel(PagedArgs a)
     if (r >= rows) return;
     const int64_t row = r / p.n_q_heads, h = r - row * p.n_q_heads;
     T *o = (T *)p.o + row * p.o_stride_tok + h * p.o_stride_head;
-    const float inv = M == -INFINITY ? 0.f : 1.f / L;
+    const bool none = M == -INFINITY && L == 0.f;
+    const float inv = none ? 0.f : 1.f / L;
 #pragma unroll
     for (int e = 0; e < E; ++e) st(o + lane * E + e, acc[e] * inv);
-    if (lane == 0 && p.lse) p.lse[h * p.n_tokens + row] = M == -INFINITY ? -INFINITY : __builtin_fmaf(M, 0.69314718055994530942f, logf(L));
+    if (lane == 0 && p.lse) p.lse[h * p.n_tokens + row] = none ? -INFINITY : __builtin_fmaf(M, 0.69314718055994530942f, logf(L));
 }
 
 // 16 bytes a thread: a token's key (blockIdx.y 0) or value row, all heads.  Bound by memory, few tokens by the launch and three loads that depend on

@@ -1,0 +1,138 @@
+"""Paged calls whose keys are cut into parts: what is not finite in a query, a key or a value comes out as it does where a row's keys are not cut (the
+scalar kernels), whatever part it stands in."""
+import math
+
+import pytest
+import torch
+
+from paper_2503_02356_amd import binding as B
+from tests import plain_window as W
+from tests.test_gpu_paged import Batch
+
+pytestmark = pytest.mark.gpu
+BF16, FP32 = torch.bfloat16, torch.float32
+NAN, INF = float("nan"), float("inf")
+KINDS = [(BF16, 128), (BF16, 64), (FP32, 128), (FP32, 64)]
+# sequences, (query heads, key/value heads), page, window: many parts, some, parts of mixed batches, of windows
+CALLS = [([(1, 5000)], (8, 2), 16, 0), ([(40, 3000)], (8, 2), 64, 0), ([(1, 3000), (70, 2500), (1, 900), (3, 4000)], (4, 2), 32, 0),
+         ([(1, 5000), (2, 300)], (14, 2), 64, 2500)]
+
+
+def parts(b):
+    p = b.params()
+    return B.cf_attn_paged_workspace_bytes(p) // (p.n_tokens * p.n_q_heads * (p.head_dim * 4 + 8))
+
+
+def both(b):
+    """(o, lse) of the matrix kernels and of the scalar ones."""
+    r = []
+    for flags in (0, B.CF_FLAG_SCALAR_KERNELS):
+        b.o.fill_(7), b.lse.fill_(7)
+        B.cf_attn_paged_fwd(b.params(flags))
+        torch.cuda.synchronize()
+        r.append((b.o.double(), b.lse.double()))
+    return r
+
+
+def same_kind(b, what):
+    (o, lse), (o1, lse1) = both(b)
+    for name, x, y in (("o", o, o1), ("lse", lse, lse1)):
+        for kind in (torch.isnan, torch.isposinf, torch.isneginf):
+            assert bool(torch.equal(kind(x), kind(y))), (what, name, kind.__name__, int(kind(x).sum()), int(kind(y).sum()))
+    return o, lse
+
+
+def rows_of(b, i):
+    first = sum(a for a, _ in b.seqs[:i])
+    return slice(first, first + b.seqs[i][0])
+
+
+def check_others(b, ref, tol, o, lse, affected, what):
+    """Rows and heads that do not see it are what they are without it."""
+    keep = ~affected
+    W.check(dict(o=o[keep], lse=lse.t()[keep]), dict(o=ref["o"][keep], lse=ref["lse"].t()[keep]), dict(o=tol["o"][keep], lse=tol["lse"].t()[keep]), what)
+
+
+@pytest.mark.parametrize("dtype,D", KINDS)
+@pytest.mark.parametrize("n", range(len(CALLS)))
+def test_what_is_not_finite_in_a_cut_call(dtype, D, n):
+    seqs, (Hq, Hkv), page, window = CALLS[n]
+    b = Batch(seqs, Hq, Hkv, D, dtype, page, window, seed=20 + n)
+    b.append()
+    assert parts(b) > 1
+    ref = b.reference()
+    tol = W.tolerances(ref, dtype, D, dtype == BF16)
+    G = Hq // Hkv
+    affected = torch.zeros(b.o.shape[:2], dtype=torch.bool, device=b.o.device)
+    for i in (0, len(seqs) - 1):
+        rows, length = rows_of(b, i), seqs[i][1]
+        first, last = rows.start, rows.stop - 1
+        # a query: its row and head, and no other
+        for value in (NAN, INF):
+            keep = b.q[last, 1].clone()
+            b.q[last, 1, 5] = value
+            o, lse = same_kind(b, ("query", value, i))
+            assert bool(o[last, 1].isnan().all()) and bool(lse[1, last].isnan())
+            affected.zero_()
+            affected[last, 1] = True
+            check_others(b, ref, tol, o, lse, affected, ("query", value, i))
+            b.q[last, 1] = keep
+        affected.zero_()
+        affected[rows, G:] = True                    # the rows of the sequence that see keys of the last key/value head
+        for which in ("kp", "vp"):
+            pages = getattr(b, which)
+            for value in (NAN, INF, -INF):
+                for lo, hi in ((length - 1 - seqs[i][0], length - seqs[i][0]), (length // 2, length // 2 + 1), (length // 2 - 700, length // 2 + 700),
+                               (max(0, length - window if window else 0), length)):
+                    at = [(int(b.table_host[i, j // page]), j % page) for j in range(max(0, lo), min(hi, length))]
+                    assert at and all(0 <= x < b.n_pages for x, _ in at)
+                    pg, row = (torch.tensor(x, device=b.o.device) for x in zip(*at))
+                    keep = pages[pg, row, Hkv - 1].clone()
+                    pages[pg, row, Hkv - 1, 3] = value
+                    what = (which, value, i, lo, hi)
+                    o, lse = same_kind(b, what)
+                    check_others(b, ref, tol, o, lse, affected, what)
+                    seen = lo >= 0 and (not window or hi > length - window)
+                    if seen and which == "kp" and value != value:
+                        assert bool(o[first + seqs[i][0] - 1, G:].isnan().all()) and bool(lse[G:, last].isnan().all()), what
+                    if seen and which == "vp" and lo >= 0:
+                        assert not bool(o[last, G:, 3].isfinite().any()) and bool(lse[G:, last].isfinite().all()), what
+                        assert bool(o[last, G:, :3].isfinite().all()) and bool(o[last, G:, 4:].isfinite().all()), what
+                    pages[pg, row, Hkv - 1] = keep
+
+
+@pytest.mark.parametrize("dtype,D", KINDS)
+def test_a_value_whose_weight_is_zero(dtype, D):
+    """An infinite value of a visible key whose weight is no number above 0 in 32 bits: infinity by the definition, or 0 times infinity, but no
+    number.  (Which of the two depends on how the weight is formed: e^-120 at once is 0, as a product over tiles or parts, e^-60 e^-60 applied to an
+    infinite sum one after the other, it leaves infinity.  So the scalar kernels may have the other one.)"""
+    b = Batch([(1, 5000)], 8, 2, D, dtype, 16, seed=30, scale=10.0)
+    b.append()
+    assert parts(b) > 16
+    j = 1234
+    k = b.keys[0][0].double()
+    scores = (b.q[0].double() * k.repeat_interleave(4, 1)).sum(-1) * b.scale
+    assert bool((scores.amax(0) - scores[j] > 120).all())        # e^-120 = 2^-173
+    at = (int(b.table_host[0, j // 16]), j % 16)
+    assert 0 <= at[0] < b.n_pages
+    b.vp[at[0], at[1], 1, 3] = INF
+    for o, lse in both(b):
+        assert not bool(o[0, 4:, 3].isfinite().any()) and bool(o[0, :4].isfinite().all()) and bool(lse.isfinite().all())
+        assert bool(o[0, 4:, :3].isfinite().all()) and bool(o[0, 4:, 4:].isfinite().all())
+
+
+@pytest.mark.parametrize("dtype,D", KINDS)
+def test_rows_without_keys_in_a_cut_call(dtype, D):
+    """Sequences without a key, and rows all of whose pages are none, beside long ones: zeros, whatever the workspace holds."""
+    hidden = {(2, c): -1 for c in range(20)}
+    b = Batch([(1, 5000), (1, 0), (1, 300), (3, 2)], 8, 2, D, dtype, 16, hidden=hidden, seed=31)
+    b.append()
+    need = B.cf_attn_paged_workspace_bytes(b.params())
+    assert parts(b) > 1
+    for fill in (0.0, NAN):
+        ws = torch.full((need // 4,), fill, device=b.o.device)
+        B.cf_attn_paged_fwd(b.params(workspace=ws.view(torch.uint8)))
+        torch.cuda.synchronize()
+        b.check(dict(o=b.o, lse=b.lse), fill)
+        for row in (1, 2, 3):
+            assert bool((b.o[row] == 0).all()) and bool((b.lse[:, row] == -math.inf).all())
