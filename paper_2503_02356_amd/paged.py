@@ -109,13 +109,21 @@ class PagedCache:
 
 def plan_forward(plan, cache, inputs, scale=None):
     """Forward passes of a plan's chunks over a cache, in the order of section 4.2 (a group's chunks ascending); a group's sequences leave
-    the cache behind its last chunk.  inputs(chunk) -> q [T,Hq,D], k, v [T,Hkv,D] of the chunk's tokens on the device.  Yields
-    (chunk, o, lse)."""
+    the cache behind its last chunk, or where the passes end before it.  inputs(chunk) -> q [T,Hq,D], k, v [T,Hkv,D] of the chunk's tokens on the
+    device.  Yields (chunk, o, lse).  The cache may hold other sequences, under any names: they stay as they are (the plan's have names that
+    nobody else has)."""
+    run = object()
     for g in range(plan.n_groups):
-        for c in plan.group(g):
-            segs = plan.chunk_segments(int(c))
-            q, k, v = inputs(int(c))
-            lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-            yield int(c), cache.attend([sid for sid, _, _ in segs], [n for _, _, n in segs], q, k, v, scale, lse), lse
-        for name in list(cache.seqs):
-            cache.close(name)
+        names = {}                                   # of the group, in the order of their beginnings
+        try:
+            for c in plan.group(g):
+                segs = plan.chunk_segments(int(c))
+                q, k, v = inputs(int(c))
+                lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+                own = [(run, sid) for sid, _, _ in segs]
+                names.update(dict.fromkeys(own))
+                yield int(c), cache.attend(own, [n for _, _, n in segs], q, k, v, scale, lse), lse
+        finally:
+            for name in names:
+                if name in cache.seqs:
+                    cache.close(name)
