@@ -540,6 +540,28 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
                 }
         }
         // Each operand is made right before its use (all four at once: 4 registers too many); D = 64 splits it in three.
+        // (Windowed, D = 64: one of the three after the other, for 8 registers less, as many fragments in the ring as it takes.)
+        if constexpr (LIST && D == 64) {
+            static_assert(RING == DB, "the fragments of an operand");
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float f[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = value(g / 2, (8 * (g % 2) + e) % NS, 0);
+#pragma unroll
+                for (int t = 0; t < 3; ++t) {
+                    const bf16x8 w = split_off(f);
+#pragma unroll
+                    for (int j = 0; j < DB; ++j) {
+                        const int n = 2 * ROWS + g * DB + j;
+                        accumulate_in_place<D>(g / 2 ? dk[j] : dv[j], ring[n % RING], w);
+                        if (t == 2) fetch(n + RING);
+                    }
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            return;
+        }
         bf16x8 w, ws[3];
 #pragma unroll
         for (int m = 0; m < 2 * COLS; ++m) {
@@ -551,10 +573,10 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
                     float f[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f[e] = value(x, (8 * (g % 2) + e) % NS, 0);
-                    split<LIST ? 2 : 3>(f, ws);
+                    split_exact(f, ws);
                 }
 #pragma unroll
-                for (int t = 0; t < (LIST ? 2 : 3); ++t) accumulate_in_place<D>(x ? dk[j] : dv[j], ring[n % RING], ws[t]);
+                for (int t = 0; t < 3; ++t) accumulate_in_place<D>(x ? dk[j] : dv[j], ring[n % RING], ws[t]);
             } else {
                 accumulate_in_place<D>(x ? dk[j] : dv[j], ring[n % RING], w);
             }
@@ -716,7 +738,7 @@ __global__ __launch_bounds__(256, 2) void mfma_dkv_kernel(BwdArgs b, const float
 
 // One call with a window: the keys that some row sees, by a work list at either head_dim.  D = 64: with two fragments in flight it fits the
 // registers of three workgroups to a compute unit (16/4 heads, forward and backward, us, with four and two workgroups / so: 4096 packed around 300,
-// window 128 76.0 / 75.5, 4096 behind 5000, window 1000 179.9 / 175.3, 16384, window 512 305.5 / 301.6).  28/4 heads, D = 128: 8192 rows behind 24576 keys, window
+// window 128 79.6 / 78.6, 4096 behind 5000, window 1000 195.0 / 181.7, 16384, window 512 333.2 / 328.3).  28/4 heads, D = 128: 8192 rows behind 24576 keys, window
 // 4096 910-1000 us (1.0 PFLOP/s); packed around 600, window 512 155 us, where the longest slot has 1.4 averages of pairs and an item's 128 KB
 // of atomic adds count (an only writer's rows added with loads and stores instead: 333 us a step against 336, no gain).
 template <int D>

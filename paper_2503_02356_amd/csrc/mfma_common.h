@@ -128,9 +128,23 @@ __device__ __forceinline__ void split_exact(const float (&f)[8], bf16x8 (&w)[3])
     for (int t = 0; t < 3; ++t) w[t] = __builtin_bit_cast(bf16x8, u[t]);
 }
 
-// Windowed calls take two operands: eight bits taken off by truncation, the rounding of the rest, 2^-16 of the value left over (far below
-// what the results' own bf16 leaves of O and dQ; dK and dV are off by as much).  16/4 heads, 4096 tokens packed around 300, window 128, forward and
-// backward: with three 83 us, with two 75; 16384 rows, window 512 362 and 306.
+// The upper eight bits of eight values as an operand; what is left stays.
+__device__ __forceinline__ bf16x8 split_off(float (&f)[8])
+{
+    i32x4 u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const unsigned b0 = __float_as_uint(f[2 * e]), b1 = __float_as_uint(f[2 * e + 1]);
+        u[e] = __builtin_amdgcn_perm(b1, b0, 0x07060302);
+        f[2 * e] -= __uint_as_float(b0 & 0xffff0000u);
+        f[2 * e + 1] -= __uint_as_float(b1 & 0xffff0000u);
+    }
+    return __builtin_bit_cast(bf16x8, u);
+}
+
+// Windowed forward and dQ take two operands: eight bits taken off by truncation, the rounding of the rest, 2^-16 of the value left over, far
+// below what the results' own bf16 leaves (errors of O and dQ, 100 rows of 64: 1.57e-3 and 1.66e-3 with two as with three).  dK and dV leave in
+// fp32 and take three, of any mask (with two 5e-6 instead of 2.5e-7).
 template <int WORDS>
 __device__ __forceinline__ void split(const float (&f)[8], bf16x8 (&w)[3])
 {
