@@ -14,7 +14,11 @@
 // Pages: 16 consecutive keys lie in one page (a page holds a multiple of 16), so that each copy instruction (512 / D rows of a tile) has one
 // base, found with scalar instructions from a table entry that was loaded a tile ahead.  Keys that are hidden as a whole group (no such page,
 // or behind the last key) are copied from a row of zeros, never from the pages, and masked.
-// P enters the second product as bf16 (half a step, 2^-8 of the value, as o itself is rounded; its sum is taken before that).
+// P's sum is taken in fp32.  Into the second product P goes as bf16 with, where rows are few, the bf16 rounding of what that rounding leaves (2^-16 of
+// the value is left over): the wavefronts wait for memory and have the time (64 tokens behind up to 16384 keys 440.6 us without, 441.2 with; o's error
+// against 64 bits 2.2e-3 without, 1.6e-3 with, which is o's own rounding).  Where rows are many it is one operand (half a step, 2^-8 of the value,
+// as o itself is rounded), as cf_attn_fwd has it at head_dim 128: a second one is half of the products again (8192 rows behind 24576 keys 2883 us,
+// with it 4044; o's error 2.3e-3 and 1.7e-3).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -118,9 +122,8 @@ __device__ __forceinline__ void row_again(const PagedArgs &a, const TileRows &t,
 }
 
 // One block of KB x 16 keys, for QB x 16 rows: scores of a K tile, masks, the running softmax, P.
-// RESIDUAL: P enters the second product with the bf16 rounding of what its own rounding leaves (16 bits and more), as a chunk's kernels have
-// it at head_dim 64 and for a sequence's first rows; the wavefronts of few rows have time for it.
-template <int D, int KB, int QB, bool RESIDUAL = false>
+// RESIDUAL: P enters the second product with the bf16 rounding of what its own rounding leaves (16 bits and more).
+template <int D, int KB, int QB, bool RESIDUAL>
 struct Rows {
     static constexpr int KS = D / F::K, DB = D / 16, NS = KB * F::R;
     bf16x8 q[QB][KS];
@@ -316,7 +319,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs &a, const TileRows &t,
     issue(tiles.start(first), stage_a);
     if (first + 1 < end) find_pages(tiles.start(first + 1), pages);
 
-    Rows<D, BN / 16, 2> r;
+    Rows<D, BN / 16, 2, false> r;
     r.clear();
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {
@@ -437,7 +440,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, 
         issue(src.k, start_of(u), pages, k_tile);
         issue(src.v, start_of(u), pages, v_tile);
     }
-    Rows<D, FEW / 16, QB, CHUNK> r;
+    Rows<D, FEW / 16, QB, true> r;
     r.clear();
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {

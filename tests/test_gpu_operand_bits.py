@@ -4,6 +4,7 @@ import torch
 
 from paper_2503_02356_amd import binding as B
 from tests import plain_window as W
+from tests.test_gpu_paged import Batch
 from tests.test_gpu_window import HUGE, Chunk
 
 pytestmark = pytest.mark.gpu
@@ -24,3 +25,20 @@ def test_windowed_gradients_at_head_dim_64(segs, window, sinks, names, flags):
         off = float((got[name].double() - ref[name]).norm() / ref[name].norm())
         print(name, off)
         assert off < 20 * 2.0 ** -24, (name, off)
+
+
+def check_rounding_of_o_alone(b, got, rows, what):
+    """o is off by its own rounding and by what two bf16 operands leave of P: half a step of half a step, 2^-16 of sum P |v|."""
+    ref = b.reference()
+    tol = W.tolerances(ref, BF16, b.D, False)["o"] + 2.0 ** -16 * ref["o_abs"]
+    W.check(dict(o=got["o"][rows]), dict(o=ref["o"][rows]), dict(o=tol[rows]), what)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (900, 20)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_paged_tiles_of_few_rows(D, page, window, sinks):
+    b = Batch([(1, 5000), (2, 300), (1, 64), (8, 700)], 8, 2, D, BF16, page, window, sinks, seed=40)
+    check_rounding_of_o_alone(b, b.run(max_kv_len=5000), slice(0, 12), "tokens")
+    b = Batch([(1, 2000)] * 6 + [(300, 900)], 8, 2, D, BF16, page, window, sinks, seed=41)
+    check_rounding_of_o_alone(b, b.run(), slice(0, 6), "tokens beside a chunk")
