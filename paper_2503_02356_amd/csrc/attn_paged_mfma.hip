@@ -16,9 +16,10 @@
 // or behind the last key) are copied from a row of zeros, never from the pages, and masked.
 // P's sum is taken in fp32.  Into the second product P goes as bf16 with, where rows are few, the bf16 rounding of what that rounding leaves (2^-16 of
 // the value is left over): the wavefronts wait for memory and have the time (64 tokens behind up to 16384 keys 440.6 us without, 441.2 with; o's error
-// against 64 bits 2.2e-3 without, 1.6e-3 with, which is o's own rounding).  Where rows are many it is one operand (half a step, 2^-8 of the value,
-// as o itself is rounded), as cf_attn_fwd has it at head_dim 128: a second one is half of the products again (8192 rows behind 24576 keys 2883 us,
-// with it 4044; o's error 2.3e-3 and 1.7e-3).
+// against 64 bits 2.2e-3 without, 1.6e-3 with, which is o's own rounding).  Where rows are many it is as in cf_attn_fwd, so that evaluating over pages is
+// what training computed: at head_dim 64 P keeps its bits (two operands leave 1.66e-3 in o, cf_attn_fwd's three 1.6e-3, one 2.3e-3; 8192 rows behind
+// 24576 keys, 16/4 heads 1061 us with one, 1495 with two), at head_dim 128 it is one operand (half a step, 2^-8 of the value, as o itself
+// is rounded; 8192 rows behind 24576 keys 2883 us, with two 4044; o's error 2.3e-3 and 1.7e-3).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -319,7 +320,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs &a, const TileRows &t,
     issue(tiles.start(first), stage_a);
     if (first + 1 < end) find_pages(tiles.start(first + 1), pages);
 
-    Rows<D, BN / 16, 2, false> r;
+    Rows<D, BN / 16, 2, D == 64> r;
     r.clear();
 #pragma unroll
     for (int qb = 0; qb < 2; ++qb) {

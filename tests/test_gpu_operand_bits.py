@@ -42,3 +42,12 @@ def test_paged_tiles_of_few_rows(D, page, window, sinks):
     check_rounding_of_o_alone(b, b.run(max_kv_len=5000), slice(0, 12), "tokens")
     b = Batch([(1, 2000)] * 6 + [(300, 900)], 8, 2, D, BF16, page, window, sinks, seed=41)
     check_rounding_of_o_alone(b, b.run(), slice(0, 6), "tokens beside a chunk")
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (900, 20)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_paged_tiles_of_many_rows_at_head_dim_64(page, window, sinks):
+    """As cf_attn_fwd, which takes P whole there."""
+    for seqs in ([(700, 1500)], [(1, 2000)] * 6 + [(300, 900)], [(40, 3000)], [(1, 60), (400, 400), (130, 900)]):
+        b = Batch(seqs, 8, 2, 64, BF16, page, window, sinks, seed=42)
+        check_rounding_of_o_alone(b, b.run(), slice(None), seqs)
