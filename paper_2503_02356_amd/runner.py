@@ -184,10 +184,11 @@ class ChunkAttention:
             ws_bytes = max(ws_bytes, self.attn.bwd_workspace_bytes(ch["fwd"]))
             self.chunks.append(ch)
         # Calls in flight together need a backward workspace each: one per stream, and on a single stream as many in turn
-        # as backward calls share a launch.
+        # as backward calls share a launch (windowed calls share none).
+        together = 1 if self.attn.window is not None else calls_together(ws_bytes)
         self.workspaces = [torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
                            for _ in range(0 if self.fused_launch else self.n_streams if self.n_streams > 1 else
-                                          min(calls_together(ws_bytes), len(self.chunks)))]
+                                          min(together, len(self.chunks)))]
         self.streams = [torch.cuda.Stream(device=dev) for _ in range(self.n_streams)] if self.n_streams > 1 else []
         # groups go, in plan order, to the stream with the least work so far (work = unmasked pairs)
         load, lane_of = [0] * self.n_streams, {}
