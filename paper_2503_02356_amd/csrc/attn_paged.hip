@@ -129,19 +129,22 @@ __global__ __launch_bounds__(256) void kv_append_kernel(cf_kv_append_params p, i
     const int bytes = p.dtype == CF_BF16 ? 2 : 4, per_row = units * p.n_kv_heads;      // units: 16-byte pieces of a head's row
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t row = id / per_row;
-    if (row >= min(p.n_tokens, p.cu_seqlens_q[p.n_seqs])) return;
     const int rest = (int)(id - row * per_row), h = rest / units, unit = rest - h * units;
-    // The sequence of the wavefront's first row, 64 bounds at a time; the others' are that or one of the next.
-    const int lane = threadIdx.x & 63, first = __builtin_amdgcn_readfirstlane((int)row);
+    // The sequence of the wavefront's first row, 64 bounds at a time, by all lanes, those behind the last row too (one that has left has no bound to
+    // compare).  The others' are that or one of the next, or lie behind a run of empty ones: looked for at twice the distance each time.
+    const int lane = threadIdx.x & 63, end = min(p.n_tokens, p.cu_seqlens_q[p.n_seqs]), first = __builtin_amdgcn_readfirstlane((int)row);
+    if (first >= end) return;
     int lo = 0, hi = p.n_seqs;
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) / 64, g = lo + lane * step;
         const unsigned long long before = __ballot(g < hi && p.cu_seqlens_q[min(g, hi - 1)] <= first);
-        lo += (63 - __clzll((long long)before)) * step;      // (lane 0 is in it, and always says yes)
+        lo += (63 - __clzll((long long)before)) * step;      // (lane 0 always says yes)
         hi = min(hi, lo + step);
     }
-    int seq = lo;
-    while (p.cu_seqlens_q[seq + 1] <= row) ++seq;
+    if (row >= end) return;
+    int far = 1;
+    while (far < p.n_seqs - lo && p.cu_seqlens_q[lo + far] <= row) far *= 2;
+    const int near = lo + far / 2, seq = near + find_segment(p.cu_seqlens_q + near, min(far, p.n_seqs - lo) - far / 2, (int)row);
     const NewRows rows(p.cu_seqlens_q[seq], p.cu_seqlens_q[seq + 1], p.kv_lens[seq]);
     const PageTable table{p.block_table + (int64_t)seq * p.table_stride, p.pages_per_seq, shift, p.n_pages};
     const int position = rows.position((int)row - rows.q0), page = table.page_of(position);
