@@ -3,7 +3,8 @@
 Memory placement and descriptors only -- every arithmetic step runs inside cf_attn_paged_fwd, every copy inside cf_kv_append.
 The runner's state buffers hold a split sequence's keys and values in one contiguous piece of its full length, for as long as gradients
 are to be added to it.  Forward passes alone need no such piece: here a sequence takes pages from a pool as it grows, in any order, gives them
-back when it is done, and with a window those that no later query sees, so that a window bounds what a sequence of any length holds.
+back when it is done, and with a window those that no later query sees, so that a window bounds the pages that a sequence of any length holds.  (Its
+row of the table, 4 bytes a page, stays as long as the sequence, and goes to the GPU with every call.)
 """
 import numpy as np
 import torch
@@ -52,13 +53,16 @@ class PagedCache:
         self.peak_pages = max(self.peak_pages, self.used_pages())
 
     def _give_back(self, names):
+        kept = -(-self.n_sinks // self.page_size)    # columns with sinks
         for name in names:
             length, pages = self.seqs[name]
             first = length - self.window + 1         # the first key that the next token's window holds
-            for c in range(min(len(pages), max(0, first) // self.page_size)):
-                if pages[c] >= 0 and c * self.page_size >= self.n_sinks:
-                    self.free.append(pages[c])
-                    pages[c] = -1
+            begin = end = min(len(pages), max(0, first) // self.page_size)
+            while begin > kept and pages[begin - 1] >= 0:        # (those before it have been given back)
+                begin -= 1
+            for c in range(begin, end):
+                self.free.append(pages[c])
+                pages[c] = -1
 
     def attend(self, names, counts, q, k, v, scale=None, lse=None):
         """counts[i] new tokens of sequence names[i] (new names begin a sequence), their rows one behind the other in q [T,Hq,D] and k, v
