@@ -34,7 +34,7 @@ __global__ __launch_bounds__(W * 64, 4) void f32_paged_kernel(PagedArgs a)
     const int part = id % a.parts;
     if (!find_tile<RB>(a, id / a.parts, t)) return;
     const int lowest = t.position(0), highest = t.position(t.rows - 1);
-    const int keys = at_most(highest + 1, a.p.pages_per_seq << a.shift);
+    const int keys = keys_within(highest, a.p.pages_per_seq, a.shift);
     const KeyTiles<RB, WindowMask> blocks(a.mask, lowest, keys);
     const int n = at_least(0, blocks.n), first = at_most(n, a.parts > 1 ? part * a.tiles_per_part : 0);
     const int end = a.parts > 1 && part + 1 < a.parts ? at_most(n, first + a.tiles_per_part) : n;
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(W * 64, 4) void f32_paged_kernel(PagedArgs a)
         const int k0 = blocks.start(b), page = src.page_of(k0);
         if (page < 0) continue;
         const int64_t at = src.offset(page, k0);
-        const int last = at_most(RB - 1, src.last - k0);
+        const int last = at_most(RB - 1, src.room(k0));
         f32x4 kf[S::J], x[4][S::NC];
         load_row<D>((const float *)(src.k + at + (int64_t)at_most(col, last) * src.row_bytes), quarter, kf);
         if (D == 64) load_columns<D>((const float *)(src.v + at), src.row_bytes, last, lane, x);
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(W * 64, 4) void f32_paged_kernel(PagedArgs a)
     });
 }
 
-int64_t groups_most(const cf_attn_paged_params &p) { return ((int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads) / RB + p.n_seqs) * p.n_kv_heads; }
+int64_t groups_most(const cf_attn_paged_params &p) { return places_most(p.n_tokens, p.n_seqs, p.n_q_heads / p.n_kv_heads, RB) * p.n_kv_heads; }
 
 }  // namespace
 

@@ -308,7 +308,7 @@ __device__ __forceinline__ void many_rows(const PagedArgs &a, const TileRows &t,
             for (int g = 0; g < 4; ++g) {
                 const int key = start + 16 * g, page = src.page_of(key);
                 const int64_t at = page < 0 ? 0 : src.offset(page, key);
-                const int room = page < 0 ? 0 : src.last - key;
+                const int room = page < 0 ? 0 : src.room(key);
                 hidden |= (unsigned)(page < 0) << g;
                 if (D == 64 && (wave >> 1) != (g & 1)) continue;
                 group_dma.issue(page < 0 ? (const char *)zeros : src.k + at, room, stage + g * GROUP);
@@ -413,13 +413,13 @@ __device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, 
     // (the same number of copies whatever the pages are: they are counted)
     auto issue = [&](const char *base, int start, const int (&p)[2], char *tile) {
         if constexpr (WHOLE) {
-            const bool none = !src.is_page(p[0]) || start > src.last;
-            dma.issue(uniform(none ? (const char *)zeros : base + src.offset(p[0], start)), none ? 0 : src.last - start, tile);
+            const bool none = src.none(p[0], start);
+            dma.issue(uniform(none ? (const char *)zeros : base + src.offset(p[0], start)), none ? 0 : src.room(start), tile);
         } else {
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
-                const bool none = !src.is_page(p[g]) || start + 16 * g > src.last;
-                half_dma.issue(uniform(none ? (const char *)zeros : base + src.offset(p[g], start + 16 * g)), none ? 0 : src.last - start - 16 * g,
+                const bool none = src.none(p[g], start + 16 * g);
+                half_dma.issue(uniform(none ? (const char *)zeros : base + src.offset(p[g], start + 16 * g)), none ? 0 : src.room(start + 16 * g),
                                tile + g * (16 * 2 * D));
             }
         }
@@ -458,7 +458,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs &a, const TileRows &t, 
         const int start = start_of(u), next = u + 4;
         const bool more = next < blocks;
         // (keys behind the last one are those of later rows, or behind the table's last column, where groups end)
-        const unsigned hidden = (unsigned)(!src.is_page(pages[0]) || start > src.last) | (unsigned)(!src.is_page(pages[1]) || start + 16 > src.last) << 1;
+        const unsigned hidden = (unsigned)src.none(pages[0], start) | (unsigned)src.none(pages[1], start + 16) << 1;
         if (more) find_pages(start_of(next), next_pages);
         f32x4 s[FEW / 16][QB];
         wait_older();                                // K is there
@@ -560,7 +560,7 @@ __global__ __launch_bounds__(256, 2) void mfma_paged_kernel(PagedArgs a)
     constexpr bool CHUNK = MODE == kChunk || MODE == kChunkHalf;
     if (!find_tile<MODE == kChunkHalf ? FEW / 2 : MODE == kFew || MODE == kChunk ? FEW : BM, CHUNK>(a, id / a.parts, t)) return;
     const int lowest = t.position(0), highest = t.position(t.rows - 1);
-    const int keys = CHUNK ? highest + 1 : at_most(highest + 1, a.p.pages_per_seq << a.shift);
+    const int keys = CHUNK ? highest + 1 : keys_within(highest, a.p.pages_per_seq, a.shift);
     const KeyTiles<BN, WindowMask> tiles(a.mask, lowest, keys);
     // (BOTH: tiles of many rows are cut a third as often, for a part of them leaves four times as much to be joined)
     const int thirds = MODE == kBoth && t.rows > FEW ? 3 : 1, per_part = a.tiles_per_part * thirds, last_part = (a.parts - 1) / thirds;
@@ -593,7 +593,7 @@ Mode mode_of(const cf_attn_paged_params &p)
 }
 int64_t tiles_most(const cf_attn_paged_params &p)
 {
-    return (int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads) / (mode_of(p) == kFew ? FEW : BM) + p.n_seqs;
+    return places_most(p.n_tokens, p.n_seqs, p.n_q_heads / p.n_kv_heads, mode_of(p) == kFew ? FEW : BM);
 }
 
 }  // namespace
