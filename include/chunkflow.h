@@ -344,7 +344,7 @@ int cf_attn_calls(const cf_attn_call *calls, int64_t n, void *hip_stream);
  * The same attention with a sliding window and sinks: query i of a segment, at position p = i + (Lk_g - Lq_g), sees key j iff
  * j <= p and (j > p - window or j < n_sinks): its last `window` keys, itself among them, and the segment's first n_sinks keys.  A
  * window of Lk_g or more is no window.  Positions are those of the whole sequence, as with the causal mask, so a slice behind a
- * retained prefix reads of it what its rows see and leaves the rest of k, v, d_k and d_v untouched.
+ * retained prefix needs of it what its rows see: the rest of k and v is in no result, and the rest of d_k and d_v stays as it is.
  *   window   >= 1        n_sinks  >= 0
  * cf_attn_window_fwd / cf_attn_window_bwd take the arguments of cf_attn_fwd / cf_attn_bwd (layouts, flags, q_tiles, dK/dV that are added
  * to) and give their results and errors; window < 1, n_sinks < 0 or a NULL window -> CF_EINVAL.  Workspace: at least
@@ -373,10 +373,12 @@ int64_t cf_count_window_pairs(const int32_t *cu_seqlens_q_host, const int32_t *c
  *   Query row i of sequence g has position p = kv_lens[g] - Lq_g + i and sees the keys j <= p; with window > 0 of these only
  *   j > p - window or j < n_sinks (as in cf_attn_window_fwd; window 0: n_sinks must be 0).
  *   A page number outside [0, n_pages) is no page: its keys are hidden (pages that a window has left behind can be given back and
- *   marked -1), and so are keys behind the table's last column.  A row that sees no key has o = 0 and lse = -infinity.
+ *   marked -1), and so are keys behind the table's last column.  A row that sees no key, or none whose score is above -infinity, has
+ *   o = 0 and lse = -infinity.
  *   Sequences may be empty (Lq_g = 0).  Rows of q and o from cu_seqlens_q[n_seqs] on (a padded batch) are neither read nor written.
- * Key and value rows that no row of a call sees are not read, whatever stands there (the rest of a page may be uninitialised).
- * Infinities and NaNs in a key or value reach only the rows that see it.  Results are bitwise reproducible.
+ * What stands in key and value rows that no row of a call sees is in no result.  Rows behind a sequence's last key (the rest of a page) and
+ * those of no page are not read at all; others may be read together with rows that are seen.
+ * Infinities and NaNs in a query reach its row and head, in a key or a value the rows that see it, and no others.  Results are bitwise reproducible.
  * cu_seqlens_q is NOT validated (as in cf_attn_fwd); kv_lens and block_table may hold anything: no access leaves the pages.
  * max_kv_len is the longest kv_lens that the caller expects (0: as many as the table's columns hold); it decides how the work is cut, not
  * what is computed.  Long caches with few rows are cut along the keys; the parts are joined through the workspace, at least

@@ -486,7 +486,7 @@ __device__ __forceinline__ void dkv_body(const BwdArgs &b, const float *__restri
 #pragma unroll
                 for (int kb = 0; kb < N; ++kb) {
                     const int key = kw0 + F::M * kb + lane_ % F::M;
-                    const int far = key < mask.sinks ? 64 : key + mask.window - off - q0 - lane_ / F::M * 4;     // rows from here on do not see it
+                    const int far = key < mask.sinks ? 64 : mask.window - (off + q0 - key) - lane_ / F::M * 4;     // rows from here on do not see it
 #pragma unroll
                     for (int i = 0; i < NS; ++i) s[i / F::R][kb][i % F::R] = F::place(i) >= far ? 0.f : s[i / F::R][kb][i % F::R];
                 }

@@ -5,11 +5,11 @@
 // transposed as in attn_mfma_fwd.hip: S^T = K Q^T, O^T += V^T P^T, the row on the lane axis) takes a tile and a part of its keys:
 //   many rows  (more than 32)  a wavefront has 32 rows; key tiles of 64 are shared through LDS, double buffered.  Bound by the MFMAs and
 //              the arithmetic between them, like the forward kernel of a chunk (8192 rows behind 24576 keys, 28/4 heads, D = 128: 2.96 ms,
-//              1137 TFLOP/s; that kernel on contiguous keys 2.93).
+//              1137 TFLOP/s; that kernel on contiguous keys 2.85).
 //   few rows   every wavefront has all of them and takes every fourth block of 32 keys, copied into its own part of LDS: it waits for
 //              nobody.  Bound by the memory that holds the cache: 16 KB of keys and values a wavefront, 8 wavefronts a compute unit, are in
 //              flight or in use.  The four results meet in LDS at the end.  (64 tokens behind up to 16384 keys, 32/8 heads, D = 128, pages of 64:
-//              2.43 GB in 439 us, 5.5 TB/s; 256 with a window of 1024, 16/4, D = 64, pages of 32: 58 us, 4.7 TB/s.)
+//              2.43 GB in 441 us, 5.5 TB/s; 256 with a window of 1024, 16/4, D = 64, pages of 32: 58 us, 4.7 TB/s.)
 // A long cache with few tiles is cut into parts, joined by a kernel behind this one (attn_paged.hip).
 // Pages: 16 consecutive keys lie in one page (a page holds a multiple of 16), so that each copy instruction (512 / D rows of a tile) has one
 // base, found with scalar instructions from a table entry that was loaded a tile ahead.  Keys that are hidden as a whole group (no such page,
@@ -18,7 +18,7 @@
 // the value is left over): the wavefronts wait for memory and have the time (64 tokens behind up to 16384 keys 440.6 us without, 441.2 with; o's error
 // against 64 bits 2.2e-3 without, 1.6e-3 with, which is o's own rounding).  Where rows are many it is as in cf_attn_fwd, so that evaluating over pages is
 // what training computed: at head_dim 64 P keeps its bits (two operands leave 1.66e-3 in o, cf_attn_fwd's three 1.6e-3, one 2.3e-3; 8192 rows behind
-// 24576 keys, 16/4 heads 1061 us with one, 1495 with two), at head_dim 128 it is one operand (half a step, 2^-8 of the value, as o itself
+// 24576 keys, 16/4 heads 1061 us with one, 1495 with two; cf_attn_fwd 1845), at head_dim 128 it is one operand (half a step, 2^-8 of the value, as o itself
 // is rounded; 8192 rows behind 24576 keys 2883 us, with two 4044; o's error 2.3e-3 and 1.7e-3).
 #include <hip/hip_runtime.h>
 
@@ -585,7 +585,10 @@ __global__ __launch_bounds__(256, 2) void mfma_paged_kernel(PagedArgs a)
 }
 
 // Tiles of single tokens and short runs only, of chunks only, or of both?  By the mean number of token-head rows of a sequence; every kernel
-// takes any of them.
+// takes any of them.  From how many on a call goes as chunks only, 256 / 512 / 1024 rows, us, 28/4 heads, D = 128: 40 tokens behind up to 4000 keys
+// beside a chunk of 4096 301 / 301 / 917, 5 behind up to 8000 beside 700 132 / 132 / 177, 10 behind up to 30000 beside 1000 613 / 613 / 629; 32/8, 16
+// beside four of 500 137 / 146 / 146, 30 beside two of 2048 162 / 520 / 520; 16/4, D = 64, 10 behind up to 9000 beside 2000 157 / 157 / 132.  (A call's
+// mean says little of its sequences: with a few long chunks beside tokens, a call for each kind may be faster than one for both.)
 Mode mode_of(const cf_attn_paged_params &p)
 {
     const int64_t rows = (int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads);
@@ -602,8 +605,15 @@ int64_t paged_mfma_launch_size(const PagedArgs &a) { return tiles_most(a.p) * a.
 
 // Parts: so many that the chip's 512 workgroup slots each get several, of four key tiles at least (two blocks of 32 keys to a wavefront; 32/8
 // heads, us, parts of at least 2 / 4 / 6 tiles: one token behind 2000 keys 10.2 / 10.3 / 11.0, 8192 13.9 / 13.6 / 13.7, 4 behind up to 8192
-// 24.7 / 21.9 / 18.9).  Rounds of slots, tokens: 64 behind up to 16384 keys 486 us with 4, 442 with 5, 459 with 8, 443 with 12; 128 behind up
-// to 2048 138 / 131 / 149 / 141.
+// 24.7 / 21.9 / 18.9).
+// Rounds of slots, us, D = 128 but where it says 64:
+//   tokens, 3 / 4 / 5 / 6 / 8        32/8 heads: 8 behind up to 8000 keys 47.7 / 48.4 / 48.9 / 49.1 / 49.0, 32 up to 16000 214 / 217 / 209 / 210 / 210, 64 up to
+//                                    16384 448 / 484 / 440 / 447 / 457, 128 up to 2000 146 / 146 / 141 / 141 / 156; 16/4, 64, 256 up to 4000 146 / 146 / 117 / 118 / 134
+//   beside chunks, 4 / 6 / 8 / 12    32/8: 40 up to 9000 beside a chunk of 500 185 / 189 / 195 / 207, 100 up to 3000 beside three of 300 235 / 187 / 291 / 217;
+//                                    28/4: 20 up to 20000 beside 1000 290 / 325 / 325 / 393; 64/8: 30 up to 9000 beside 500 527 / 300 / 359 / 317; 16/4, 64: 60 up
+//                                    to 6000 beside two of 400 84 / 97 / 79 / 102.  None is best everywhere.
+// Tiles of many rows beside tokens are cut into as many parts / half / a third / a sixth of them: of the same five calls 218 / 197 / 195 / 184,
+// 247 / 270 / 291 / 301, 355 / 329 / 325 / 319, 340 / 313 / 359 / 518, 86 / 81 / 79 / 136; with few tokens, 28/4, 8 up to 4000 beside 200, 28.6 / 32.5 / 37.6 / 59.4.
 void cut_paged_mfma(PagedArgs &a)
 {
     const cf_attn_paged_params &p = a.p;

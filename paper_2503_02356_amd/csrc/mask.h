@@ -3,7 +3,8 @@
 //   WindowMask  of these the last `window` ones and the first `sinks` ones:  j <= p and (j > p - window or j < sinks)
 // A row's visible keys are the sinks that lie before its window, then one stretch that ends at its position.  Kernels go over tiles of
 // keys, so their lists of tiles have the same two parts.
-// window >= 1 and sinks >= 0 are at most the keys of a call (its entry points see to that), so that no sum here leaves 32 bits.
+// window is from 1 to 2^31 - 1, sinks from 0 to the keys of a call (its entry points see to that).  Sums that could leave 32 bits with fewer than
+// 2^31 - 128 keys have 64 (more keys are 256 GB of keys alone, at one head of 64).
 #pragma once
 #include <stdint.h>
 

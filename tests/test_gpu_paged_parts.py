@@ -136,3 +136,24 @@ def test_rows_without_keys_in_a_cut_call(dtype, D):
         b.check(dict(o=b.o, lse=b.lse), fill)
         for row in (1, 2, 3):
             assert bool((b.o[row] == 0).all()) and bool((b.lse[:, row] == -math.inf).all())
+
+
+@pytest.mark.parametrize("dtype,D", KINDS)
+@pytest.mark.parametrize("flags", [0, B.CF_FLAG_SCALAR_KERNELS])
+def test_scores_that_are_all_minus_infinity(dtype, D, flags):
+    """Zeros, as where there is no key; a single score above it and the row is that key's value."""
+    for seqs in ([(1, 5000), (1, 40)], [(40, 3000), (3, 50)]):
+        b = Batch(seqs, 4, 2, D, dtype, 16, seed=32)
+        b.append()
+        b.q[:, :, 3] = 1.0
+        b.kp[..., 3] = -INF
+        B.cf_attn_paged_fwd(b.params(flags))
+        torch.cuda.synchronize()
+        assert bool((b.o == 0).all()) and bool((b.lse == -INF).all())
+        j = 20                                       # of the second sequence, seen by all of its rows
+        b.kp[int(b.table_host[1, j // 16]), j % 16, :, 3] = 0.0
+        B.cf_attn_paged_fwd(b.params(flags))
+        torch.cuda.synchronize()
+        first = seqs[0][0]
+        assert bool((b.o[:first] == 0).all()) and bool((b.lse[:, :first] == -INF).all())
+        assert bool(torch.equal(b.o[first:], b.keys[1][1][j].repeat_interleave(2, 0).expand(seqs[1][0], -1, -1))) and bool(b.lse[:, first:].isfinite().all())
