@@ -392,7 +392,7 @@ typedef struct {
     int32_t head_dim;                   /* 64 or 128                                             */
     float softmax_scale;                /* finite                                                */
     int32_t n_tokens;                   /* rows of q and o, >= 1; n_tokens * n_q_heads < 2^31    */
-    int32_t n_seqs;                     /* >= 1                                                  */
+    int32_t n_seqs;                     /* 1 .. 2^30                                             */
     const int32_t *cu_seqlens_q;        /* device, [n_seqs+1]                                    */
     const int32_t *kv_lens;             /* device, [n_seqs]                                      */
     const int32_t *block_table;         /* device, [n_seqs][pages_per_seq]                       */

@@ -179,7 +179,8 @@ int check_common(const char *who, int dtype, int D, int n_tokens, int n_seqs, co
 {
     if (dtype != CF_BF16 && dtype != CF_FP32) return fail(CF_EUNSUPPORTED, "%s: dtype %d not supported", who, dtype);
     if (D != 64 && D != 128) return fail(CF_EUNSUPPORTED, "%s: head_dim %d not supported (64 or 128)", who, D);
-    if (n_tokens < 1 || n_seqs < 1) return fail(CF_EINVAL, "%s: need n_tokens >= 1 and n_seqs >= 1 (got %d, %d)", who, n_tokens, n_seqs);
+    if (n_tokens < 1 || n_seqs < 1 || n_seqs > (1 << 30))        // (the kernels' searches add two places or double one)
+        return fail(CF_EINVAL, "%s: need n_tokens >= 1 and 1 <= n_seqs <= 2^30 (got %d, %d)", who, n_tokens, n_seqs);
     if (page_size < 16 || page_size > 65536 || (page_size & (page_size - 1)))
         return fail(CF_EINVAL, "%s: page_size %d must be a power of two from 16 to 65536", who, page_size);
     if (n_pages < 1 || pages < 1 || (int64_t)pages * page_size > (1 << 30) || table_stride < pages)

@@ -16,7 +16,9 @@ class PagedCache:
     """A pool of n_pages pages of page_size tokens and the tables of the sequences that live in it.
 
     window, n_sinks: of every call (0: a query sees all keys before it); pages behind the window of a sequence's next token are given back
-    as soon as the tokens up to it have attended."""
+    as soon as the tokens up to it have attended.
+    A call lays its tables out on the host and copies them: a program that captures its steps into a graph keeps tables of its own and makes the two
+    calls of the binding (cf_kv_append, cf_attn_paged_fwd) itself."""
 
     def __init__(self, n_pages, page_size, n_kv_heads, head_dim, dtype=torch.bfloat16, device="cuda:0", window=0, n_sinks=0):
         self.page_size, self.window, self.n_sinks, self.dev = int(page_size), int(window), int(n_sinks), torch.device(device)
