@@ -292,7 +292,7 @@ def _power(most):
     """The least power of two, from 2^LEAST on, 448 times which is not less than `most`."""
     m, e = torch.frexp(most)                       # most = m 2^e, m from 0.5 on
     e = torch.where(most == 0, LEAST, e - 9 + (m > 0.875).int()).clamp(min=LEAST)
-    return torch.ldexp(torch.ones_like(most), e)
+    return ((e + 127) << 23).view(torch.float32)   # (from its bits: a power function need not be exact)
 
 
 def _plain_append(s):
@@ -474,7 +474,8 @@ def exact(case, seed):
                 lead = b - first * BLOCK
                 values[lead:lead + a] = x[row:row + a]
                 most = values.view(n, BLOCK, Hkv, D).abs().amax((1, 3))
-                power = 2.0 ** torch.ceil(torch.log2(most / 448)).clamp(min=LEAST)
+                e = torch.ceil(torch.log2(most / 448)).clamp(min=LEAST)          # (log2 of 0: LEAST)
+                power = ((e.long() + 1023) << 52).view(torch.float64)
                 power = torch.where(448 * power / 2 >= most, power / 2, torch.where(448 * power < most, power * 2, power)).clamp(min=2.0 ** LEAST)
                 if lead:
                     before = scales[number[0], :, block[0]]
