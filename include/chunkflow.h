@@ -9,7 +9,9 @@
  *      of a long sequence that also attends to the retained key/value state of that sequence's
  *      earlier chunks, the key/value gradients of those earlier rows being accumulated by the
  *      later chunks' backward passes (section 4.2); the same with a sliding window and sinks; and,
- *      forward only, over a paged key/value cache.
+ *      forward only, over a paged key/value cache, of the model's type or of 8 bits; the rotation of
+ *      queries and keys by their positions, for a chunk (and back, for its gradients) and on the way
+ *      into a paged cache.
  *
  * Conventions
  *   - Every function returns CF_OK (0) or a negative error code; nothing throws, aborts or prints.
@@ -433,6 +435,98 @@ typedef struct {
     int64_t page_stride, page_stride_tok, page_stride_head;
 } cf_kv_append_params;
 int cf_kv_append(const cf_kv_append_params *p, void *hip_stream);
+
+/*
+ * Rotation of queries and keys by their positions.  The elements of a head are taken in rot_dim / 2 pairs, pair i being elements
+ * (i, i + rot_dim / 2), or (2 i, 2 i + 1) where interleaved is not 0; those from rot_dim on are in no pair and stay.  At position p pair i = (a, b)
+ * becomes (a cos t - b sin t, a sin t + b cos t), t = p * inv_freq[i].  The angle is taken in 64 bits, so that far positions are as exact as near
+ * ones, sines and products in fp32; results are rounded once.
+ */
+typedef struct {
+    const float *inv_freq;              /* device, [rot_dim/2]: angle of a pair per position, in radians */
+    int32_t rot_dim;                    /* a multiple of 16, 16 .. head_dim                      */
+    int32_t interleaved;
+} cf_rotation;
+
+/*
+ * Queries and keys of one training chunk, and their gradients.  Row i of segment g (rows [cu_seqlens_q[g], cu_seqlens_q[g+1]) of x and y) has
+ * the position that cf_attn_fwd gives it: (Lk_g - Lq_g) + i.  inverse 0: y = the rotated x.  inverse 1: x turned back, which is the gradient of x
+ * where x here is that of y: dQ of a chunk as cf_attn_bwd leaves it, dK of a sequence (cu_seqlens = {0, L} in both lists) once all of its chunks have
+ * been added to it.  Only the new rows of a dependent chunk are rotated: those before them in the state have been.
+ * y may be x (same strides and dtype); otherwise they may not overlap.  Rows from cu_seqlens_q[n_segments] on are neither read nor written.
+ * Infinities and NaNs in x reach the other element of their pair; one in inv_freq, that pair of every row.
+ */
+typedef struct {
+    int32_t n_heads;                    /* 0: no such tensor                                     */
+    int32_t dtype_in, dtype_out;        /* CF_BF16 to CF_BF16, CF_FP32 to either                 */
+    const void *x;                      /* device, [T][n_heads][D]                               */
+    int64_t x_stride_tok, x_stride_head;
+    void *y;                            /* device, [T][n_heads][D], written                      */
+    int64_t y_stride_tok, y_stride_head;
+} cf_rotate_tensor;
+typedef struct {
+    int32_t head_dim;                   /* 64 or 128                                             */
+    int32_t inverse;                    /* 0 or 1                                                */
+    int32_t n_tokens, n_segments;       /* >= 1                                                  */
+    const int32_t *cu_seqlens_q, *cu_seqlens_k;     /* device, [n_segments+1]                    */
+    cf_rotation rotation;
+    cf_rotate_tensor q, k;              /* at least one of them                                  */
+} cf_rotate_params;
+/* Errors: NULL or misaligned pointers (16 bytes; inv_freq and lists 4), sizes and strides out of range (bf16: multiples of 8 elements, fp32: of 4) ->
+ * CF_EINVAL; head_dim / dtypes not built -> CF_EUNSUPPORTED; launch failure -> CF_EHIP. */
+int cf_rotate(const cf_rotate_params *p, void *hip_stream);
+
+/*
+ * cf_kv_append with the rotation on the way: keys go into the pages rotated by their positions, values as they are, and the same rows' queries,
+ * where q is not NULL, into q_out (in place or not, as in cf_rotate).  A row whose key is dropped for its position has its query turned by the
+ * position, a negative one by position 0.  Everything else as in cf_kv_append; q has its dtype.
+ */
+typedef struct {
+    cf_rotation rotation;
+    int32_t n_q_heads, reserved;
+    const void *q;                      /* device, [T][Hq][D], or NULL                           */
+    int64_t q_stride_tok, q_stride_head;
+    void *q_out;                        /* device, [T][Hq][D], written                           */
+    int64_t q_out_stride_tok, q_out_stride_head;
+} cf_append_rotation;
+int cf_kv_append_rotated(const cf_kv_append_params *p, const cf_append_rotation *r, void *hip_stream);
+
+/*
+ * A cache of 8 bits.  Pages as above with one byte an element, an e4m3 number (1 sign bit, 4 exponent bits of bias 7, 3 mantissa bits, no
+ * infinities, NaN 0x7f and 0xff, largest 448), and for every CF_KV8_BLOCK consecutive tokens of a page and every key/value head a power of two that
+ * its numbers are multiplied with: scales [n_pages][Hkv][page_size / CF_KV8_BLOCK] fp32, blocks of a page and head next to each other.  Of a
+ * scale the exponent counts alone (a number that is no power of two counts as the one below, 0 as 2^-127; infinities and NaNs make the block NaN).
+ * A power of two costs nothing next to any other factor, since e4m3 numbers have a fixed number of bits whatever their size, and it multiplies exactly.
+ */
+#define CF_KV8_BLOCK 16
+
+/*
+ * cf_kv_append into a cache of 8 bits, r as in cf_kv_append_rotated or NULL (nothing is rotated).  A block that gets new rows takes the least scale
+ * 2^e, e >= -110, for which none of its new finite elements is above 448 * 2^e, unless older rows stand before the new ones in it: then
+ * the larger of that and the scale it has, and where this grows, the older rows' numbers are rounded to it again.  Elements are rounded to the nearest
+ * number (ties to even), those below 2^-120 may become 0, infinities and NaNs become NaN (and no part of the scale).
+ * Rows behind a block's new ones stay as they are.  Two sequences of a call may not add to the same block.
+ * a.dtype is that of k, v and q; a's pages are bytes, a's page strides are multiples of 16, at least head_dim.
+ */
+typedef struct {
+    cf_kv_append_params a;
+    float *k_scales, *v_scales;         /* device, same strides for both                         */
+    int64_t scale_stride_page, scale_stride_head;   /* >= page_size / CF_KV8_BLOCK               */
+} cf_kv_append8_params;
+int cf_kv_append8(const cf_kv_append8_params *p, const cf_append_rotation *r, void *hip_stream);
+
+/*
+ * cf_attn_paged_fwd over a cache of 8 bits: the same mask, pages, lengths, workspace (cf_attn_paged8_workspace_bytes), results and errors, with keys
+ * and values that are number * scale.  a.dtype is that of q and o; a's pages are bytes, a.page_stride, a.kv_stride_tok and a.kv_stride_head multiples of
+ * 16, at least head_dim.  The numbers enter the products as they are, with the precision that those of a cache of a.dtype have.
+ */
+typedef struct {
+    cf_attn_paged_params a;
+    const float *k_scales, *v_scales;
+    int64_t scale_stride_page, scale_stride_head;
+} cf_attn_paged8_params;
+int64_t cf_attn_paged8_workspace_bytes(const cf_attn_paged8_params *p);
+int cf_attn_paged8_fwd(const cf_attn_paged8_params *p, void *hip_stream);
 
 /*
  * Measurement aid (not part of the paper's method): when both events (hipEvent_t, created by the

@@ -22,7 +22,8 @@ CF_PLAN_MERGE_TAILS = 1
 EXPORTS = ["cf_last_error", "cf_version", "cf_build_chunks", "cf_build_chunks_ex", "cf_attn_q_tiles", "cf_plan_free", "cf_plan_get",
            "cf_build_schedule", "cf_schedule_stats", "cf_attn_fwd", "cf_attn_bwd_workspace_bytes", "cf_attn_bwd", "cf_attn_fwd_batch", "cf_attn_bwd_batch",
            "cf_attn_calls", "cf_attn_window_fwd", "cf_attn_window_bwd", "cf_attn_window_bwd_workspace_bytes", "cf_count_window_pairs",
-           "cf_attn_paged_fwd", "cf_attn_paged_workspace_bytes", "cf_kv_append", "cf_count_pairs", "cf_profile_next_call", "cf_attn_bwd_static", "cf_sim_1f1b", "cf_sim_1f1b_sequences"]
+           "cf_attn_paged_fwd", "cf_attn_paged_workspace_bytes", "cf_kv_append", "cf_rotate", "cf_kv_append_rotated", "cf_kv_append8",
+           "cf_attn_paged8_fwd", "cf_attn_paged8_workspace_bytes", "cf_count_pairs", "cf_profile_next_call", "cf_attn_bwd_static", "cf_sim_1f1b", "cf_sim_1f1b_sequences"]
 
 
 class CfError(RuntimeError):
@@ -105,6 +106,37 @@ class KvAppendParams(C.Structure):
                 ("page_stride_head", C.c_int64)]
 
 
+class Rotation(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32)]
+
+
+class RotateTensor(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("dtype_in", C.c_int32), ("dtype_out", C.c_int32), ("x", C.c_void_p), ("x_stride_tok", C.c_int64),
+                ("x_stride_head", C.c_int64), ("y", C.c_void_p), ("y_stride_tok", C.c_int64), ("y_stride_head", C.c_int64)]
+
+
+class RotateParams(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("inverse", C.c_int32), ("n_tokens", C.c_int32), ("n_segments", C.c_int32), ("cu_seqlens_q", C.c_void_p),
+                ("cu_seqlens_k", C.c_void_p), ("rotation", Rotation), ("q", RotateTensor), ("k", RotateTensor)]
+
+
+class AppendRotation(C.Structure):
+    _fields_ = [("rotation", Rotation), ("n_q_heads", C.c_int32), ("reserved", C.c_int32), ("q", C.c_void_p), ("q_stride_tok", C.c_int64),
+                ("q_stride_head", C.c_int64), ("q_out", C.c_void_p), ("q_out_stride_tok", C.c_int64), ("q_out_stride_head", C.c_int64)]
+
+
+class KvAppend8Params(C.Structure):
+    _fields_ = [("a", KvAppendParams), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p), ("scale_stride_page", C.c_int64),
+                ("scale_stride_head", C.c_int64)]
+
+
+class AttnPaged8Params(C.Structure):
+    _fields_ = [("a", AttnPagedParams), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p), ("scale_stride_page", C.c_int64),
+                ("scale_stride_head", C.c_int64)]
+
+
+CF_KV8_BLOCK = 16
+
 _lib = None
 
 
@@ -138,6 +170,12 @@ def lib():
         L.cf_attn_window_bwd.argtypes = [C.POINTER(AttnBwdParams), C.POINTER(AttnWindow), C.c_void_p]
         L.cf_attn_window_bwd_workspace_bytes.argtypes = [C.POINTER(AttnFwdParams), C.POINTER(AttnWindow)]
         L.cf_attn_window_bwd_workspace_bytes.restype = C.c_int64
+        L.cf_rotate.argtypes = [C.POINTER(RotateParams), C.c_void_p]
+        L.cf_kv_append_rotated.argtypes = [C.POINTER(KvAppendParams), C.POINTER(AppendRotation), C.c_void_p]
+        L.cf_kv_append8.argtypes = [C.POINTER(KvAppend8Params), C.POINTER(AppendRotation), C.c_void_p]
+        L.cf_attn_paged8_fwd.argtypes = [C.POINTER(AttnPaged8Params), C.c_void_p]
+        L.cf_attn_paged8_workspace_bytes.argtypes = [C.POINTER(AttnPaged8Params)]
+        L.cf_attn_paged8_workspace_bytes.restype = C.c_int64
         L.cf_count_window_pairs.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(AttnWindow)]
         L.cf_count_window_pairs.restype = C.c_int64
         L.cf_attn_paged_workspace_bytes.argtypes = [C.POINTER(AttnPagedParams)]
@@ -416,7 +454,7 @@ def _stream_for(params, stream):
         return stream
     import torch
     t = params._keepalive[0] if hasattr(params, "_keepalive") else None
-    t = t._keepalive[0] if isinstance(t, AttnFwdParams) else t
+    t = t._keepalive[0] if isinstance(t, C.Structure) else t
     if t is not None and t.device.index != torch.cuda.current_device():
         raise ValueError(f"the tensors are on cuda:{t.device.index}, the current device is cuda:{torch.cuda.current_device()}")
     return _stream()
@@ -482,13 +520,21 @@ def make_paged_params(q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, s
     """q, o [T,Hq,D]; k_pages, v_pages [n_pages,page_size,Hkv,D]; lse [Hq,T] fp32 or None; cu_q [n_seqs+1], kv_lens [n_seqs], block_table
     [n_seqs,pages] int32 device tensors.  workspace: uint8 device tensor, or None: one of the size that the call needs is made here and
     kept with the parameters."""
+    assert q.dtype == k_pages.dtype == v_pages.dtype
+    p = AttnPagedParams()
+    _fill_paged(p, q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, scale, max_kv_len, window, n_sinks, flags, workspace)
+    workspace = _paged_workspace(p, cf_attn_paged_workspace_bytes, p, q, workspace)
+    p._keepalive = (q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, workspace)      # see make_fwd_params
+    return p
+
+
+def _fill_paged(p, q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, scale, max_kv_len, window, n_sinks, flags, workspace):
     import torch
     T, Hq, D = q.shape
     _check_paged(cu_q, kv_lens, block_table, k_pages, v_pages, q, o, *(t for t in (lse, workspace) if t is not None))
-    assert q.is_cuda and q.stride(2) == 1 and o.stride(2) == 1 and q.dtype == k_pages.dtype == v_pages.dtype == o.dtype
+    assert q.is_cuda and q.stride(2) == 1 and o.stride(2) == 1 and q.dtype == o.dtype
     assert o.shape == q.shape and k_pages.shape[3] == D
     assert lse is None or (lse.is_contiguous() and tuple(lse.shape) == (Hq, T) and lse.dtype == torch.float32)
-    p = AttnPagedParams()
     p.dtype, p.flags, p.n_q_heads, p.n_kv_heads, p.head_dim = _dtype_code(q), int(flags), Hq, k_pages.shape[2], D
     p.softmax_scale, p.n_tokens, p.n_seqs = float(scale), T, kv_lens.numel()
     p.cu_seqlens_q, p.kv_lens, p.block_table = cu_q.data_ptr(), kv_lens.data_ptr(), block_table.data_ptr()
@@ -500,14 +546,17 @@ def make_paged_params(q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, s
     p.page_stride, p.kv_stride_tok, p.kv_stride_head = k_pages.stride(0), k_pages.stride(1), k_pages.stride(2)
     p.o, p.o_stride_tok, p.o_stride_head = o.data_ptr(), o.stride(0), o.stride(1)
     p.lse = lse.data_ptr() if lse is not None else None
+
+
+def _paged_workspace(p, bytes_needed, params, q, workspace):
+    import torch
     if workspace is None:
-        need = cf_attn_paged_workspace_bytes(p)
+        need = bytes_needed(params)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     if workspace is not None:
         assert workspace.is_contiguous()
         p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    p._keepalive = (q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, workspace)      # see make_fwd_params
-    return p
+    return workspace
 
 
 def cf_attn_paged_workspace_bytes(params):
@@ -520,10 +569,17 @@ def cf_attn_paged_fwd(params, stream=None):
 
 def make_kv_append_params(k, v, k_pages, v_pages, cu_q, kv_lens, block_table):
     """k, v [T,Hkv,D] (views with the same strides); the rest as in make_paged_params."""
+    assert k.dtype == k_pages.dtype == v_pages.dtype
+    p = KvAppendParams()
+    _fill_append(p, k, v, k_pages, v_pages, cu_q, kv_lens, block_table)
+    p._keepalive = (k, v, k_pages, v_pages, cu_q, kv_lens, block_table)      # see make_fwd_params
+    return p
+
+
+def _fill_append(p, k, v, k_pages, v_pages, cu_q, kv_lens, block_table):
     _check_paged(cu_q, kv_lens, block_table, k_pages, v_pages, k, v)
     assert k.is_cuda and k.stride(2) == 1 and k.stride() == v.stride() and k.shape == v.shape
-    assert k.dtype == v.dtype == k_pages.dtype == v_pages.dtype and tuple(k.shape[1:]) == tuple(k_pages.shape[2:])
-    p = KvAppendParams()
+    assert k.dtype == v.dtype and tuple(k.shape[1:]) == tuple(k_pages.shape[2:])
     p.dtype, p.n_kv_heads, p.head_dim, p.n_tokens, p.n_seqs = _dtype_code(k), k.shape[1], k.shape[2], k.shape[0], kv_lens.numel()
     p.pages_per_seq, p.page_size, p.n_pages = block_table.shape[1], k_pages.shape[1], k_pages.shape[0]
     p.table_stride = block_table.stride(0) if block_table.shape[0] > 1 else block_table.shape[1]
@@ -531,9 +587,131 @@ def make_kv_append_params(k, v, k_pages, v_pages, cu_q, kv_lens, block_table):
     p.k, p.v, p.kv_stride_tok, p.kv_stride_head = k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1)
     p.k_pages, p.v_pages = k_pages.data_ptr(), v_pages.data_ptr()
     p.page_stride, p.page_stride_tok, p.page_stride_head = k_pages.stride(0), k_pages.stride(1), k_pages.stride(2)
-    p._keepalive = (k, v, k_pages, v_pages, cu_q, kv_lens, block_table)      # see make_fwd_params
-    return p
 
 
 def cf_kv_append(params, stream=None):
     _check(lib().cf_kv_append(C.byref(params), _stream_for(params, stream)))
+
+
+# ---------------------------------------------------------------------------------------------- rotation, a cache of 8 bits
+def make_rotation(inv_freq, interleaved=False):
+    """inv_freq: contiguous fp32 device tensor, a pair's angle per position; its pairs are elements (i, i + n) of a head, n = inv_freq.numel(), or
+    (2 i, 2 i + 1) where interleaved."""
+    import torch
+    assert inv_freq.is_cuda and inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous()
+    r = Rotation(inv_freq.data_ptr(), 2 * inv_freq.numel(), int(bool(interleaved)))
+    r._keepalive = (inv_freq,)
+    return r
+
+
+def _rotate_tensor(x, y):
+    assert x.is_cuda and x.device == y.device and x.dim() == 3 and x.shape == y.shape and x.stride(2) == y.stride(2) == 1
+    return RotateTensor(x.shape[1], _dtype_code(x), _dtype_code(y), x.data_ptr(), x.stride(0), x.stride(1), y.data_ptr(), y.stride(0), y.stride(1))
+
+
+def make_rotate_params(cu_q, cu_k, rotation, q=None, k=None, inverse=False):
+    """q, k: (x, y) of [T,H,D] tensors, y may be x; None: no such tensor.  cu_q, cu_k: as in make_fwd_params.  inverse: the gradients' way back."""
+    given = [t for t in (q, k) if t is not None]
+    assert given and all(t[0].shape[0] == given[0][0].shape[0] and t[0].shape[2] == given[0][0].shape[2] for t in given)
+    for t in (cu_q, cu_k):
+        assert t.is_cuda and t.is_contiguous() and t.element_size() == 4 and not t.is_floating_point()
+    assert cu_q.numel() == cu_k.numel()
+    x = given[0][0]
+    assert all(t.device == x.device for t in (cu_q, cu_k, rotation._keepalive[0]) + tuple(t[0] for t in given))
+    p = RotateParams()
+    p.head_dim, p.inverse, p.n_tokens, p.n_segments = x.shape[2], int(bool(inverse)), x.shape[0], cu_q.numel() - 1
+    p.cu_seqlens_q, p.cu_seqlens_k = cu_q.data_ptr(), cu_k.data_ptr()
+    p.rotation = rotation
+    if q is not None:
+        p.q = _rotate_tensor(*q)
+    if k is not None:
+        p.k = _rotate_tensor(*k)
+    p._keepalive = (x, q, k, cu_q, cu_k, rotation)      # see make_fwd_params
+    return p
+
+
+def cf_rotate(params, stream=None):
+    _check(lib().cf_rotate(C.byref(params), _stream_for(params, stream)))
+
+
+def make_append_rotation(rotation, q=None, q_out=None):
+    """What cf_kv_append_rotated and cf_kv_append8 turn: the keys, and where given the same rows' queries q [T,Hq,D] into q_out (may be q)."""
+    r = AppendRotation()
+    r.rotation = rotation
+    if q is not None:
+        assert q_out.dtype == q.dtype
+        t = _rotate_tensor(q, q_out)
+        r.n_q_heads, r.q, r.q_stride_tok, r.q_stride_head = t.n_heads, t.x, t.x_stride_tok, t.x_stride_head
+        r.q_out, r.q_out_stride_tok, r.q_out_stride_head = t.y, t.y_stride_tok, t.y_stride_head
+    r._keepalive = (rotation, q, q_out)
+    return r
+
+
+def _check_append_rotation(append, rotation):
+    """The queries are the rows of the call's keys (an address says nothing of it)."""
+    k, q = append._keepalive[0], rotation._keepalive[1]
+    k = k if not isinstance(k, C.Structure) else k._keepalive[0]
+    assert rotation.rotation.rot_dim <= k.shape[2] and rotation._keepalive[0]._keepalive[0].device == k.device
+    assert q is None or (q.shape[0] == k.shape[0] and q.shape[2] == k.shape[2] and q.dtype == k.dtype and q.device == k.device)
+
+
+def cf_kv_append_rotated(params, rotation, stream=None):
+    """params: make_kv_append_params; rotation: make_append_rotation."""
+    if hasattr(params, "_keepalive"):
+        _check_append_rotation(params, rotation)
+    _check(lib().cf_kv_append_rotated(C.byref(params), C.byref(rotation), _stream_for(params, stream)))
+
+
+def _check_scales(k_pages, v_pages, k_scales, v_scales):
+    import torch
+    for t in (k_pages, v_pages):
+        assert t.dtype in (torch.uint8, torch.float8_e4m3fn)
+    for t in (k_scales, v_scales):
+        assert t.dtype == torch.float32 and t.device == k_pages.device and (t.stride(2) == 1 or t.shape[2] == 1)
+        assert tuple(t.shape) == (k_pages.shape[0], k_pages.shape[2], k_pages.shape[1] // CF_KV8_BLOCK)
+    assert k_scales.stride() == v_scales.stride()
+
+
+def make_kv_append8_params(k, v, k_pages, v_pages, k_scales, v_scales, cu_q, kv_lens, block_table):
+    """k_pages, v_pages [n_pages,page_size,Hkv,D] of float8_e4m3fn or uint8; k_scales, v_scales [n_pages,Hkv,page_size/16] fp32; the rest as in
+    make_kv_append_params."""
+    _check_scales(k_pages, v_pages, k_scales, v_scales)
+    p = KvAppend8Params()
+    _fill_append(p.a, k, v, k_pages, v_pages, cu_q, kv_lens, block_table)
+    p.k_scales, p.v_scales, p.scale_stride_page, p.scale_stride_head = k_scales.data_ptr(), v_scales.data_ptr(), *_scale_strides(k_scales)
+    p._keepalive = (k, v, k_pages, v_pages, k_scales, v_scales, cu_q, kv_lens, block_table)      # see make_fwd_params
+    return p
+
+
+def _scale_strides(t):
+    """(A dimension of one has any stride.)"""
+    n = t.shape[2]
+    head = t.stride(1) if t.shape[1] > 1 else n
+    return (t.stride(0) if t.shape[0] > 1 else max(n, head)), head
+
+
+def cf_kv_append8(params, rotation=None, stream=None):
+    """params: make_kv_append8_params; rotation: make_append_rotation, or None."""
+    if rotation is not None and hasattr(params, "_keepalive"):
+        _check_append_rotation(params, rotation)
+    _check(lib().cf_kv_append8(C.byref(params), C.byref(rotation) if rotation is not None else None, _stream_for(params, stream)))
+
+
+def make_paged8_params(q, k_pages, v_pages, k_scales, v_scales, o, lse, cu_q, kv_lens, block_table, scale, max_kv_len=0, window=0, n_sinks=0,
+                       flags=0, workspace=None):
+    """As make_paged_params, over the pages of make_kv_append8_params."""
+    _check_scales(k_pages, v_pages, k_scales, v_scales)
+    p = AttnPaged8Params()
+    _fill_paged(p.a, q, k_pages, v_pages, o, lse, cu_q, kv_lens, block_table, scale, max_kv_len, window, n_sinks, flags, workspace)
+    p.k_scales, p.v_scales, p.scale_stride_page, p.scale_stride_head = k_scales.data_ptr(), v_scales.data_ptr(), *_scale_strides(k_scales)
+    workspace = _paged_workspace(p.a, cf_attn_paged8_workspace_bytes, p, q, workspace)
+    p._keepalive = (q, k_pages, v_pages, k_scales, v_scales, o, lse, cu_q, kv_lens, block_table, workspace)      # see make_fwd_params
+    return p
+
+
+def cf_attn_paged8_workspace_bytes(params):
+    return _check(lib().cf_attn_paged8_workspace_bytes(C.byref(params)))
+
+
+def cf_attn_paged8_fwd(params, stream=None):
+    _check(lib().cf_attn_paged8_fwd(C.byref(params), _stream_for(params, stream)))

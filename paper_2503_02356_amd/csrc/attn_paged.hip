@@ -8,7 +8,9 @@
 #include <algorithm>
 
 #include "common.h"
+#include "kv_append.h"
 #include "paged.h"
+#include "paged_checks.h"
 
 namespace cf {
 namespace {
@@ -172,65 +174,6 @@ hipError_t run_join(const PagedArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) % n) == 0; }
-
-int check_common(const char *who, int dtype, int D, int n_tokens, int n_seqs, const int32_t *cu, const int32_t *lens, const int32_t *table,
-                 int64_t table_stride, int pages, int page_size, int n_pages)
-{
-    if (dtype != CF_BF16 && dtype != CF_FP32) return fail(CF_EUNSUPPORTED, "%s: dtype %d not supported", who, dtype);
-    if (D != 64 && D != 128) return fail(CF_EUNSUPPORTED, "%s: head_dim %d not supported (64 or 128)", who, D);
-    if (n_tokens < 1 || n_seqs < 1 || n_seqs > (1 << 30))        // (the kernels' searches add two places or double one)
-        return fail(CF_EINVAL, "%s: need n_tokens >= 1 and 1 <= n_seqs <= 2^30 (got %d, %d)", who, n_tokens, n_seqs);
-    if (page_size < 16 || page_size > 65536 || (page_size & (page_size - 1)))
-        return fail(CF_EINVAL, "%s: page_size %d must be a power of two from 16 to 65536", who, page_size);
-    if (n_pages < 1 || pages < 1 || (int64_t)pages * page_size > (1 << 30) || table_stride < pages)
-        return fail(CF_EINVAL, "%s: need n_pages >= 1, 1 <= pages_per_seq <= table_stride, pages_per_seq * page_size <= 2^30 (got %d, %d, %lld)", who,
-                    n_pages, pages, (long long)table_stride);
-    if (!cu || !lens || !table) return fail(CF_EINVAL, "%s: NULL device pointer", who);
-    if (!aligned(cu, 4) || !aligned(lens, 4) || !aligned(table, 4)) return fail(CF_EINVAL, "%s: misaligned descriptor", who);
-    return CF_OK;
-}
-
-int check_strides(const char *who, int dtype, int D, std::initializer_list<int64_t> strides)
-{
-    const int64_t vec = dtype == CF_BF16 ? 8 : 4;
-    for (int64_t s : strides)
-        if (s < D || s % vec != 0)
-            return fail(CF_EINVAL, "%s: stride %lld must be >= head_dim and a multiple of %lld elements", who, (long long)s, (long long)vec);
-    return CF_OK;
-}
-
-int check_paged(const cf_attn_paged_params *p, const char *who, bool sizes_only, PagedArgs *a)
-{
-    if (!p) return fail(CF_EINVAL, "%s: params is NULL", who);
-    if (p->n_q_heads < 1 || p->n_kv_heads < 1 || p->n_q_heads % p->n_kv_heads != 0 || p->n_q_heads > 65535)
-        return fail(CF_EINVAL, "%s: n_q_heads %d must be a positive multiple of n_kv_heads %d, at most 65535", who, p->n_q_heads, p->n_kv_heads);
-    static const int32_t dummy[1] = {0};
-    const int32_t *cu = sizes_only ? dummy : p->cu_seqlens_q, *lens = sizes_only ? dummy : p->kv_lens, *table = sizes_only ? dummy : p->block_table;
-    if (int rc = check_common(who, p->dtype, p->head_dim, p->n_tokens, p->n_seqs, cu, lens, table, p->table_stride, p->pages_per_seq, p->page_size,
-                              p->n_pages))
-        return rc;
-    if ((int64_t)p->n_tokens * p->n_q_heads > 0x7fffffffLL)
-        return fail(CF_EINVAL, "%s: n_tokens * n_q_heads = %lld must be below 2^31", who, (long long)p->n_tokens * p->n_q_heads);
-    if (p->flags & ~CF_FLAG_SCALAR_KERNELS) return fail(CF_EINVAL, "%s: unknown flags 0x%x", who, p->flags);
-    if (p->max_kv_len < 0 || p->window < 0 || p->n_sinks < 0 || (p->window == 0 && p->n_sinks != 0))
-        return fail(CF_EINVAL, "%s: need max_kv_len, window, n_sinks >= 0 and no sinks without a window (got %d, %d, %d)", who, p->max_kv_len, p->window,
-                    p->n_sinks);
-    a->p = *p;
-    const int capacity = p->pages_per_seq * p->page_size;
-    a->mask = p->window == 0 ? WindowMask{0x7fffffff, 0} : WindowMask{p->window, std::min(p->n_sinks, capacity)};
-    a->shift = __builtin_ctz((unsigned)p->page_size);
-    if (sizes_only) return CF_OK;
-    if (!p->q || !p->k_pages || !p->v_pages || !p->o) return fail(CF_EINVAL, "%s: NULL device pointer", who);
-    if (!(p->softmax_scale - p->softmax_scale == 0.f)) return fail(CF_EINVAL, "%s: softmax_scale is not finite", who);
-    if (int rc = check_strides(who, p->dtype, p->head_dim, {p->q_stride_tok, p->q_stride_head, p->page_stride, p->kv_stride_tok, p->kv_stride_head,
-                                                            p->o_stride_tok, p->o_stride_head}))
-        return rc;
-    if (!aligned(p->q, 16) || !aligned(p->k_pages, 16) || !aligned(p->v_pages, 16) || !aligned(p->o, 16) || !aligned(p->lse, 4))
-        return fail(CF_EINVAL, "%s: q, pages and o must be 16-byte aligned", who);
-    return CF_OK;
-}
-
 // The matrix kernels' offsets inside a group of 16 keys have 32 bits, and a HIP launch holds fewer than 2^32 work-items.  (Wider rows and
 // larger calls: a wavefront to a row.)
 enum Path { kRows, kMfma, kF32 };
@@ -275,13 +218,7 @@ extern "C" int cf_attn_paged_fwd(const cf_attn_paged_params *p, void *hip_stream
     cf::PagedArgs a;
     if (int rc = cf::check_paged(p, who, false, &a)) return rc;
     const int64_t need = cf::cut(a);
-    if (need > 0) {
-        if (!p->workspace || !cf::aligned(p->workspace, 256)) return cf::fail(CF_EINVAL, "%s: workspace must be non-NULL and 256-byte aligned", who);
-        if (p->workspace_bytes < need)
-            return cf::fail(CF_EINVAL, "%s: workspace has %lld bytes, %lld needed", who, (long long)p->workspace_bytes, (long long)need);
-        a.part_o = static_cast<float *>(p->workspace);
-        a.part_ml = reinterpret_cast<float2 *>(a.part_o + (int64_t)a.parts * p->n_tokens * p->n_q_heads * p->head_dim);
-    }
+    if (int rc = cf::take_workspace(who, need, &a)) return rc;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const cf::Path path = cf::path_of(a);
     hipError_t e;
@@ -297,15 +234,7 @@ extern "C" int cf_kv_append(const cf_kv_append_params *p, void *hip_stream)
 {
     const char *who = "cf_kv_append";
     if (!p) return cf::fail(CF_EINVAL, "%s: params is NULL", who);
-    if (p->n_kv_heads < 1 || p->n_kv_heads > 65535) return cf::fail(CF_EINVAL, "%s: n_kv_heads %d must be from 1 to 65535", who, p->n_kv_heads);
-    if (int rc = cf::check_common(who, p->dtype, p->head_dim, p->n_tokens, p->n_seqs, p->cu_seqlens_q, p->kv_lens, p->block_table, p->table_stride,
-                                  p->pages_per_seq, p->page_size, p->n_pages))
-        return rc;
-    if (!p->k || !p->v || !p->k_pages || !p->v_pages) return cf::fail(CF_EINVAL, "%s: NULL device pointer", who);
-    if (int rc = cf::check_strides(who, p->dtype, p->head_dim, {p->kv_stride_tok, p->kv_stride_head, p->page_stride, p->page_stride_tok, p->page_stride_head}))
-        return rc;
-    if (!cf::aligned(p->k, 16) || !cf::aligned(p->v, 16) || !cf::aligned(p->k_pages, 16) || !cf::aligned(p->v_pages, 16))
-        return cf::fail(CF_EINVAL, "%s: k, v and pages must be 16-byte aligned", who);
+    if (int rc = cf::check_append(p, who, false)) return rc;
     const int units = p->head_dim * (p->dtype == CF_BF16 ? 2 : 4) / 16;
     const int64_t blocks = ((int64_t)p->n_tokens * p->n_kv_heads * units + 255) / 256;
     if (blocks * 256 > 0xffffffffLL) return cf::fail(CF_EINVAL, "%s: %d tokens of %d heads are more than one launch holds", who, p->n_tokens, p->n_kv_heads);

@@ -1,0 +1,56 @@
+// A paged cache of 8 bits: its numbers' powers of two, and which blocks of it a call adds to.  Runs on the CPU too.
+#pragma once
+#include <string.h>
+
+#include "pages.h"
+
+namespace cf {
+
+constexpr int kBlock8 = 16;              // tokens that share a scale (CF_KV8_BLOCK)
+constexpr int kLeast8 = -110;            // exponent of the least scale that is written: below it e4m3 times it would leave bf16's normal numbers
+constexpr int kMost8 = 120;              // of the largest that a block of finite fp32 elements needs
+
+CF_BOTH unsigned bits_of(float x)
+{
+    unsigned u;
+    memcpy(&u, &x, 4);
+    return u;
+}
+CF_BOTH float float_of(unsigned u)
+{
+    float x;
+    memcpy(&x, &u, 4);
+    return x;
+}
+CF_BOTH float power8(int e) { return float_of((unsigned)(e + 127) << 23); }      // 2^e, -126 .. 127
+
+// The least e from kLeast8 on with most <= 448 * 2^e, for a finite most >= 0:  most = 1.f * 2^E,  448 = 1.75 * 2^8.
+CF_BOTH int exponent_for(float most)
+{
+    const unsigned u = bits_of(most);
+    return at_least(kLeast8, (int)(u >> 23) - 127 - 8 + ((u & 0x7fffff) > 0x600000));
+}
+// The exponent that a scale in the pages stands for, as far as a block that is added to may keep it.
+CF_BOTH int exponent_of(float scale) { return at_most(kMost8, at_least(kLeast8, (int)(bits_of(scale) >> 23 & 255) - 127)); }
+// What a scale multiplies with: its exponent alone (as the conversion instructions of the matrix kernels take it).
+CF_BOTH float factor8(float scale)
+{
+    const unsigned e = bits_of(scale) >> 23 & 255;
+    return float_of(e == 0 ? 0x400000u : e == 255 ? 0x7fc00000u : e << 23);
+}
+
+// The blocks of 16 keys that a sequence's new rows go into, [first, first + n), and those of all sequences in one list: sequence g's from
+// first_block_place(cu_seqlens_q[g], g) on.  Lq rows touch (Lq + 14) / 16 + 1 blocks at most, and two sequences' places are Lq / 16 + 2,
+// rounded either way, apart.
+CF_BOTH int first_block_place(int begin, int seq) { return begin / kBlock8 + 2 * seq; }
+CF_BOTH int64_t block_places(int64_t tokens, int64_t seqs) { return tokens / kBlock8 + 2 * seqs; }
+struct NewBlocks {
+    int begin, end;                      // positions of the new rows
+    int first, n;
+    CF_BOTH NewBlocks(const NewRows &rows) : begin(at_least(0, rows.first_position)), end(rows.first_position + rows.lq), first(begin / kBlock8), n(0)
+    {
+        if (end > begin) n = (end - 1) / kBlock8 - first + 1;
+    }
+};
+
+}  // namespace cf

@@ -1,0 +1,229 @@
+"""Attention over a paged cache of 8 bits, on the GPU, against the definition in 64 bits over what the cache holds."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2503_02356_amd import binding as B
+from tests import plain_cache8 as P
+from tests import plain_window as W
+from tests.test_gpu_paged import Batch, SEQS, ints
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, FP32 = torch.bfloat16, torch.float32
+SCALAR = B.CF_FLAG_SCALAR_KERNELS
+KINDS = [(FP32, 64, 0), (FP32, 128, 0), (BF16, 64, 0), (BF16, 128, 0), (BF16, 128, SCALAR), (FP32, 64, SCALAR)]
+NAN = float("nan")
+
+
+@pytest.fixture(autouse=True)
+def _seeded():
+    torch.manual_seed(1234)
+
+
+class Batch8(Batch):
+    """Its pages, new rows among them, in 8 bits; what nobody has written is NaN there too."""
+
+    def __init__(self, *args, heads_first=False, far=0, **more):
+        super().__init__(*args, heads_first=heads_first, far=far, **more)
+        self.append()
+        self.codes, self.scales = [], []
+        g = torch.Generator(device=DEV)
+        g.manual_seed(99)
+        for x in (self.kp, self.vp):
+            if far:                                  # (too many to convert: those that are used)
+                used = torch.unique(torch.tensor(self.table_host[(self.table_host >= 0) & (self.table_host < self.n_pages)], device=DEV).long())
+                codes = torch.empty(x.shape, dtype=torch.uint8, device=DEV)
+                scales = torch.empty(x.shape[0], x.shape[2], x.shape[1] // 16, device=DEV)
+                codes[used], scales[used] = P.quantised(x[used])
+            else:                                    # blocks of different sizes
+                size = torch.exp(0.7 * torch.randn(x.shape[0], x.shape[1] // 16, 1, x.shape[2], 1, generator=g, device=DEV))
+                x = (x.float().reshape(x.shape[0], -1, 16, *x.shape[2:]) * size).reshape(x.shape)
+                codes, scales = P.quantised(x)
+            if heads_first:
+                codes, scales = codes.transpose(1, 2).contiguous().transpose(1, 2), scales.transpose(0, 1).contiguous().transpose(0, 1)
+            self.codes.append(codes)
+            self.scales.append(scales)
+        self.kp = self.vp = None
+        self.read()
+
+    def read(self):
+        """The keys and values that the cache holds."""
+        for i, (_, n) in enumerate(self.seqs):
+            at = torch.arange(n, device=DEV)
+            number = torch.tensor(self.table_host[i], device=DEV).long()[at // self.page]
+            number = torch.where((number >= 0) & (number < self.n_pages), number, 0)
+            self.keys[i] = tuple(P.values(c[number, at % self.page], s[number, :, at % self.page // 16][:, :, None]) for c, s in zip(self.codes, self.scales))
+
+    def params(self, flags=0, max_kv_len=0, workspace=None):
+        return B.make_paged8_params(self.q, *self.codes, *self.scales, self.o, self.lse, self.cu, self.lens, self.table, self.scale, max_kv_len,
+                                    self.window, self.sinks, flags, workspace)
+
+    def run(self, flags=0, max_kv_len=0):
+        B.cf_attn_paged8_fwd(self.params(flags, max_kv_len))
+        torch.cuda.synchronize()
+        return dict(o=self.o.clone(), lse=self.lse.clone())
+
+
+@pytest.mark.parametrize("dtype,D,flags", KINDS)
+@pytest.mark.parametrize("s", range(len(SEQS)))
+def test_against_the_definition(dtype, D, flags, s):
+    for n, (page, Hq, Hkv) in enumerate([(16, 4, 2), (64, 7, 1), (256, 3, 3), (32, 16, 1)]):
+        b = Batch8(SEQS[s], Hq, Hkv, D, dtype, page, pad=n, columns=n, seed=s + n, heads_first=n == 1)
+        b.check(b.run(flags, max_kv_len=[0, 5000, 1, 100][n]), (SEQS[s], page, Hq, Hkv))
+
+
+@pytest.mark.parametrize("dtype,D,flags", KINDS)
+def test_windows_and_pages_that_were_given_back(dtype, D, flags):
+    for n, (window, sinks, page) in enumerate([(1, 0, 16), (64, 4, 16), (65, 64, 32), (500, 1, 128), (2000, 0, 16), (40, 200, 64), (2**31 - 1, 1000, 16)]):
+        seqs = [(1, 1500), (33, 900), (1, 30), (200, 200), (2, 130)]
+        hidden = {(i, c): -1 for i, (a, m) in enumerate(seqs) for c in range(-(-m // page)) if (c + 1) * page <= m - a - window + 1 and c * page >= sinks}
+        b = Batch8(seqs, 4, 2, D, dtype, page, window, sinks, hidden, seed=n)
+        b.check(b.run(flags), (window, sinks, page))
+
+
+@pytest.mark.parametrize("dtype,D,flags", KINDS)
+def test_pages_that_are_none(dtype, D, flags):
+    hidden = {(0, 1): -1, (0, 5): 10**6, (1, 0): 2**31 - 1, (2, 3): -2**31, (2, 4): -5, (3, 0): -1, (3, 1): -1}
+    seqs = [(40, 130), (3, 10), (20, 80), (2, 32), (1, 200)]
+    b = Batch8(seqs, 6, 2, D, dtype, 16, hidden=hidden, seed=3)
+    got = b.run(flags)
+    b.check(got, "hidden pages")
+    assert (got["o"][43 + 20:43 + 22] == 0).all() and torch.isinf(got["lse"][:, 63:65]).all() and (got["o"][40:43] == 0).all()
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (30, 20), (60, 3)])
+@pytest.mark.parametrize("dtype,D,flags", KINDS)
+def test_lengths_beyond_the_table(dtype, D, flags, window, sinks):
+    b = Batch8([(4, 100), (1, 64), (40, 300)], 4, 2, D, dtype, 16, window, sinks, seed=4)
+    b.table = b.table[:, :3]                         # 48 keys of each
+    b.run(flags)
+    b.table_host = b.table_host.copy()
+    b.table_host[:, 3:] = -1
+    b.check(dict(o=b.o, lse=b.lse), "narrow table")
+
+
+@pytest.mark.parametrize("what", ["key", "value", "key scale", "value scale"])
+@pytest.mark.parametrize("dtype,D,flags", KINDS)
+def test_what_is_not_finite_reaches_the_rows_that_see_it(dtype, D, flags, what):
+    """A NaN number of key 160 (rows at positions 160 .. 199, i.e. 20 .. 59), or a NaN scale of keys 160 .. 175."""
+    b = Batch8([(60, 200), (1, 90)], 4, 2, D, dtype, 32, window=50, seed=5)
+    good = b.run(flags)
+    at, i = int(b.table_host[0, 160 // 32]), int("value" in what)
+    if "scale" in what:
+        b.scales[i][at, 1, 160 % 32 // 16] = NAN
+    else:
+        b.codes[i][at, 160 % 32, 1, 3] = 0xff
+    b.run(flags)
+    for rows in (slice(0, 20), slice(60, 61)):
+        # two runs of one call: the same sums in another order at most (row_again), half a step of o and the rounding of P
+        assert torch.allclose(b.o[rows].float(), good["o"][rows].float(), atol=2.0 ** -4 if dtype == BF16 else 1e-4, rtol=2.0 ** -7)
+        assert torch.isfinite(b.lse[:, rows]).all() and torch.isfinite(b.o[rows]).all()
+    assert torch.isfinite(b.o[:, :2]).all()
+    if what == "value":
+        assert not torch.isfinite(b.o[20:60, 2:, 3]).any() and torch.isfinite(b.o[20:60, 2:, 4:]).all()
+    elif what == "value scale":
+        assert not torch.isfinite(b.o[20:60, 2:]).any()
+    else:
+        assert not torch.isfinite(b.o[20:60, 2:]).any() and torch.isnan(b.lse[2:, 20:60]).all()
+
+
+@pytest.mark.parametrize("dtype,D", [(FP32, 64), (BF16, 64), (BF16, 128), (FP32, 128)])
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 1.5])
+def test_other_scales(dtype, D, scale):
+    b = Batch8([(1, 400), (50, 90)], 4, 2, D, dtype, 16, seed=6, scale=scale)
+    b.check(b.run(), scale)
+
+
+@pytest.mark.parametrize("dtype,D,flags", KINDS)
+def test_scales_that_are_no_powers_of_two(dtype, D, flags):
+    """Their exponent counts: any factor from 1 to 2, and a sign, change nothing."""
+    b = Batch8([(1, 300), (50, 90), (200, 333)], 4, 2, D, dtype, 64, seed=7)
+    want = b.run(flags)
+    for s in b.scales:
+        s *= (1 + 0.999 * torch.rand(s.shape, device=DEV)) * torch.where(torch.rand(s.shape, device=DEV) < 0.5, -1.0, 1.0)
+    got = b.run(flags)
+    assert all(bool(torch.equal(got[x], want[x])) for x in got)
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 128), (FP32, 64)])
+def test_offsets_beyond_32_bits(dtype, D):
+    page, Hkv = 256, 8
+    far = (5 << 30) // (page * Hkv * D)
+    b = Batch8([(1, 3000), (70, 500)], 16, Hkv, D, dtype, page, seed=7, far=far)
+    b.check(b.run(), "far pages")
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 128), (BF16, 64), (FP32, 64)])
+def test_runs_repeat_and_do_not_need_lse(dtype, D):
+    b = Batch8([(1, 4000), (30, 2500), (1, 7)], 8, 2, D, dtype, 64, seed=8)
+    one, two = b.run(), b.run()
+    assert bool(torch.equal(one["o"], two["o"])) and bool(torch.equal(one["lse"], two["lse"]))
+    p = B.make_paged8_params(b.q, *b.codes, *b.scales, b.o, None, b.cu, b.lens, b.table, b.scale)
+    b.o.zero_()
+    B.cf_attn_paged8_fwd(p)
+    torch.cuda.synchronize()
+    assert bool(torch.equal(b.o, one["o"]))
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 64), (BF16, 128), (FP32, 128)])
+@pytest.mark.parametrize("seqs,Hq,Hkv", [([(1, n) for n in (3, 70, 800, 2100, 16, 1)] * 6, 32, 8), ([(1, 20000)], 28, 4), ([(1, 60), (3, 40)] * 40 + [(500, 900)], 14, 2),
+                                         ([(130, 5000)], 16, 16), ([(1000, 1700), (300, 300)], 28, 4), ([(2, 9000), (1, 9000), (600, 2000)], 64, 8)])
+def test_larger_calls(dtype, D, seqs, Hq, Hkv):
+    """Calls of each kind: single tokens, chunks, both; cut along their keys or not."""
+    page = [16, 32, 64, 128][len(seqs) % 4]
+    b = Batch8(seqs, Hq, Hkv, D, dtype, page, seed=13)
+    b.check(b.run(max_kv_len=max(n for _, n in seqs)), (seqs[:3], Hq, Hkv))
+    w = Batch8(seqs, Hq, Hkv, D, dtype, page, window=300, sinks=5, seed=14)
+    w.check(w.run(max_kv_len=max(n for _, n in seqs)), "window")
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 128), (FP32, 64)])
+def test_append_and_attend_through_graphs(dtype, D):
+    """One token after the other through one captured step of append, with rotation, and attention; a second graph shares its workspace."""
+    rot = D // 2
+    b = Batch8([(1, 700), (1, 33), (1, 2)], 8, 2, D, dtype, 16, columns=3, seed=9)
+    b.table_host[:, -3:] = [[1, 2, 3]] * 3           # (not reached)
+    other = Batch8([(2, 900)], 8, 2, D, dtype, 16, seed=10)
+    need = max(B.cf_attn_paged8_workspace_bytes(x.params(max_kv_len=800)) for x in (b, other))
+    ws = torch.zeros(max(need, 256), dtype=torch.uint8, device=DEV)
+    f = (10000.0 ** (-torch.arange(rot // 2, device=DEV) / (rot // 2))).float()
+    append = B.make_kv_append8_params(b.k, b.v, *b.codes, *b.scales, b.cu, b.lens, b.table)
+    turn = B.make_append_rotation(B.make_rotation(f), b.q, b.q)
+    p, q = (x.params(max_kv_len=800, workspace=ws) for x in (b, other))
+    graphs = []
+    for call in ((lambda: (B.cf_kv_append8(append, turn), B.cf_attn_paged8_fwd(p))), (lambda: B.cf_attn_paged8_fwd(q))):
+        call()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        graphs.append(graph)
+    for step in range(4):
+        b.seqs = [(1, n + step) for n in (700, 33, 2)]
+        b.lens.copy_(ints([n for _, n in b.seqs]))
+        fresh = torch.randn(b.q.shape[0], b.q.shape[1] + 4, D, device=DEV).to(dtype)
+        b.q.copy_(fresh[:, :8]), b.k.copy_(fresh[:, 8:10]), b.v.copy_(fresh[:, 10:])
+        b.o.fill_(1), other.o.fill_(1), ws.fill_(255)
+        want, tol = P.turn_tolerance(b.q, torch.tensor([n - 1 for _, n in b.seqs], device=DEV), f, False, False, dtype)
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        assert bool(((b.q.double() - want).abs() <= tol).all())
+        b.read()
+        b.check(dict(o=b.o, lse=b.lse), step)
+        other.check(dict(o=other.o, lse=other.lse), step)
+
+
+def test_another_stream():
+    b = Batch8([(1, 4000), (64, 900)], 8, 2, 128, BF16, 64, seed=12)
+    want = b.run()
+    side = torch.cuda.Stream()
+    b.o.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        B.cf_attn_paged8_fwd(b.params())
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert bool(torch.equal(b.o, want["o"]))
