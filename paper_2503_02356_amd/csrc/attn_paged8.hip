@@ -41,15 +41,21 @@ hipError_t run_rows(const Paged8Args &a, hipStream_t s)
     return hipGetLastError();
 }
 
-bool on_matrix_kernel(const PagedArgs &)
+// The matrix kernels' offsets inside a group of 16 keys have 32 bits, and a HIP launch holds fewer than 2^32 work-items.  (Wider rows and
+// larger calls: a wavefront to a row.)
+bool on_matrix_kernel(const PagedArgs &a)
 {
-    return false;
+    return !(a.p.flags & CF_FLAG_SCALAR_KERNELS) && a.p.kv_stride_tok < (1 << 25) && paged8_mfma_launch_size(a) <= 0xffffffffLL;
 }
 // Chooses the parts; bytes of workspace.
 int64_t cut(PagedArgs &a)
 {
-    a.parts = 1, a.tiles_per_part = 1 << 28, a.part_o = nullptr, a.part_ml = nullptr;
-    return 0;
+    a.part_o = nullptr, a.part_ml = nullptr;
+    cut_paged8_mfma(a);
+    if (!on_matrix_kernel(a)) a.parts = 1;
+    if (a.parts == 1) return 0;
+    const int64_t rows = (int64_t)a.p.n_tokens * a.p.n_q_heads;
+    return a.parts * rows * (a.p.head_dim * 4 + 8);
 }
 
 int check(const cf_attn_paged8_params *p, const char *who, bool sizes_only, Paged8Args *c)
@@ -80,7 +86,8 @@ extern "C" int cf_attn_paged8_fwd(const cf_attn_paged8_params *p8, void *hip_str
     if (int rc = cf::take_workspace(who, need, &c.a)) return rc;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     hipError_t e;
-    if (p->dtype == CF_FP32) e = p->head_dim == 64 ? cf::run_rows<float, 64>(c, s) : cf::run_rows<float, 128>(c, s);
+    if (cf::on_matrix_kernel(c.a)) e = cf::launch_paged8_mfma(c, s);
+    else if (p->dtype == CF_FP32) e = p->head_dim == 64 ? cf::run_rows<float, 64>(c, s) : cf::run_rows<float, 128>(c, s);
     else e = p->head_dim == 64 ? cf::run_rows<unsigned short, 64>(c, s) : cf::run_rows<unsigned short, 128>(c, s);
     if (e == hipSuccess && c.a.parts > 1) e = cf::launch_paged_join(c.a, s);
     return e == hipSuccess ? CF_OK : cf::fail(CF_EHIP, "%s: %s", who, hipGetErrorString(e));
