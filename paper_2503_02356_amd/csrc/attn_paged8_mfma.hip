@@ -36,8 +36,9 @@ __device__ __forceinline__ int swz8(int row)
 }
 
 // The numbers of four words, times the power of two `scale`, as bf16.
-__device__ __forceinline__ bf16x8 numbers(int w0, int w1, float scale0, float scale1)
+__device__ __forceinline__ bf16x8 numbers(int w0, int w1, int bits0, int bits1)
 {
+    const float scale0 = __builtin_bit_cast(float, bits0), scale1 = __builtin_bit_cast(float, bits1);
     const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w0, scale0, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w0, scale0, true);
     const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w1, scale1, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w1, scale1, true);
     return __builtin_shufflevector(__builtin_shufflevector(a, b, 0, 1, 2, 3), __builtin_shufflevector(c, d, 0, 1, 2, 3), 0, 1, 2, 3, 4, 5, 6, 7);
@@ -45,26 +46,25 @@ __device__ __forceinline__ bf16x8 numbers(int w0, int w1, float scale0, float sc
 
 // Where a workgroup's keys and their scales stand.
 struct KeySource8 : KeySource<1> {
-    const CF_CONSTANT float *k_scales, *v_scales;        // of this head (nothing writes them meanwhile: scalar loads)
+    const CF_CONSTANT int *k_scales, *v_scales;          // of this head (nothing writes them meanwhile: scalar loads)
     int64_t scale_page;
     __device__ __forceinline__ KeySource8(const Paged8Args &c, const TileRows &t, int keys)
-        : KeySource<1>(c.a, t, keys), k_scales((const CF_CONSTANT float *)c.k_scales + (int64_t)t.kh * c.scale_head),
-          v_scales((const CF_CONSTANT float *)c.v_scales + (int64_t)t.kh * c.scale_head), scale_page(c.scale_page)
+        : KeySource<1>(c.a, t, keys), k_scales((const CF_CONSTANT int *)c.k_scales + (int64_t)t.kh * c.scale_head),
+          v_scales((const CF_CONSTANT int *)c.v_scales + (int64_t)t.kh * c.scale_head), scale_page(c.scale_page)
     {
     }
-    // The scales of N blocks from `key` on, of one page; 1 where there are none (what stands there, nobody may have written).
+    __device__ __forceinline__ int64_t scale_at(int page, int key) const { return page * scale_page + (key & ((1 << shift) - 1)) / kBlock8; }
+    // The scales of N blocks from `key` on, of one page (of none, anything: see factors).  As integers, which stay in scalar registers.
     template <int N>
-    __device__ __forceinline__ void scales(int entry, int key, float *k, float *v) const
+    __device__ __forceinline__ void scales(int entry, int key, int *k, int *v) const
     {
-        const int64_t at = none(entry, key) ? 0 : entry * scale_page + (key & ((1 << shift) - 1)) / kBlock8;
+        const int64_t at = none(entry, key) ? 0 : scale_at(entry, key);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float x = k_scales[at + i], y = v_scales[at + i];
-            const bool missing = none(entry, key + kBlock8 * i);
-            k[i] = missing ? 1.f : x, v[i] = missing ? 1.f : y;
-        }
+        for (int i = 0; i < N; ++i) k[i] = k_scales[at + i], v[i] = v_scales[at + i];
     }
 };
+// The factor of a block whose scale is `bits`: 1 where the block is hidden (what stands there, nobody may have written).
+__device__ __forceinline__ int factor(int bits, unsigned hidden, int g) { return hidden >> g & 1 ? 0x3f800000 : bits; }
 
 // Copies rows of a key tile, 16 or all 64 from its row `row0` on, into their place in LDS.  An instruction takes RPI rows, its swizzle is one of two.
 template <int D>
@@ -165,7 +165,7 @@ struct Rows8 {
     // steps' operands, so step ks has elements 64 (ks / 2) + 8 (ks % 2) + 16 group ..
     __device__ __forceinline__ static int element(int ks) { return 64 * (ks / 2) + 8 * (ks % 2) + 16 * F::group(); }
 
-    __device__ __forceinline__ void scores(const char *k_tile, const float (&scale)[4], const WindowMask &mask, int start, int lowest, int highest,
+    __device__ __forceinline__ void scores(const char *k_tile, const int (&scale)[4], const WindowMask &mask, int start, int lowest, int highest,
                                            unsigned groups, float c2, f32x4 (&s)[4][QB])
     {
         i32x4 w[4][KS / 2];
@@ -192,7 +192,7 @@ struct Rows8 {
         }
         settle<D, 4, QB>(s, m, l, o, pos, mask, start, lowest, highest, groups, c2);
     }
-    __device__ __forceinline__ void values(const char *v_tile, const float (&scale)[4], const f32x4 (&s)[4][QB])
+    __device__ __forceinline__ void values(const char *v_tile, const int (&scale)[4], const f32x4 (&s)[4][QB])
     {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -244,7 +244,7 @@ __device__ __forceinline__ void few_rows8(const Paged8Args &c, const TileRows &t
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) p[g] = src.entry(start + KEYS * g);
     };
-    auto find_scales = [&](int start, const int (&p)[GROUPS], float (&k)[4], float (&v)[4]) {
+    auto find_scales = [&](int start, const int (&p)[GROUPS], int (&k)[4], int (&v)[4]) {
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) src.scales<KEYS / kBlock8>(p[g], start + KEYS * g, k + KEYS / kBlock8 * g, v + KEYS / kBlock8 * g);
     };
@@ -269,7 +269,7 @@ __device__ __forceinline__ void few_rows8(const Paged8Args &c, const TileRows &t
         scalar_loads_done();
     };
     int pages[GROUPS] = {}, next_pages[GROUPS] = {};
-    float k_scale[4] = {}, v_scale[4] = {};
+    int k_scale[4] = {}, v_scale[4] = {};
     int u = first + wave;
     if (u < end) {
         find_pages(tiles.start(u), pages);
@@ -303,12 +303,14 @@ __device__ __forceinline__ void few_rows8(const Paged8Args &c, const TileRows &t
 #pragma unroll
         for (int g = 0; g < 4; ++g) hidden |= (unsigned)src.none(pages[WHOLE ? 0 : g], start + 16 * g) << g;
         int after[GROUPS] = {};
-        float k_next[4] = {}, v_next[4] = {};
+        int k_next[4] = {}, v_next[4] = {};
         if (more) find_scales(tiles.start(u + 4), next_pages, k_next, v_next);
         if (u + 8 < end) find_pages(tiles.start(u + 8), after);
         f32x4 s[4][QB];
         wait_older();                                // K is there
         scalar_loads_done();
+#pragma unroll
+        for (int g = 0; g < 4; ++g) k_scale[g] = factor(k_scale[g], hidden, g), v_scale[g] = factor(v_scale[g], hidden, g);
         r.scores(k_tile, k_scale, mask, start, lowest, highest, hidden, c2, s);
         if (more) {
             reads_done();
@@ -399,50 +401,74 @@ template <int D, bool WHOLE>
 __device__ __forceinline__ void many_rows8(const Paged8Args &c, const TileRows &t, const KeyTiles<BN, WindowMask> &tiles, int first, int end, int keys,
                                            int part, char *stage_a, char *stage_b)
 {
-    // A lane converts LOADS units of 16 bytes of K and of V: unit lane % UNITS of row STEP * i + thread / UNITS, whose block of 16 keys is the
-    // wavefront's own.
-    constexpr int TILE = BN * 2 * D, UNITS = D / 16, STEP = 256 / UNITS, LOADS = BN / STEP;
+    // A lane converts a unit of 16 bytes of K and of V of LOADS rows: a wavefront has 16 rows, one block of keys, of 4 units each.  What it
+    // writes into a bf16 tile is served 8 lanes at a time, over 32 banks: lanes 8 x .. + 7 are 4 units of rows x and x + 8, whose swizzles differ in bit 0, so
+    // that the one's even units stand beside the other's odd ones.
+    constexpr int TILE = BN * 2 * D, LOADS = D / 64, GROUPS = WHOLE ? 1 : 4;
     const PagedArgs &a = c.a;
-    const int wave = wave_id(), col = F::column(), group = F::group();
+    const int wave = wave_id(), col = F::column(), group = F::group(), lane = threadIdx.x & 63;
     const int x0 = 32 * wave, rows = at_most(32, t.rows - x0);           // this wavefront's rows of the tile (rows <= 0: none)
     const KeySource8 src(c, t, keys);
-    const int my_row = threadIdx.x / UNITS, my_unit = threadIdx.x % UNITS;
-    int to[2];                                                           // where a lane's two units of bf16 go (swz() has period 16 rows)
+    const int my_row = 8 * (lane >> 2 & 1) + (lane >> 3), my_unit = (lane & 3) + (D == 128 ? 4 * (wave & 1) : 0);      // row of the block
+    const unsigned my_off = (unsigned)my_row * src.row_bytes + 16 * my_unit;
+    auto block = [&](int i) { return D == 128 ? (wave >> 1) + 2 * i : wave; };
+    int to[2];                                                           // (swz() has period 16 rows)
 #pragma unroll
-    for (int y = 0; y < 2; ++y) to[y] = tile_off<D>(my_row, 2 * my_unit + y);
-    auto block = [&](int i) { return 16 * ((D == 128 ? wave >> 1 : wave) + STEP / 16 * i); };      // first key of the lane's block in the tile
-    constexpr int GROUPS = WHOLE ? 1 : 4;
+    for (int y = 0; y < 2; ++y) to[y] = tile_off<D>(my_row, 2 * my_unit + y) + (D == 128 ? wave >> 1 : wave) * (16 * 2 * D);
     i32x4 pages = {0, 0, 0, 0}, next_pages = pages;
-    float k_scale[LOADS], v_scale[LOADS];
+    int k_scale[LOADS], v_scale[LOADS];              // (in vector registers: there are too few scalar ones, and their loads would have to be waited for early)
     i32x4 k_raw[LOADS], v_raw[LOADS];
-    unsigned coming_hidden = 0;                      // blocks of 16 keys of the tile in the registers that are hidden as a whole
+    unsigned coming_hidden = 0;                      // blocks of the tile in the registers that are hidden as a whole
+    // (addresses of the lane, in vector registers)
+    const CF_GLOBAL char *k_lane = (const CF_GLOBAL char *)src.k + my_off, *v_lane = (const CF_GLOBAL char *)src.v + my_off;
+    const CF_GLOBAL int *k_scale_lane = (const CF_GLOBAL int *)src.k_scales, *v_scale_lane = (const CF_GLOBAL int *)src.v_scales;
+    asm volatile("" : "+v"(k_lane), "+v"(v_lane), "+v"(k_scale_lane), "+v"(v_scale_lane));
+    auto my_page = [&](const i32x4 &p, int i) {
+        return WHOLE ? p[0] : D == 128 ? (wave < 2 ? p[2 * i] : p[2 * i + 1]) : wave < 2 ? (wave == 0 ? p[0] : p[1]) : wave == 2 ? p[2] : p[3];
+    };
     auto find_pages = [&](int start, i32x4 &p) {
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) p[g] = src.entry(start + 16 * g);
     };
     auto load = [&](int start) {
-        coming_hidden = 0;
+        bool plain = start + BN - 1 <= src.last;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) coming_hidden |= (unsigned)src.none(pages[WHOLE ? 0 : g], start + 16 * g) << g;
+        for (int g = 0; g < GROUPS; ++g) plain = plain && src.is_page(pages[g]);
+        coming_hidden = 0;
+        if (!plain) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) coming_hidden |= (unsigned)src.none(pages[WHOLE ? 0 : g], start + 16 * g) << g;
+        }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int b = block(i), key = start + b;
-            const int page = WHOLE ? pages[0] : D == 128 ? (wave < 2 ? pages[2 * i] : pages[2 * i + 1]) : wave < 2 ? (wave == 0 ? pages[0] : pages[1]) : wave == 2 ? pages[2] : pages[3];
-            const bool none = src.none(page, key);
-            const int64_t at = none ? 0 : src.offset(page, key);
-            src.scales<1>(page, key, &k_scale[i], &v_scale[i]);
-            const unsigned off = none ? 16 * my_unit : (unsigned)min(my_row + STEP * i - b, src.room(key)) * src.row_bytes + 16 * my_unit;
-            k_raw[i] = *(const i32x4 *)(uniform(none ? (const char *)zeros : src.k + at) + off);
-            v_raw[i] = *(const i32x4 *)(uniform(none ? (const char *)zeros : src.v + at) + off);
+            const int key = start + 16 * block(i);
+            const int page = my_page(pages, i);
+            if (plain) {
+                const int64_t at = src.offset(page, key), scale = src.scale_at(page, key);
+                k_raw[i] = *(const CF_GLOBAL i32x4 *)(k_lane + at), v_raw[i] = *(const CF_GLOBAL i32x4 *)(v_lane + at);
+                k_scale[i] = k_scale_lane[scale], v_scale[i] = v_scale_lane[scale];
+            } else {
+                const bool none = src.none(page, key);
+                const int64_t at = none ? 0 : src.offset(page, key), scale = none ? 0 : src.scale_at(page, key);
+                const int64_t back = (int64_t)(my_row - min(my_row, none ? 0 : src.room(key))) * src.row_bytes;
+                const CF_GLOBAL char *k = k_lane + at - back, *v = v_lane + at - back;
+                k_raw[i] = *(const CF_GLOBAL i32x4 *)(none ? (const CF_GLOBAL char *)zeros : k), v_raw[i] = *(const CF_GLOBAL i32x4 *)(none ? (const CF_GLOBAL char *)zeros : v);
+                k_scale[i] = k_scale_lane[scale], v_scale[i] = v_scale_lane[scale];
+            }
         }
     };
     auto convert = [&](char *stage) {
+        if (coming_hidden != 0) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                k_scale[i] = factor(k_scale[i], coming_hidden, block(i)), v_scale[i] = factor(v_scale[i], coming_hidden, block(i));
+        }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-                *(bf16x8 *)(stage + STEP * i * 2 * D + to[y]) = numbers(k_raw[i][2 * y], k_raw[i][2 * y + 1], k_scale[i], k_scale[i]);
-                *(bf16x8 *)(stage + TILE + STEP * i * 2 * D + to[y]) = numbers(v_raw[i][2 * y], v_raw[i][2 * y + 1], v_scale[i], v_scale[i]);
+                *(bf16x8 *)(stage + 32 * i * 2 * D + to[y]) = numbers(k_raw[i][2 * y], k_raw[i][2 * y + 1], k_scale[i], k_scale[i]);
+                *(bf16x8 *)(stage + TILE + 32 * i * 2 * D + to[y]) = numbers(v_raw[i][2 * y], v_raw[i][2 * y + 1], v_scale[i], v_scale[i]);
             }
     };
     find_pages(tiles.start(first), pages);
@@ -471,13 +497,15 @@ __device__ __forceinline__ void many_rows8(const Paged8Args &c, const TileRows &
     auto do_tile = [&](int n, const char *stage, char *next) {
         const int start = tiles.start(n);
         const unsigned hid = hidden;
+        // (the table's entries are asked for before the conversion and waited for behind it: with scalar loads in flight no LDS read can be waited
+        // for but all of them)
+        pages = next_pages;
+        if (n + 3 < end) find_pages(tiles.start(n + 3), next_pages);
         if (n + 1 < end) {
             convert(next);
             hidden = coming_hidden;
         }
-        pages = next_pages;
         if (n + 2 < end) load(tiles.start(n + 2));
-        if (n + 3 < end) find_pages(tiles.start(n + 3), next_pages);
         scalar_loads_done();
         if (rows > 0 && start <= highest && (start + BN > lowest + 1 - mask.window || start < mask.sinks)) {
             f32x4 s[BN / 16][2];
