@@ -83,19 +83,26 @@ struct Dma8 {
             lane_off[i] = (unsigned)r * row_bytes + unit16[i];
         }
     }
-    // src: the group's first row; room: its rows that may be read, less one; rows behind them read the last of these
+    // src: the group's first row
     template <int GROUP>
-    __device__ __forceinline__ void issue(const char *src, int room, char *tile, int row0) const
+    __device__ __forceinline__ void issue(const char *src, char *tile, int row0) const
     {
         const __amdgpu_buffer_rsrc_t rsrc = TileDma<64, 128>::descriptor(src);
 #pragma unroll
         for (int c = 0; c < GROUP / RPI; ++c) {
             const int at = row0 / RPI + c;
-            CF_LDS void *to = (CF_LDS void *)(tile + at * 1024);
-            if (room >= GROUP - 1)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, to, 16, (int)lane_off[kind(at)], (int)(RPI * c * row_bytes), 0, 0);
-            else
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, to, 16, (int)((unsigned)min(r + RPI * c, room) * row_bytes + unit16[kind(at)]), 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (CF_LDS void *)(tile + at * 1024), 16, (int)lane_off[kind(at)], (int)(RPI * c * row_bytes), 0, 0);
+        }
+    }
+    // room: its rows that may be read, less one; rows behind them read the last of these
+    template <int GROUP>
+    __device__ __forceinline__ void issue_ragged(__amdgpu_buffer_rsrc_t rsrc, int room, char *tile, int row0) const
+    {
+#pragma unroll
+        for (int c = 0; c < GROUP / RPI; ++c) {
+            const int at = row0 / RPI + c;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (CF_LDS void *)(tile + at * 1024), 16,
+                                                     (int)((unsigned)min(r + RPI * c, room) * row_bytes + unit16[kind(at)]), 0, 0, 0);
         }
     }
 };
@@ -192,8 +199,16 @@ struct Rows8 {
         }
         settle<D, 4, QB>(s, m, l, o, pos, mask, start, lowest, highest, groups, c2);
     }
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
     __device__ __forceinline__ void values(const char *v_tile, const int (&scale)[4], const f32x4 (&s)[4][QB])
     {
+        // (all reads together: left to itself the compiler waits for each where it is used)
+        i32x2 w[2][DB];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) w[t][db] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((CF_LDS i32x2 *)(v_tile + t * (32 * D) + (tr8 ^ (db << 4))));
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             bf16x8 p[QB][3];
@@ -213,8 +228,7 @@ struct Rows8 {
             }
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
-                const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((CF_LDS i32x2 *)(v_tile + t * (32 * D) + (tr8 ^ (db << 4))));
-                const bf16x8 v = numbers(w[0], w[1], scale[2 * t], scale[2 * t + 1]);
+                const bf16x8 v = numbers(w[t][db][0], w[t][db][1], scale[2 * t], scale[2 * t + 1]);
 #pragma unroll
                 for (int n = 0; n < PP; ++n)
 #pragma unroll
@@ -222,7 +236,6 @@ struct Rows8 {
             }
         }
     }
-    typedef int i32x2 __attribute__((ext_vector_type(2)));
 };
 
 // Few rows: all of them in every wavefront, which has key tiles of its own.
@@ -250,11 +263,20 @@ __device__ __forceinline__ void few_rows8(const Paged8Args &c, const TileRows &t
     };
     // (the same number of copies whatever the pages are: they are counted)
     auto issue = [&](const char *base, int start, const int (&p)[GROUPS], char *tile) {
+        bool full = start + BN - 1 <= src.last;
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            const int key = start + KEYS * g;
-            const bool none = src.none(p[g], key);
-            dma.template issue<KEYS>(uniform(none ? (const char *)zeros : base + src.offset(p[g], key)), none ? 0 : src.room(key), tile, KEYS * g);
+        for (int g = 0; g < GROUPS; ++g) full = full && src.is_page(p[g]);
+        if (full) {
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) dma.template issue<KEYS>(base + src.offset(p[g], start + KEYS * g), tile, KEYS * g);
+        } else {
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const int key = start + KEYS * g;
+                const bool none = src.none(p[g], key);
+                dma.template issue_ragged<KEYS>(TileDma<64, 128>::descriptor(uniform(none ? (const char *)zeros : base + src.offset(p[g], key))),
+                                                none ? 0 : src.room(key), tile, KEYS * g);
+            }
         }
     };
     // vmcnt(COPIES): all but the copies issued last have landed
