@@ -593,10 +593,8 @@ __global__ __launch_bounds__(256, 2) void mfma_paged8_kernel(Paged8Args c)
     const int lowest = t.position(0), highest = t.position(t.rows - 1);
     const int keys = keys_within(highest, a.p.pages_per_seq, a.shift);
     const KeyTiles<BN, WindowMask> tiles(a.mask, lowest, keys);
-    // (BOTH: tiles of many rows are cut a third as often, for a part of them leaves four times as much to be joined)
-    const int thirds = MODE == kBoth && t.rows > FEW ? 3 : 1, per_part = a.tiles_per_part * thirds, last_part = (a.parts - 1) / thirds;
-    const int n = at_least(0, tiles.n), first = at_most(n, a.parts == 1 ? 0 : part > last_part ? n : part * per_part);
-    const int end = a.parts > 1 && part < last_part ? at_most(n, first + per_part) : n;
+    const int n = at_least(0, tiles.n), first = at_most(n, a.parts == 1 ? 0 : part * a.tiles_per_part);
+    const int end = part < a.parts - 1 ? at_most(n, first + a.tiles_per_part) : n;
     if (first >= end) {                              // no keys: what is left of the rows
         const PagedArgs &e = arguments();
         for (int x = threadIdx.x; x < t.rows && e.parts > 1; x += 256) e.part_ml[t.flat(e, x) * e.parts + part] = make_float2(-INFINITY, 0.f);
@@ -618,6 +616,7 @@ __global__ __launch_bounds__(256, 2) void mfma_paged8_kernel(Paged8Args c)
     }
 }
 
+int few_of(const cf_attn_paged_params &p) { return p.dtype == CF_FP32 ? FEW_F32 : FEW; }
 // As in attn_paged_mfma.hip.
 Mode mode_of(const cf_attn_paged_params &p)
 {
@@ -627,7 +626,7 @@ Mode mode_of(const cf_attn_paged_params &p)
 }
 int64_t tiles_most(const cf_attn_paged_params &p)
 {
-    return places_most(p.n_tokens, p.n_seqs, p.n_q_heads / p.n_kv_heads, mode_of(p) != kFew ? BM : p.dtype == CF_FP32 ? FEW_F32 : FEW);
+    return places_most(p.n_tokens, p.n_seqs, p.n_q_heads / p.n_kv_heads, mode_of(p) == kFew ? few_of(p) : BM);
 }
 
 template <typename T, int D, bool WHOLE>
@@ -655,18 +654,40 @@ hipError_t launch(const Paged8Args &c, hipStream_t s)
 
 int64_t paged8_mfma_launch_size(const PagedArgs &a) { return tiles_most(a.p) * a.p.n_kv_heads * a.parts * 256; }
 
+// Parts.  A part costs what it finds before its first keys and leaves behind its last ones, some 3 key tiles' time, and a join, 3 us and more: parts of 8 key
+// tiles at least (two to a wavefront; in fp32, whose tiles take longer, and beside chunks 4): 16 tokens behind up to 500 keys, 28/4 heads, whole 8.1 us, cut 10.3; 8 behind up to
+// 8000, 32/8, parts of 4 / 8 tiles at least 34.3 / 30.5.
+// Where all tiles see about as many keys (chunks, windows) the workgroup slots' rounds decide: of 1 .. 64 parts those whose rounds, of a part's tiles and those 3
+// each, are shortest (1000 rows behind 30000 keys, 28/4: 3 / 5 / 7 parts 565 / 541 / 488 us).
+// Single tokens whose lengths nobody knows here: enough parts for 5 rounds (us, rounds 3 / 4 / 5 / 6 / 8: 64 tokens behind up to 16384 keys, 32/8, 266 / 301 / 262 / 268 / 280; 32 up
+// to 16000 139 / 141 / 132 / 134 / 135; 128 up to 2000 85 / 85 / 73 / 73 / 101; 256 up to 4000, 16/4, D = 64, 127 / 127 / 97 / 97 / 108.  Longer parts first and short ones
+// last, in the order of the parts, gains nothing: the memory's rate, 5.3 TB/s where all sequences are equally long, is all but reached).
+// Tokens beside chunks, all cut alike: 5 rounds (us, rounds 3 / 5 / 8: 40 up to 9000 keys beside a chunk of 500, 32/8, 201 / 130 / 138; 100 up to 3000 beside three of 300
+// 151 / 142 / 181; 20 up to 20000 beside 1000, 28/4, 409 / 395 / 424; 30 up to 9000 beside 500, 64/8, 127 / 138 / 193; 60 up to 6000 beside two of 400, 16/4, D = 64, 54 / 74 /
+// 67; with chunks cut a third as often, as in attn_paged_mfma.hip, at 8 rounds 126, 234, 457, 260, 81).
 void cut_paged8_mfma(PagedArgs &a)
 {
     const cf_attn_paged_params &p = a.p;
-    const int64_t capacity = (int64_t)p.pages_per_seq * p.page_size, G = p.n_q_heads / p.n_kv_heads;
+    const int64_t capacity = (int64_t)p.pages_per_seq * p.page_size, G = p.n_q_heads / p.n_kv_heads, slots = 512;
     int64_t keys = p.max_kv_len > 0 ? std::min<int64_t>(p.max_kv_len, capacity) : capacity;
     int64_t tiles = (keys + BN - 1) / BN;
     if (p.window > 0) tiles = std::min(tiles, ((int64_t)p.window + BM / G) / BN + 2 + ((int64_t)a.mask.sinks + BN - 1) / BN);
-    const int64_t groups = tiles_most(p) * p.n_kv_heads, slots = 512;
     const Mode mode = mode_of(p);
-    const int64_t rounds = mode == kMany ? 1 : mode == kFew ? 5 : 8, enough = mode == kMany ? 1 : 4;
-    const int64_t parts = std::min<int64_t>({(rounds * slots + groups - 1) / groups, (tiles + 3) / 4, kMostParts});
-    a.parts = groups >= enough * slots ? 1 : (int)std::max<int64_t>(1, parts);
+    const int64_t rows = mode == kFew ? few_of(p) : BM, groups = std::max<int64_t>(p.n_seqs, (p.n_tokens * G + rows - 1) / rows) * p.n_kv_heads;      // (tiles that there are at least)
+    const int64_t least = mode == kFew && p.dtype == CF_BF16 ? 8 : 4, most = std::min<int64_t>((tiles + least - 1) / least, kMostParts);
+    auto rounds_of = [&](int64_t parts) { return (groups * parts + slots - 1) / slots; };
+    int64_t parts = 1;
+    if (groups < (mode == kMany ? 1 : 4) * slots) {
+        if (mode == kMany || (mode == kFew && p.window > 0)) {
+            auto time = [&](int64_t n) { return rounds_of(n) * ((tiles + n - 1) / n + 3) + (n > 1 ? 3 : 0); };
+            for (int64_t n = 2; n <= most; ++n)
+                if (time(n) < time(parts)) parts = n;
+        } else {
+            const int64_t places = tiles_most(p) * p.n_kv_heads;
+            parts = std::min((5 * slots + places - 1) / places, most);
+        }
+    }
+    a.parts = (int)std::max<int64_t>(1, parts);
     a.tiles_per_part = (int)((tiles + a.parts - 1) / a.parts);
 }
 
