@@ -18,6 +18,7 @@ struct TurnArgs {
     int64_t table_stride, page_stride;
     int pages, shift, n_pages;
     int per_group;               // heads
+    int stream;                  // a call so large that its results go past the caches
     TurnTensor t[3];             // without heads: none
     __host__ __device__ int all_groups() const { return t[0].groups + t[1].groups + t[2].groups; }
     void group();                // chooses the groups of heads
@@ -32,9 +33,9 @@ TurnArgs turn_args(const cf_rotation *r, int D, int n_tokens, int n_seqs, const 
 void queries_of(TurnArgs &a, const cf_append_rotation *r, int dtype);
 void pages_of(TurnArgs &a, const cf_kv_append_params *p);
 
-// Unit u of a row, of group `group` of the heads of all tensors.
-template <bool INTERLEAVED>
-__device__ __forceinline__ void turn_group(const TurnArgs &a, int row, int u, int position, int seq, int group)
+// Unit u of a row, of group `group` of the heads of all tensors.  where(seq, position): finds them.
+template <bool INTERLEAVED, bool STREAM, typename Where>
+__device__ __forceinline__ void turn_group(const TurnArgs &a, int row, int u, int group, Where where)
 {
     int i = 0;
     if (group >= a.t[0].groups) {
@@ -42,18 +43,34 @@ __device__ __forceinline__ void turn_group(const TurnArgs &a, int row, int u, in
         if (group >= a.t[1].groups) group -= a.t[1].groups, i = 2;
     }
     const TurnTensor &t = a.t[i];
-    const Unit unit(u, a.rot, INTERLEAVED);
-    int64_t y_at = row * t.y_tok;
-    if (t.paged) {
+    const Unit unit(u, 16 << a.units_shift, a.rot, INTERLEAVED);
+    const int h0 = group * a.per_group;
+    int seq = 0, position = 0;
+    auto place = [&]() -> int64_t {
+        where(seq, position);
+        if (!t.paged) return row * t.y_tok;
         const PageTable table{a.table + (int64_t)seq * a.table_stride, a.pages, a.shift, a.n_pages};
         const int page = table.page_of(position);
-        if (page < 0) return;
-        y_at = (int64_t)page * a.page_stride + (int64_t)table.row_in_page(position) * t.y_tok;
-    }
-    Turn turn;
-    if (t.turned && unit.turned) turn.set(a.inv_freq + 8 * u, max(position, 0), a.inverse);
-    const int h0 = group * a.per_group;
-    turn_heads<INTERLEAVED>(t, turn, unit, row, y_at, h0, min(h0 + a.per_group, t.n_heads));
+        return page < 0 ? -1 : (int64_t)page * a.page_stride + (int64_t)table.row_in_page(position) * t.y_tok;
+    };
+    turn_heads<INTERLEAVED, STREAM>(t, unit, row, h0, min(h0 + a.per_group, t.n_heads), place,
+                                    [&](Turn &turn) { turn.set(a.inv_freq, unit, max(position, 0), a.inverse); });
+}
+
+// Rows of workgroups of 256 lanes, a lane to a unit, of which `end` are some.
+template <bool INTERLEAVED, bool STREAM>
+__device__ __forceinline__ void turn_rows(const TurnArgs &a, int end, int group)
+{
+    const int row = blockIdx.x * (256 >> a.units_shift) + (threadIdx.x >> a.units_shift), first = __builtin_amdgcn_readfirstlane(row);
+    if (first >= end) return;
+    const int r = min(row, end - 1);                 // (all lanes look for the sequences)
+    const int seq_of_row = sequence_of(a.cu, a.n_seqs, first, r);
+    if (row >= end) return;
+    turn_group<INTERLEAVED, STREAM>(a, row, threadIdx.x & ((1 << a.units_shift) - 1), group, [&](int &seq, int &position) {
+        seq = seq_of_row;
+        const NewRows rows(a.cu[seq], a.cu[seq + 1], a.chunk ? a.lens[seq + 1] - a.lens[seq] : a.lens[seq]);
+        position = rows.position(row - rows.q0);
+    });
 }
 
 }  // namespace cf

@@ -66,7 +66,7 @@ __device__ __forceinline__ void add_to_block(const Append8Args &a, int end, int 
 
     const int u = lane % UNITS;
     const bool turned = !values && a.turn.inv_freq != nullptr;
-    const Unit unit(u, turned ? a.turn.rot : 0, INTERLEAVED);
+    const Unit unit(u, D, turned ? a.turn.rot : 0, INTERLEAVED);
     float e0[PASSES][8], e1[PASSES][8];
     bool fresh[PASSES];
     float most = 0.f;
@@ -77,8 +77,9 @@ __device__ __forceinline__ void add_to_block(const Append8Args &a, int end, int 
         fresh[i] = key >= blocks.begin && key < blocks.end && row < end;
         if (fresh[i]) {
             const T *from = (const T *)(values ? a.v : a.k) + (int64_t)row * a.kv_tok + (int64_t)h * a.kv_head;
-            load8(from + unit.at[0], e0[i]);
-            load8(from + unit.at[1], e1[i]);
+            Eight<T> w0, w1;
+            w0.load(from + unit.at[0]), w1.load(from + unit.at[1]);
+            w0.get(e0[i]), w1.get(e1[i]);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) e0[i][e] = e1[i][e] = 0.f;
@@ -86,10 +87,10 @@ __device__ __forceinline__ void add_to_block(const Append8Args &a, int end, int 
     }
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
-        if (turned && unit.turned && fresh[i]) {
+        if (turned && unit.any() && fresh[i]) {
             Turn turn;
-            turn.set(a.turn.inv_freq + 8 * u, key0 + STEP * i + lane / UNITS, false);
-            turn.apply<INTERLEAVED>(e0[i], e1[i]);
+            turn.set(a.turn.inv_freq, unit, key0 + STEP * i + lane / UNITS, false);
+            turn.apply<INTERLEAVED>(unit, e0[i], e1[i]);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -124,14 +125,9 @@ __device__ __forceinline__ void add_to_block(const Append8Args &a, int end, int 
 template <typename T, int D, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void append8_kernel(Append8Args a)
 {
-    constexpr int UNITS = D / 16;
     const int end = min(a.turn.n_tokens, a.turn.cu[a.turn.n_seqs]);
     if ((int)blockIdx.y < a.turn.t[0].groups) {
-        const int row = blockIdx.x * (256 / UNITS) + threadIdx.x / UNITS, first = __builtin_amdgcn_readfirstlane(row);
-        if (first >= end) return;
-        const int r = min(row, end - 1), seq = sequence_of(a.turn.cu, a.turn.n_seqs, first, r);
-        const NewRows rows(a.turn.cu[seq], a.turn.cu[seq + 1], a.turn.lens[seq]);
-        if (row < end) turn_group<INTERLEAVED>(a.turn, row, threadIdx.x % UNITS, rows.position(r - rows.q0), seq, blockIdx.y);
+        turn_rows<INTERLEAVED, false>(a.turn, end, blockIdx.y);
         return;
     }
     const int which = blockIdx.y - a.turn.t[0].groups, place = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));

@@ -9,18 +9,10 @@ namespace cf {
 namespace {
 
 // A lane a unit of a row (rotation.h) of the heads of a group; a group of heads to each blockIdx.y.
-template <bool INTERLEAVED>
+template <bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(256) void turn_rows_kernel(TurnArgs a)
 {
-    const int row = blockIdx.x * (256 >> a.units_shift) + (threadIdx.x >> a.units_shift), u = threadIdx.x & ((1 << a.units_shift) - 1);
-    const int end = min(a.n_tokens, a.cu[a.n_seqs]), first = __builtin_amdgcn_readfirstlane(row);
-    if (first >= end) return;
-    const int r = min(row, end - 1), seq = sequence_of(a.cu, a.n_seqs, first, r);
-    const int keys = a.chunk ? a.lens[seq + 1] - a.lens[seq] : a.lens[seq];
-    const NewRows rows(a.cu[seq], a.cu[seq + 1], keys);
-    const int position = rows.position(r - rows.q0);
-    if (row >= end) return;
-    turn_group<INTERLEAVED>(a, row, u, position, seq, blockIdx.y);
+    turn_rows<INTERLEAVED, STREAM>(a, min(a.n_tokens, a.cu[a.n_seqs]), blockIdx.y);
 }
 
 }  // namespace
@@ -29,8 +21,8 @@ hipError_t launch_turn_rows(const TurnArgs &a, hipStream_t s)
 {
     const int rows = 256 >> a.units_shift;
     const dim3 grid((unsigned)(((int64_t)a.n_tokens + rows - 1) / rows), (unsigned)a.all_groups());
-    if (a.interleaved) turn_rows_kernel<true><<<grid, 256, 0, s>>>(a);
-    else turn_rows_kernel<false><<<grid, 256, 0, s>>>(a);
+    if (a.interleaved) a.stream ? turn_rows_kernel<true, true><<<grid, 256, 0, s>>>(a) : turn_rows_kernel<true, false><<<grid, 256, 0, s>>>(a);
+    else a.stream ? turn_rows_kernel<false, true><<<grid, 256, 0, s>>>(a) : turn_rows_kernel<false, false><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -110,8 +102,9 @@ void TurnArgs::group()
     int heads = 0;
     for (TurnTensor &x : t) heads += x.n_heads;
     const int64_t blocks = ((int64_t)n_tokens + (256 >> units_shift) - 1) / (256 >> units_shift);
-    per_group = (int)std::min<int64_t>(16, std::max<int64_t>(1, blocks * heads / 2048));
+    per_group = (int)std::min<int64_t>(16, std::max<int64_t>(1, blocks * heads / 1024));
     for (TurnTensor &x : t) x.group(per_group);
+    stream = blocks * heads >= 2048 && (interleaved || rot == 16 << units_shift);
 }
 
 }  // namespace cf
