@@ -122,23 +122,28 @@ __device__ __forceinline__ void add_to_block(const Append8Args &a, int end, int 
     if (lane == 0 && !(older && exponent == had)) *scale = power8(exponent);
 }
 
-template <typename T, int D, bool INTERLEAVED>
+template <typename T, int D, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(256) void append8_kernel(Append8Args a)
 {
     const int end = min(a.turn.n_tokens, a.turn.cu[a.turn.n_seqs]);
     if ((int)blockIdx.y < a.turn.t[0].groups) {
-        turn_rows<INTERLEAVED, false>(a.turn, end, blockIdx.y);
+        turn_rows<INTERLEAVED, STREAM>(a.turn, end, blockIdx.y);
         return;
     }
     const int which = blockIdx.y - a.turn.t[0].groups, place = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     if (place < (int)block_places(end, a.turn.n_seqs)) add_to_block<T, D, INTERLEAVED>(a, end, place, which & 1, which >> 1);
 }
 
+template <typename T, int D, bool STREAM>
+void launch(const Append8Args &a, dim3 grid, hipStream_t s)
+{
+    if (a.turn.interleaved) append8_kernel<T, D, true, STREAM><<<grid, 256, 0, s>>>(a);
+    else append8_kernel<T, D, false, STREAM><<<grid, 256, 0, s>>>(a);
+}
 template <typename T, int D>
 void launch(const Append8Args &a, dim3 grid, hipStream_t s)
 {
-    if (a.turn.interleaved) append8_kernel<T, D, true><<<grid, 256, 0, s>>>(a);
-    else append8_kernel<T, D, false><<<grid, 256, 0, s>>>(a);
+    a.turn.stream ? launch<T, D, true>(a, grid, s) : launch<T, D, false>(a, grid, s);
 }
 
 }  // namespace

@@ -102,9 +102,9 @@ void TurnArgs::group()
     int heads = 0;
     for (TurnTensor &x : t) heads += x.n_heads;
     const int64_t blocks = ((int64_t)n_tokens + (256 >> units_shift) - 1) / (256 >> units_shift);
-    per_group = (int)std::min<int64_t>(16, std::max<int64_t>(1, blocks * heads / 1024));
+    per_group = (int)std::min<int64_t>(16, std::max<int64_t>(1, blocks * heads / 512));
     for (TurnTensor &x : t) x.group(per_group);
-    stream = blocks * heads >= 2048 && (interleaved || rot == 16 << units_shift);
+    stream = blocks * heads >= 1024;
 }
 
 }  // namespace cf
