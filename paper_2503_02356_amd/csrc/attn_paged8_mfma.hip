@@ -239,12 +239,12 @@ struct Rows8 {
 };
 
 // Few rows: all of them in every wavefront, which has key tiles of its own.
-// WHOLE: a page holds 64 keys or more, so that a key tile has one base, else one for each 16 keys.
-template <typename T, int D, int QB, bool WHOLE>
+// GROUPS: of a key tile, each in one page: 1 where a page holds 64 keys or more, 2 of 32, 4 of 16.
+template <typename T, int D, int QB, int GROUPS>
 __device__ __forceinline__ void few_rows8(const Paged8Args &c, const TileRows &t, const KeyTiles<BN, WindowMask> &tiles, int first, int end, int keys, int part,
                                           char *k_stage, char *v_stage)
 {
-    constexpr int TILE = BN * D, COPIES = TILE / 1024, GROUPS = WHOLE ? 1 : 4, KEYS = BN / GROUPS;
+    constexpr int TILE = BN * D, COPIES = TILE / 1024, KEYS = BN / GROUPS;
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : 2;
     const PagedArgs &a = c.a;
@@ -261,21 +261,29 @@ __device__ __forceinline__ void few_rows8(const Paged8Args &c, const TileRows &t
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) src.scales<KEYS / kBlock8>(p[g], start + KEYS * g, k + KEYS / kBlock8 * g, v + KEYS / kBlock8 * g);
     };
+    // Where a tile's groups stand, and whether all of them are there as a whole.
+    int64_t at[GROUPS];
+    bool full;
+    auto find_groups = [&](int start, const int (&p)[GROUPS]) {
+        full = start + BN - 1 <= src.last;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            full = full && src.is_page(p[g]);
+            at[g] = src.offset(p[g], start + KEYS * g);
+        }
+    };
     // (the same number of copies whatever the pages are: they are counted)
     auto issue = [&](const char *base, int start, const int (&p)[GROUPS], char *tile) {
-        bool full = start + BN - 1 <= src.last;
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) full = full && src.is_page(p[g]);
         if (full) {
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) dma.template issue<KEYS>(base + src.offset(p[g], start + KEYS * g), tile, KEYS * g);
+            for (int g = 0; g < GROUPS; ++g) dma.template issue<KEYS>(base + at[g], tile, KEYS * g);
         } else {
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) {
                 const int key = start + KEYS * g;
                 const bool none = src.none(p[g], key);
-                dma.template issue_ragged<KEYS>(TileDma<64, 128>::descriptor(uniform(none ? (const char *)zeros : base + src.offset(p[g], key))),
-                                                none ? 0 : src.room(key), tile, KEYS * g);
+                dma.template issue_ragged<KEYS>(TileDma<64, 128>::descriptor(uniform(none ? (const char *)zeros : base + at[g])), none ? 0 : src.room(key), tile,
+                                                KEYS * g);
             }
         }
     };
@@ -296,6 +304,7 @@ __device__ __forceinline__ void few_rows8(const Paged8Args &c, const TileRows &t
     if (u < end) {
         find_pages(tiles.start(u), pages);
         if (u + 4 < end) find_pages(tiles.start(u + 4), next_pages);
+        find_groups(tiles.start(u), pages);
         issue(src.k, tiles.start(u), pages, k_tile);
         issue(src.v, tiles.start(u), pages, v_tile);
         find_scales(tiles.start(u), pages, k_scale, v_scale);
@@ -323,7 +332,7 @@ __device__ __forceinline__ void few_rows8(const Paged8Args &c, const TileRows &t
         // (keys behind the last one are those of later rows, or behind the table's last column, where groups end)
         unsigned hidden = 0;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) hidden |= (unsigned)src.none(pages[WHOLE ? 0 : g], start + 16 * g) << g;
+        for (int g = 0; g < 4; ++g) hidden |= (unsigned)src.none(pages[g * GROUPS / 4], start + 16 * g) << g;
         int after[GROUPS] = {};
         int k_next[4] = {}, v_next[4] = {};
         if (more) find_scales(tiles.start(u + 4), next_pages, k_next, v_next);
@@ -335,6 +344,7 @@ __device__ __forceinline__ void few_rows8(const Paged8Args &c, const TileRows &t
         for (int g = 0; g < 4; ++g) k_scale[g] = factor(k_scale[g], hidden, g), v_scale[g] = factor(v_scale[g], hidden, g);
         r.scores(k_tile, k_scale, mask, start, lowest, highest, hidden, c2, s);
         if (more) {
+            find_groups(tiles.start(u + 4), next_pages);
             reads_done();
             issue(src.k, tiles.start(u + 4), next_pages, k_tile);
             wait_older();                            // V is there
@@ -574,7 +584,7 @@ __device__ __forceinline__ void many_rows8(const Paged8Args &c, const TileRows &
 
 // MODE: kFew: tiles of FEW rows (FEW_F32 in fp32), kMany: of BM rows, kBoth: of BM rows, by what a tile holds.
 enum Mode { kFew, kMany, kBoth };
-template <typename T, int D, Mode MODE, bool WHOLE>
+template <typename T, int D, Mode MODE, int GROUPS>
 __global__ __launch_bounds__(256, 2) void mfma_paged8_kernel(Paged8Args c)
 {
     // Separate arrays: the compiler must see that what is written to one does not touch what is read from the other.
@@ -607,12 +617,12 @@ __global__ __launch_bounds__(256, 2) void mfma_paged8_kernel(Paged8Args c)
         return;
     }
     if constexpr (F32) {
-        few_rows8<T, D, 1, WHOLE>(c, t, tiles, first, end, keys, part, stage_a, stage_b);
+        few_rows8<T, D, 1, GROUPS>(c, t, tiles, first, end, keys, part, stage_a, stage_b);
     } else if (MODE == kMany || (MODE == kBoth && t.rows > FEW)) {
-        many_rows8<D, WHOLE>(c, t, tiles, first, end, keys, part, stage_a, stage_b);
+        many_rows8<D, GROUPS == 1>(c, t, tiles, first, end, keys, part, stage_a, stage_b);
     } else if constexpr (MODE != kMany) {
-        if (t.rows > 16) few_rows8<T, D, 2, WHOLE>(c, t, tiles, first, end, keys, part, stage_a, stage_b);
-        else few_rows8<T, D, 1, WHOLE>(c, t, tiles, first, end, keys, part, stage_a, stage_b);
+        if (t.rows > 16) few_rows8<T, D, 2, GROUPS>(c, t, tiles, first, end, keys, part, stage_a, stage_b);
+        else few_rows8<T, D, 1, GROUPS>(c, t, tiles, first, end, keys, part, stage_a, stage_b);
     }
 }
 
@@ -629,17 +639,17 @@ int64_t tiles_most(const cf_attn_paged_params &p)
     return places_most(p.n_tokens, p.n_seqs, p.n_q_heads / p.n_kv_heads, mode_of(p) == kFew ? few_of(p) : BM);
 }
 
-template <typename T, int D, bool WHOLE>
+template <typename T, int D, int GROUPS>
 hipError_t launch(const Paged8Args &c, hipStream_t s)
 {
     const dim3 grid((unsigned)(tiles_most(c.a.p) * c.a.p.n_kv_heads * c.a.parts));
     if constexpr (sizeof(T) == 4) {
-        mfma_paged8_kernel<T, D, kFew, WHOLE><<<grid, 256, 0, s>>>(c);
+        mfma_paged8_kernel<T, D, kFew, GROUPS><<<grid, 256, 0, s>>>(c);
     } else {
         switch (mode_of(c.a.p)) {
-            case kFew: mfma_paged8_kernel<T, D, kFew, WHOLE><<<grid, 256, 0, s>>>(c); break;
-            case kMany: mfma_paged8_kernel<T, D, kMany, WHOLE><<<grid, 256, 0, s>>>(c); break;
-            default: mfma_paged8_kernel<T, D, kBoth, WHOLE><<<grid, 256, 0, s>>>(c);
+            case kFew: mfma_paged8_kernel<T, D, kFew, GROUPS><<<grid, 256, 0, s>>>(c); break;
+            case kMany: mfma_paged8_kernel<T, D, kMany, GROUPS == 1 ? 1 : 4><<<grid, 256, 0, s>>>(c); break;
+            default: mfma_paged8_kernel<T, D, kBoth, GROUPS><<<grid, 256, 0, s>>>(c);
         }
     }
     return hipGetLastError();
@@ -647,7 +657,7 @@ hipError_t launch(const Paged8Args &c, hipStream_t s)
 template <typename T, int D>
 hipError_t launch(const Paged8Args &c, hipStream_t s)
 {
-    return c.a.p.page_size >= BN ? launch<T, D, true>(c, s) : launch<T, D, false>(c, s);
+    return c.a.p.page_size >= BN ? launch<T, D, 1>(c, s) : c.a.p.page_size == 32 ? launch<T, D, 2>(c, s) : launch<T, D, 4>(c, s);
 }
 
 }  // namespace
