@@ -1,11 +1,14 @@
 """Key/value pages of many sequences, and the forward passes of a chunk plan over them (evaluating or serving what has been trained).
 
-Memory placement and descriptors only -- every arithmetic step runs inside cf_attn_paged_fwd, every copy inside cf_kv_append.
+Memory placement and descriptors only -- every arithmetic step runs inside cf_attn_paged_fwd and cf_attn_paged8_fwd, every copy inside cf_kv_append,
+cf_kv_append_rotated and cf_kv_append8.
 The runner's state buffers hold a split sequence's keys and values in one contiguous piece of its full length, for as long as gradients
 are to be added to it.  Forward passes alone need no such piece: here a sequence takes pages from a pool as it grows, in any order, gives them
 back when it is done, and with a window those that no later query sees, so that a window bounds the pages that a sequence of any length holds.  (Its
 row of the table, 4 bytes a page, stays as long as the sequence, and goes to the GPU with every call.)
 """
+import math
+
 import numpy as np
 import torch
 
@@ -17,13 +20,22 @@ class PagedCache:
 
     window, n_sinks: of every call (0: a query sees all keys before it); pages behind the window of a sequence's next token are given back
     as soon as the tokens up to it have attended.
+    eight_bits: keys and values are held in 8 bits, with a power of two for each 16 tokens of a page and head (k_scales, v_scales); dtype is that of the
+    tensors that attend() takes.
+    rotation (binding.make_rotation): attend() rotates keys and queries by their positions; without it they come rotated, where they are to be.
     A call lays its tables out on the host and copies them: a program that captures its steps into a graph keeps tables of its own and makes the two
-    calls of the binding (cf_kv_append, cf_attn_paged_fwd) itself."""
+    calls of the binding (cf_kv_append, cf_attn_paged_fwd, or those of their kind) itself."""
 
-    def __init__(self, n_pages, page_size, n_kv_heads, head_dim, dtype=torch.bfloat16, device="cuda:0", window=0, n_sinks=0):
+    def __init__(self, n_pages, page_size, n_kv_heads, head_dim, dtype=torch.bfloat16, device="cuda:0", window=0, n_sinks=0, eight_bits=False, rotation=None):
         self.page_size, self.window, self.n_sinks, self.dev = int(page_size), int(window), int(n_sinks), torch.device(device)
-        self.k_pages = torch.empty((n_pages, page_size, n_kv_heads, head_dim), dtype=dtype, device=self.dev)
+        self.dtype, self.eight_bits, self.rotation = dtype, bool(eight_bits), rotation
+        self.k_pages = torch.empty((n_pages, page_size, n_kv_heads, head_dim), dtype=torch.float8_e4m3fn if eight_bits else dtype, device=self.dev)
         self.v_pages = torch.empty_like(self.k_pages)
+        if eight_bits:
+            if page_size % B.CF_KV8_BLOCK:
+                raise ValueError(f"pages of {page_size} tokens do not hold whole blocks of {B.CF_KV8_BLOCK}")
+            self.k_scales = torch.empty((n_pages, n_kv_heads, page_size // B.CF_KV8_BLOCK), dtype=torch.float32, device=self.dev)
+            self.v_scales = torch.empty_like(self.k_scales)
         self.free = list(range(n_pages - 1, -1, -1))
         self.seqs = {}                               # name -> [length, pages (-1: given back)]
         self.peak_pages = 0
@@ -104,11 +116,29 @@ class PagedCache:
         n = len(names)
         cu, kv_lens, block_table = desc[:n + 1], desc[n + 1:2 * n + 1], desc[2 * n + 1:].view(table.shape)
         o = torch.empty_like(q) if sum(counts) == q.shape[0] else torch.zeros_like(q)
-        append = B.make_kv_append_params(k, v, self.k_pages, self.v_pages, cu, kv_lens, block_table)
-        attention = B.make_paged_params(q, self.k_pages, self.v_pages, o, lse, cu, kv_lens, block_table,
-                                        scale if scale is not None else q.shape[2] ** -0.5, max_kv_len=int(lens.max()), window=self.window,
-                                        n_sinks=self.n_sinks)
-        B.cf_kv_append(append)
+        where, scale = (cu, kv_lens, block_table), scale if scale is not None else q.shape[2] ** -0.5
+        how = dict(max_kv_len=int(lens.max()), window=self.window, n_sinks=self.n_sinks)
+        turn, queries = None, q
+        if self.rotation is not None:
+            queries = torch.empty_like(q)            # (the caller's stay)
+            turn = B.make_append_rotation(self.rotation, q, queries)
+        if self.eight_bits:
+            assert q.dtype == self.dtype
+            if not math.isfinite(scale) or (turn is None and (q.data_ptr() % 16 or any(s * q.element_size() % 16 for s in q.stride()[:2]))):
+                # (the append may round older rows again: what the attention would refuse is refused before)
+                raise ValueError("q must be 16-byte aligned, with strides that are, and scale finite")
+            cache = (self.k_pages, self.v_pages, self.k_scales, self.v_scales)
+            append = B.make_kv_append8_params(k, v, *cache, *where)
+            attention = B.make_paged8_params(queries, *cache, o, lse, *where, scale, **how)
+            B.cf_kv_append8(append, turn)
+            B.cf_attn_paged8_fwd(attention)
+            return o
+        append = B.make_kv_append_params(k, v, self.k_pages, self.v_pages, *where)
+        attention = B.make_paged_params(queries, self.k_pages, self.v_pages, o, lse, *where, scale, **how)
+        if turn is None:
+            B.cf_kv_append(append)
+        else:
+            B.cf_kv_append_rotated(append, turn)
         B.cf_attn_paged_fwd(attention)
         return o
 

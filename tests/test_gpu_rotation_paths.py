@@ -1,0 +1,155 @@
+"""Rotation and the cache of 8 bits as they are used: training a sequence in slices, evaluating it over pages, serving token by token."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2503_02356_amd import binding as B
+from paper_2503_02356_amd.paged import PagedCache, plan_forward
+from tests import plain_cache8 as P
+from tests import plain_window as W
+from tests.test_gpu_paged import ints
+from tests.test_gpu_rotation import frequencies
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, FP32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(autouse=True)
+def _seeded():
+    torch.manual_seed(77)
+
+
+def rel(a, b):
+    return float((a.double() - b).norm() / b.norm())
+
+
+@pytest.mark.parametrize("dtype,D,rot,interleaved", [(FP32, 64, 64, False), (FP32, 128, 64, True), (BF16, 128, 128, False), (BF16, 64, 32, True)])
+def test_training_in_slices(dtype, D, rot, interleaved):
+    """A sequence in three slices: queries and keys rotated (keys into the state), attention, its backward in descending order, dQ of each slice and dK of the
+    whole state rotated back -- against the gradients of rotation and attention of the unsplit sequence in 64 bits.
+    fp32: as the attention's own bound (1e-5 of the norm); bf16: the rounding of rotated queries and keys, of o, dQ, dK and of the products, at most half
+    a step 2^-9 in the mean each, of six tensors."""
+    L, Hq, Hkv, cuts = 330, 4, 2, [0, 100, 228, 330]
+    scale, f = float(np.float32(1 / np.sqrt(D))), frequencies(rot)
+    q, k, v, d_o = (torch.randn(L, H, D, device=DEV).to(dtype) for H in (Hq, Hkv, Hkv, Hq))
+    r = B.make_rotation(f, interleaved)
+    state_k, state_v = torch.empty(L, Hkv, D, device=DEV, dtype=dtype), v.clone()
+    d_kv = torch.zeros(2, L, Hkv, D, device=DEV)
+    o, lse, qr, d_qr, d_q = torch.empty_like(q), [], torch.empty_like(q), torch.empty_like(q), torch.empty_like(q)
+    for a, b in zip(cuts, cuts[1:]):
+        cu_q, cu_k = ints([0, b - a]), ints([0, b])
+        B.cf_rotate(B.make_rotate_params(cu_q, cu_k, r, q=(q[a:b], qr[a:b]), k=(k[a:b], state_k[a:b])))
+        lse.append(torch.empty(Hq, b - a, device=DEV))
+        B.cf_attn_fwd(B.make_fwd_params(qr[a:b], state_k[:b], state_v[:b], o[a:b], lse[-1], cu_q, cu_k, scale))
+    for i in (2, 1, 0):
+        a, b = cuts[i], cuts[i + 1]
+        cu_q, cu_k = ints([0, b - a]), ints([0, b])
+        p = B.make_fwd_params(qr[a:b], state_k[:b], state_v[:b], o[a:b], lse[i], cu_q, cu_k, scale)
+        ws = torch.empty(B.cf_attn_bwd_workspace_bytes(p), dtype=torch.uint8, device=DEV)
+        B.cf_attn_bwd(B.make_bwd_params(p, d_o[a:b], d_qr[a:b], d_kv[0, :b], d_kv[1, :b], ws))
+        B.cf_rotate(B.make_rotate_params(cu_q, cu_k, r, q=(d_qr[a:b], d_q[a:b]), inverse=True))
+    whole = ints([0, L])
+    d_k = torch.empty(L, Hkv, D, device=DEV, dtype=dtype)
+    B.cf_rotate(B.make_rotate_params(whole, whole, r, k=(d_kv[0], d_k), inverse=True))
+    in_place = d_kv[0].clone()
+    B.cf_rotate(B.make_rotate_params(whole, whole, r, k=(in_place, in_place), inverse=True))
+    torch.cuda.synchronize()
+    assert bool(torch.equal(in_place.to(dtype), d_k))
+
+    pos = torch.arange(L, device=DEV)
+    qd, kd, vd = (x.double().requires_grad_() for x in (q, k, v))
+    qt, kt = (P.turned(x, pos, f, interleaved)[0] for x in (qd, kd))
+    seen = W.visible(L, L, 0, 0, DEV)
+    want = torch.stack([torch.softmax((qt[:, h] @ kt[:, h // 2].T * scale).masked_fill(~seen, -float("inf")), 1) @ vd[:, h // 2] for h in range(Hq)], 1)
+    want.backward(d_o.double())
+    bound = 1e-5 if dtype == FP32 else 6 * 2.0 ** -9
+    for name, got, ref in (("o", o, want.detach()), ("dq", d_q, qd.grad), ("dk", d_k, kd.grad), ("dv", d_kv[1], vd.grad)):
+        assert rel(got, ref) < bound, (name, rel(got, ref))
+
+
+LENS, C = [700, 40, 130, 260, 1, 16], 256
+
+
+def rows_of(Hq, Hkv, D, dtype):
+    return {s: [torch.randn(n, H, D, device=DEV).to(dtype) for H in (Hq, Hkv, Hkv)] for s, n in enumerate(LENS)}
+
+
+@pytest.mark.parametrize("window", [0, 90])
+@pytest.mark.parametrize("dtype,D", [(BF16, 128), (FP32, 64)])
+def test_a_plan_over_pages_that_rotate(dtype, D, window):
+    """The same as over pages without, from queries and keys that cf_rotate has rotated as in training, bit by bit."""
+    plan, Hq, Hkv = B.cf_build_chunks(LENS, C), 4, 2
+    data, r = rows_of(Hq, Hkv, D, dtype), B.make_rotation(frequencies(D))
+    results = []
+    for turned in (False, True):
+        cache = PagedCache(80, 16, Hkv, D, dtype, window=window, rotation=None if turned else r)
+
+        def inputs(c):
+            segs = plan.chunk_segments(c)
+            q, k, v = (torch.cat([data[s][i][a:a + n] for s, a, n in segs]) for i in range(3))
+            if turned:
+                cu_q, cu_k = ints(np.cumsum([0] + [n for _, _, n in segs])), ints(np.cumsum([0] + [a + n for _, a, n in segs]))
+                B.cf_rotate(B.make_rotate_params(cu_q, cu_k, r, q=(q, q), k=(k, k)))
+            return q, k, v
+        results.append([(o.clone(), lse.clone()) for _, o, lse in plan_forward(plan, cache, inputs)])
+        assert cache.used_pages() == 0
+    torch.cuda.synchronize()
+    for (o, lse), (o2, lse2) in zip(*results):
+        assert bool(torch.equal(o, o2)) and bool(torch.equal(lse, lse2))
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (90, 3)])
+@pytest.mark.parametrize("dtype,D,rotated", [(BF16, 128, True), (BF16, 64, False), (FP32, 64, True)])
+def test_serving_from_8_bits(dtype, D, rotated, window, sinks):
+    """Prompts, then tokens, of three conversations: what every call gives is attention over what the cache holds at that time, and what it holds are the
+    (rotated) keys and values, off by the roundings to e4m3 (2^-4 of the value, of which several follow each other as a block fills up: 0.05 of the
+    norm is over twice what one leaves)."""
+    Hq, Hkv, page = 4, 2, 32
+    f = frequencies(D // 2)
+    cache = PagedCache(60, page, Hkv, D, dtype, window=window, n_sinks=sinks, eight_bits=True, rotation=B.make_rotation(f) if rotated else None)
+    true = {name: ([], []) for name in "abc"}
+    scale = float(np.float32(1 / np.sqrt(D)))
+    steps = [(["a"], [300]), (["b", "c"], [5, 77])] + [(["a", "b", "c"], [1, 1, 1])] * 20 + [(["b", "a"], [33, 1])]
+    for names, counts in steps:
+        T, pad = sum(counts), len(counts) % 2
+        q, k, v = (torch.randn(T + pad, H, D, device=DEV).to(dtype) * (1.5 if H == Hkv else 1.0) for H in (Hq, Hkv, Hkv))
+        keep = q.clone()
+        before = cache.lengths()
+        lse = torch.empty(Hq, T + pad, device=DEV)
+        o = cache.attend(names, counts, q, k, v, lse=lse)
+        torch.cuda.synchronize()
+        assert bool(torch.equal(q, keep)) and bool((o[T:] == 0).all())
+        row = 0
+        for name, n in zip(names, counts):
+            b = before.get(name, 0)
+            pos = torch.arange(b, b + n, device=DEV)
+            turn = lambda x: P.turned(x, pos, f)[0] if rotated else x.double()
+            true[name][0].append(turn(k[row:row + n]))
+            true[name][1].append(v[row:row + n].double())
+            length, pages = cache.seqs[name]
+            at = torch.arange(length, device=DEV)
+            number = torch.tensor(pages, device=DEV)[at // page]
+            held = number >= 0                       # (pages that this call's window left behind have been given back since)
+            number = number.clamp(min=0)
+            ks, vs = (P.values(c.view(torch.uint8)[number, at % page], s[number, :, at % page // 16][:, :, None])
+                      for c, s in ((cache.k_pages, cache.k_scales), (cache.v_pages, cache.v_scales)))
+            for got, want in ((ks, torch.cat(true[name][0])), (vs, torch.cat(true[name][1]))):
+                assert rel(got[held], want[held]) < 0.05
+            seen = W.visible(n, length, window, sinks, DEV)
+            whole = (seen & ~held[None]).sum(1) == 0
+            qt = turn(q[row:row + n]).to(dtype).double()
+            for h in range(Hq):
+                ref = W.attention(qt[:, h], torch.where(held[:, None], ks[:, h // 2], 0.0), torch.where(held[:, None], vs[:, h // 2], 0.0), scale, seen)
+                ref.update(keys=length, rows=1)
+                # the rotated queries' own rounding may fall the other way in the last of 24 bits: half a step of one element of q
+                tol = W.tolerances(ref, dtype, D, dtype == BF16)
+                flip = 2.0 ** -8 if dtype == BF16 else 2.0 ** -20
+                off = (o[row:row + n, h].double() - ref["o"]).abs()
+                assert bool((off <= tol["o"] + flip * ref["o_abs"])[whole].all()), (name, h, float((off - tol["o"])[whole].max()))
+                assert bool(((lse[h, row:row + n].double() - ref["lse"]).abs() <= tol["lse"] + flip * ref["score_abs"])[whole].all())
+            row += n
+    assert cache.k_pages.dtype == torch.float8_e4m3fn
+    for name in "abc":
+        cache.close(name)
+    assert cache.used_pages() == 0
