@@ -478,8 +478,8 @@ int cf_rotate(const cf_rotate_params *p, void *hip_stream);
 
 /*
  * cf_kv_append with the rotation on the way: keys go into the pages rotated by their positions, values as they are, and the same rows' queries,
- * where q is not NULL, into q_out (in place or not, as in cf_rotate).  A row whose key is dropped for its position has its query turned by the
- * position, a negative one by position 0.  Everything else as in cf_kv_append; q has its dtype.
+ * where q is not NULL, into q_out (in place or not, as in cf_rotate), those of rows whose keys are dropped too (a negative position: turned by
+ * position 0).  Everything else as in cf_kv_append; q has its dtype.
  */
 typedef struct {
     cf_rotation rotation;

@@ -573,6 +573,7 @@ def make_kv_append_params(k, v, k_pages, v_pages, cu_q, kv_lens, block_table):
     p = KvAppendParams()
     _fill_append(p, k, v, k_pages, v_pages, cu_q, kv_lens, block_table)
     p._keepalive = (k, v, k_pages, v_pages, cu_q, kv_lens, block_table)      # see make_fwd_params
+    p._rows = (k.shape[0], k.shape[2], k.dtype, k.device)
     return p
 
 
@@ -644,20 +645,21 @@ def make_append_rotation(rotation, q=None, q_out=None):
         r.n_q_heads, r.q, r.q_stride_tok, r.q_stride_head = t.n_heads, t.x, t.x_stride_tok, t.x_stride_head
         r.q_out, r.q_out_stride_tok, r.q_out_stride_head = t.y, t.y_stride_tok, t.y_stride_head
     r._keepalive = (rotation, q, q_out)
+    inv_freq = rotation._keepalive[0]
+    r._rows = None if q is None else (q.shape[0], q.shape[2], q.dtype, q.device)
+    r._device = inv_freq.device
     return r
 
 
 def _check_append_rotation(append, rotation):
     """The queries are the rows of the call's keys (an address says nothing of it)."""
-    k, q = append._keepalive[0], rotation._keepalive[1]
-    k = k if not isinstance(k, C.Structure) else k._keepalive[0]
-    assert rotation.rotation.rot_dim <= k.shape[2] and rotation._keepalive[0]._keepalive[0].device == k.device
-    assert q is None or (q.shape[0] == k.shape[0] and q.shape[2] == k.shape[2] and q.dtype == k.dtype and q.device == k.device)
+    rows = append._rows
+    assert rotation._device == rows[3] and (rotation._rows is None or rotation._rows == rows)
 
 
 def cf_kv_append_rotated(params, rotation, stream=None):
     """params: make_kv_append_params; rotation: make_append_rotation."""
-    if hasattr(params, "_keepalive"):
+    if hasattr(params, "_rows"):
         _check_append_rotation(params, rotation)
     _check(lib().cf_kv_append_rotated(C.byref(params), C.byref(rotation), _stream_for(params, stream)))
 
@@ -680,6 +682,7 @@ def make_kv_append8_params(k, v, k_pages, v_pages, k_scales, v_scales, cu_q, kv_
     _fill_append(p.a, k, v, k_pages, v_pages, cu_q, kv_lens, block_table)
     p.k_scales, p.v_scales, p.scale_stride_page, p.scale_stride_head = k_scales.data_ptr(), v_scales.data_ptr(), *_scale_strides(k_scales)
     p._keepalive = (k, v, k_pages, v_pages, k_scales, v_scales, cu_q, kv_lens, block_table)      # see make_fwd_params
+    p._rows = (k.shape[0], k.shape[2], k.dtype, k.device)
     return p
 
 
@@ -692,7 +695,7 @@ def _scale_strides(t):
 
 def cf_kv_append8(params, rotation=None, stream=None):
     """params: make_kv_append8_params; rotation: make_append_rotation, or None."""
-    if rotation is not None and hasattr(params, "_keepalive"):
+    if rotation is not None and hasattr(params, "_rows"):
         _check_append_rotation(params, rotation)
     _check(lib().cf_kv_append8(C.byref(params), C.byref(rotation) if rotation is not None else None, _stream_for(params, stream)))
 
