@@ -40,6 +40,8 @@ class Batch8(Batch):
                 size = torch.exp(0.7 * torch.randn(x.shape[0], x.shape[1] // 16, 1, x.shape[2], 1, generator=g, device=DEV))
                 x = (x.float().reshape(x.shape[0], -1, 16, *x.shape[2:]) * size).reshape(x.shape)
                 codes, scales = P.quantised(x)
+                nobody = torch.isnan(x).reshape(x.shape[0], -1, 16, *x.shape[2:]).all(4).all(2).transpose(1, 2)
+                scales = torch.where(nobody, NAN, scales).contiguous()        # (what nobody has written has no scale either)
             if heads_first:
                 codes, scales = codes.transpose(1, 2).contiguous().transpose(1, 2), scales.transpose(0, 1).contiguous().transpose(0, 1)
             self.codes.append(codes)
