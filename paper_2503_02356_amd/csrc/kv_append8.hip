@@ -111,7 +111,7 @@ __device__ __forceinline__ void add_to_block(const Append8Args &a, int end, int 
             *at = uint4{again4(w.x, factor), again4(w.y, factor), again4(w.z, factor), again4(w.w, factor)};
         }
     }
-    const float factor = power8(-exponent);
+    const float factor = inverse8(exponent);
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
         if (!fresh[i]) continue;

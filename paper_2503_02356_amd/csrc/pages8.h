@@ -30,14 +30,16 @@ CF_BOTH int exponent_for(float most)
     const unsigned u = bits_of(most);
     return at_least(kLeast8, (int)(u >> 23) - 127 - 8 + ((u & 0x7fffff) > 0x600000));
 }
-// The exponent that a scale in the pages stands for, as far as a block that is added to may keep it.
-CF_BOTH int exponent_of(float scale) { return at_most(kMost8, at_least(kLeast8, (int)(bits_of(scale) >> 23 & 255) - 127)); }
+// The exponent that a scale in the pages stands for, -127 .. 127, or 128: NaN.
+CF_BOTH int exponent_of(float scale) { return (int)(bits_of(scale) >> 23 & 255) - 127; }
 // What a scale multiplies with: its exponent alone (as the conversion instructions of the matrix kernels take it).
 CF_BOTH float factor8(float scale)
 {
     const unsigned e = bits_of(scale) >> 23 & 255;
     return float_of(e == 0 ? 0x400000u : e == 255 ? 0x7fc00000u : e << 23);
 }
+// 2^-e, by which elements are multiplied that a block of exponent e, kLeast8 .. 128, takes (128: NaN whatever they are).
+CF_BOTH float inverse8(int e) { return factor8(power8(-at_most(127, e))); }
 
 // The blocks of 16 keys that a sequence's new rows go into, [first, first + n), and those of all sequences in one list: sequence g's from
 // first_block_place(cu_seqlens_q[g], g) on.  Lq rows touch (Lq + 14) / 16 + 1 blocks at most, and two sequences' places are Lq / 16 + 2,

@@ -233,3 +233,24 @@ def test_pages_beyond_32_bits():
         P.append(small_c, small_s, x.double(), [(20, 260)], np.array([[0, 1]]), 2)
         assert bool(torch.equal(c[n - 1], small_c[0])) and bool(torch.equal(c[n - 2], small_c[1])) and not bool(c[:n - 2].any())
         assert bool(torch.equal(s[n - 2:], small_s.flip(0)))
+
+
+@pytest.mark.parametrize("D,dtype", [(64, FP32), (128, BF16)])
+def test_a_block_keeps_any_larger_scale_and_no_smaller_one(D, dtype):
+    """Scales that no append writes: above those that finite elements need the block keeps them, below the least it is rounded to that."""
+    for e in (127, 126, 125, 121, 120, -111, -112, -126, -127):
+        c = Cache8([(1, 5), (3, 20), (2, 2)], 2, D, dtype, seed=e + 200)
+        big = e > 0
+        c.k *= 2.0 ** 118 if big else 2.0 ** -116
+        c.v *= 2.0 ** 115 if big else 2.0 ** -104
+        for s in c.scales:
+            s.fill_(0.0 if e == -127 else 2.0 ** e)
+        want = [x.clone() for x in c.codes], [s.fill_(2.0 ** e) if e > -127 else s.double().fill_(2.0 ** -127) for s in (x.clone() for x in c.scales)]
+        for codes, scales, x in zip(*want, (c.k, c.v)):
+            P.append(codes, scales, x.double(), c.seqs, c.table_host, c.n_pages)
+        B.cf_kv_append8(c.params())
+        torch.cuda.synchronize()
+        for got, scales, w, ws in zip(c.codes, c.scales, *want):
+            assert P.same_numbers(got, w), e
+            kept = ws.double() == 2.0 ** e                   # (what is as it was may be 0 still)
+            assert bool(torch.equal(scales[~kept].double(), ws[~kept].double())) and bool((scales[kept] == (0.0 if e == -127 else 2.0 ** e)).all()), e

@@ -40,7 +40,10 @@ static int powers()
         if (power8(e) != std::ldexp(1.f, e) || exponent_of(power8(e)) != e || factor8(power8(e)) != power8(e) || power8(-e) * power8(e) != 1.f) return std::printf("2^%d\n", e), 1;
     // whatever stands in the pages
     for (float x : {0.f, -1.5f, 3.f, INFINITY, -INFINITY, NAN, 1e-45f, 3e38f})
-        if (exponent_of(x) < kLeast8 || exponent_of(x) > kMost8) return 1;
+        if (exponent_of(x) < -127 || exponent_of(x) > 128 || (exponent_of(x) < 128 && factor8(x) != std::ldexp(1.f, exponent_of(x)))) return 1;
+    for (int e = kLeast8; e <= 127; ++e)
+        if (inverse8(e) != std::ldexp(1.f, -e)) return std::printf("2^-%d\n", e), 1;
+    if (inverse8(128) != std::ldexp(1.f, -127)) return 1;
     return factor8(3.f) == 2.f && factor8(-1.5f) == 1.f && factor8(0.f) == std::ldexp(1.f, -127) && std::isnan(factor8(INFINITY)) && std::isnan(factor8(NAN)) ? 0 : 1;
 }
 
