@@ -8,6 +8,17 @@
 //   few rows   every wavefront has all of them and takes every fourth tile of 64 keys, copied as bytes into its own part of LDS (16 KB of keys
 //              and values are in flight or in use, as there), and converts its operands itself.
 // fp32: queries and P enter as three bf16 operands each, which make up all 24 bits of them; tiles of 16 rows, all of them few.
+// (Products of bytes would take half the instructions, but queries would have to be bytes too, and the sums of the scaled 16x16x128 one are off by up to 6e-5 of
+// the sum of their sizes: too much for scores, whose error is lse's.)
+//
+// Many rows: bound by the matrix instructions and the vector ones between them (a wavefront's key tile takes 257 vector instructions, 224 of them the bf16
+// kernel's, and 64 products).  8192 rows behind 24576 keys, 28/4 heads x 128: 3.22 ms, 1047 TFLOP/s (the bf16 kernel over a cache of twice the bytes 2.88 ms; a large
+// matrix product 1234).  Steps there, ms: LDS writes spread over the banks 4.14 -> 3.50; lane addresses instead of descriptors, which with the tile's scalars were
+// more than the scalar registers, 3.50 -> 3.23; the conversion in front of the scores 3.23, between scores and values 3.56, behind the values 3.32;
+// raised priority around the products 3.37, around the conversion 3.24; eight wavefronts of 256 rows 3.38.
+// Few rows: bound by memory.  64 tokens behind up to 16384 keys, 32/8 x 128: 257 us with its join for 1.22 GB (4.7 TB/s; 64 equally long sequences 5.3, a large copy's rate
+// 5.1).  Keys straight into registers 309 (a row's 64 bytes an instruction: twice the requests); 16-row tiles of five wavefronts 1 % slower, at D = 64 four wavefronts a SIMD
+// 4 %.  One token behind 4097 keys, 28/4: 9.5 us and 4.1 for the join.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -239,7 +250,8 @@ struct Rows8 {
 };
 
 // Few rows: all of them in every wavefront, which has key tiles of its own.
-// GROUPS: of a key tile, each in one page: 1 where a page holds 64 keys or more, 2 of 32, 4 of 16.
+// GROUPS: of a key tile, each in one page: 1 where a page holds 64 keys or more, 2 of 32, 4 of 16.  (256 tokens with a window of 1024 in pages of 32, 16/4 heads x 64,
+// with their append: 59.5 us with 4, 56.5 with 2.)
 template <typename T, int D, int QB, int GROUPS>
 __device__ __forceinline__ void few_rows8(const Paged8Args &c, const TileRows &t, const KeyTiles<BN, WindowMask> &tiles, int first, int end, int keys, int part,
                                           char *k_stage, char *v_stage)

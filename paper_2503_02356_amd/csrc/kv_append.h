@@ -21,7 +21,7 @@ struct TurnArgs {
     int stream;                  // a call so large that its results go past the caches
     TurnTensor t[3];             // without heads: none
     __host__ __device__ int all_groups() const { return t[0].groups + t[1].groups + t[2].groups; }
-    void group();                // chooses the groups of heads
+    void group(int workgroups);  // chooses the groups of heads
 };
 hipError_t launch_turn_rows(const TurnArgs &a, hipStream_t s);
 

@@ -2,7 +2,13 @@
 //
 // A wavefront has a block of 16 keys of one head, of K or of V: the new rows that fall into it (a lane a unit of 16 elements of one or two
 // of them, rotation.h), their largest element, the block's scale, the older rows again where that grows, the new rows' numbers.  No other wavefront
-// writes the block.  blockIdx.y: groups of query heads, which are turned by the way (a lane a unit of a row), then K and V of each head.
+// writes the block, so a scale is found, compared and written without atomics, the same in every run.  blockIdx.y: groups of query heads, which are turned
+// by the way (a lane a unit of a row), then K and V of each head.
+//
+// Bound by memory where a call is large, 2 bytes read and 1 written of each element (and the queries both ways), and by its launch and three trips to memory, one behind
+// the other (lists, table, rows), where it is small.  Measured, us: 8192 tokens of 28 + 4 heads x 128, 27 with their queries (5.2 TB/s: what it reads is partly in the
+// caches); one token of each of 256 sequences 7.9.  Queries in fewer workgroups than alone (rotate.hip), 128, since the blocks fill the chip with theirs (128 / 256 /
+// 512: 4000 rows of 28 + 4 heads 13.0 / 13.0 / 15.4, of 16 + 4 x 64 8.4 / 9.2 / 10.9, 256 tokens of 64 + 8 11.3 / 11.6 / 13.2).
 #include <hip/hip_runtime.h>
 
 #include "kv_append.h"
@@ -165,7 +171,7 @@ extern "C" int cf_kv_append8(const cf_kv_append8_params *p8, const cf_append_rot
     a.turn = cf::turn_args(r ? &r->rotation : nullptr, p->head_dim, p->n_tokens, p->n_seqs, p->cu_seqlens_q, p->kv_lens);
     cf::queries_of(a.turn, r, p->dtype);
     cf::pages_of(a.turn, p);
-    a.turn.group();
+    a.turn.group(128);
     a.k = p->k, a.v = p->v, a.kv_tok = p->kv_stride_tok, a.kv_head = p->kv_stride_head;
     a.k_pages = (char *)p->k_pages, a.v_pages = (char *)p->v_pages, a.page_tok = p->page_stride_tok, a.page_head = p->page_stride_head;
     a.k_scales = p8->k_scales, a.v_scales = p8->v_scales, a.scale_page = p8->scale_stride_page, a.scale_head = p8->scale_stride_head;

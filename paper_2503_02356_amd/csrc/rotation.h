@@ -4,6 +4,7 @@
 // cosines of its pairs once and turns its unit of several heads with them; since both elements of a pair are a lane's own, x may be y.
 // The angle p * inv_freq / 2 pi is taken in 64 bits and its whole turns are dropped there: what is left has an error of 2^-25 of a turn
 // (its rounding to fp32) for any position.  (In fp32 an angle of 2^18 radians would be off by 2^-6.)
+// Bound by memory, one read and one write of every element, where a call is large; by its launch and one trip to memory where it is small.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -55,7 +56,7 @@ struct Eight {
     }
 };
 
-// STREAM: past the caches (results of a large call, which would only push its inputs out).
+// STREAM: past the caches (results of a large call, which would only push its inputs out; figures at TurnArgs::group).
 template <bool STREAM, typename V>
 __device__ __forceinline__ void put(V *p, V w)
 {
@@ -148,7 +149,7 @@ struct TurnTensor {
 template <typename In, typename Out, bool INTERLEAVED, bool STREAM, typename Place, typename Angles>
 __device__ __forceinline__ void turn_heads(const TurnTensor &t, const Unit &unit, int64_t row, int h0, int h1, Place place, Angles angles)
 {
-    constexpr int AT_ONCE = 4;
+    constexpr int AT_ONCE = 4;                       // (us, 2 / 4 / 8: 32768 rows of 64 + 8 heads there and back 549 / 537 / 553, one token into pages 8.5 / 7.6 / 10.1)
     const In *x = (const In *)t.x + row * t.x_tok;
     const bool turned = t.turned && unit.any();
     if (!turned && t.x == t.y) return;               // in place

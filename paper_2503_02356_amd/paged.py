@@ -7,8 +7,6 @@ are to be added to it.  Forward passes alone need no such piece: here a sequence
 back when it is done, and with a window those that no later query sees, so that a window bounds the pages that a sequence of any length holds.  (Its
 row of the table, 4 bytes a page, stays as long as the sequence, and goes to the GPU with every call.)
 """
-import math
-
 import numpy as np
 import torch
 
@@ -124,9 +122,9 @@ class PagedCache:
             turn = B.make_append_rotation(self.rotation, q, queries)
         if self.eight_bits:
             assert q.dtype == self.dtype
-            if not math.isfinite(scale) or (turn is None and (q.data_ptr() % 16 or any(s * q.element_size() % 16 for s in q.stride()[:2]))):
+            if not abs(scale) < 3.4e38 or (turn is None and (q.data_ptr() % 16 or any(s * q.element_size() % 16 for s in q.stride()[:2]))):
                 # (the append may round older rows again: what the attention would refuse is refused before)
-                raise ValueError("q must be 16-byte aligned, with strides that are, and scale finite")
+                raise ValueError("q must be 16-byte aligned, with strides that are, and scale a finite fp32 number")
             cache = (self.k_pages, self.v_pages, self.k_scales, self.v_scales)
             append = B.make_kv_append8_params(k, v, *cache, *where)
             attention = B.make_paged8_params(queries, *cache, o, lse, *where, scale, **how)

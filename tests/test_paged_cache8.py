@@ -19,7 +19,7 @@ def test_a_refused_call_leaves_the_sequences_as_they_were(names, counts, error):
     assert state(cache) == before
 
 
-@pytest.mark.parametrize("change", [dict(scale=float("nan")), dict(scale=float("inf")), dict(q="offset"), dict(q="stride"), dict(q="dtype")])
+@pytest.mark.parametrize("change", [dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=1e39), dict(q="offset"), dict(q="stride"), dict(q="dtype")])
 def test_what_the_attention_would_refuse_comes_before_the_append(change, monkeypatch):
     from paper_2503_02356_amd import binding as B
     called = []
