@@ -61,21 +61,12 @@ __device__ __forceinline__ void add_to_block(const Append8Args &a, int end, int 
     const int x = place - first_block_place(begin, seq);
     if (x >= blocks.n) return;
     const int key0 = (blocks.first + x) * kBlock8;
-    const PageTable table{a.turn.table + (int64_t)seq * a.turn.table_stride, a.turn.pages, a.turn.shift, a.turn.n_pages};
-    const int page = table.page_of(key0);
-    if (page < 0) return;
-    const int in_page = table.row_in_page(key0);
-    float *scale = (values ? a.v_scales : a.k_scales) + (int64_t)page * a.scale_page + (int64_t)h * a.scale_head + in_page / kBlock8;
-    char *to = (values ? a.v_pages : a.k_pages) + (int64_t)page * a.turn.page_stride + (int64_t)in_page * a.page_tok + (int64_t)h * a.page_head;
-    const bool older = blocks.begin > key0;                  // (the new rows are the block's from there on)
-    const float scale_before = older ? *scale : 0.f;
-
     const int u = lane % UNITS;
     const bool turned = !values && a.turn.inv_freq != nullptr;
     const Unit unit(u, D, turned ? a.turn.rot : 0, INTERLEAVED);
-    float e0[PASSES][8], e1[PASSES][8];
+    // The new rows' loads first: they do not wait for the table.
+    Eight<T> w0[PASSES], w1[PASSES];
     bool fresh[PASSES];
-    float most = 0.f;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
         const int key = key0 + STEP * i + lane / UNITS;
@@ -83,16 +74,23 @@ __device__ __forceinline__ void add_to_block(const Append8Args &a, int end, int 
         fresh[i] = key >= blocks.begin && key < blocks.end && row < end;
         if (fresh[i]) {
             const T *from = (const T *)(values ? a.v : a.k) + (int64_t)row * a.kv_tok + (int64_t)h * a.kv_head;
-            Eight<T> w0, w1;
-            w0.load(from + unit.at[0]), w1.load(from + unit.at[1]);
-            w0.get(e0[i]), w1.get(e1[i]);
+            w0[i].load(from + unit.at[0]), w1[i].load(from + unit.at[1]);
         } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) e0[i][e] = e1[i][e] = 0.f;
+            w0[i] = w1[i] = {};
         }
     }
+    const PageTable table{a.turn.table + (int64_t)seq * a.turn.table_stride, a.turn.pages, a.turn.shift, a.turn.n_pages};
+    const int page = table.page_of(key0), in_page = table.row_in_page(key0);
+    float *scale = (values ? a.v_scales : a.k_scales) + (int64_t)max(page, 0) * a.scale_page + (int64_t)h * a.scale_head + in_page / kBlock8;
+    char *to = (values ? a.v_pages : a.k_pages) + (int64_t)page * a.turn.page_stride + (int64_t)in_page * a.page_tok + (int64_t)h * a.page_head;
+    const bool older = blocks.begin > key0;                  // (the new rows are the block's from there on)
+    const float scale_before = older ? *scale : 0.f;
+
+    float e0[PASSES][8], e1[PASSES][8];
+    float most = 0.f;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
+        w0[i].get(e0[i]), w1[i].get(e1[i]);
         if (turned && unit.any() && fresh[i]) {
             Turn turn;
             turn.set(a.turn.inv_freq, unit, key0 + STEP * i + lane / UNITS, false);
@@ -104,6 +102,7 @@ __device__ __forceinline__ void add_to_block(const Append8Args &a, int end, int 
             most = fmaxf(most, fmaxf(p < INFINITY ? p : 0.f, q < INFINITY ? q : 0.f));
         }
     }
+    if (page < 0) return;
     most = wave_max(most);
     const int wanted = exponent_for(most), had = exponent_of(scale_before), exponent = older ? max(wanted, had) : wanted;
     if (older && exponent > had) {
