@@ -57,11 +57,11 @@ __device__ __forceinline__ void turn_group(const TurnArgs &a, int row, int u, in
                                     [&](Turn &turn) { turn.set(a.inv_freq, unit, max(position, 0), a.inverse); });
 }
 
-// Rows of workgroups of 256 lanes, a lane to a unit, of which `end` are some.
+// Workgroup `block` of 256 lanes, a lane to a unit of a row, of which there are `end`.
 template <bool INTERLEAVED, bool STREAM>
-__device__ __forceinline__ void turn_rows(const TurnArgs &a, int end, int group)
+__device__ __forceinline__ void turn_rows(const TurnArgs &a, int end, int group, int block)
 {
-    const int row = blockIdx.x * (256 >> a.units_shift) + (threadIdx.x >> a.units_shift), first = __builtin_amdgcn_readfirstlane(row);
+    const int row = block * (256 >> a.units_shift) + (threadIdx.x >> a.units_shift), first = __builtin_amdgcn_readfirstlane(row);
     if (first >= end) return;
     const int r = min(row, end - 1);                 // (all lanes look for the sequences)
     const int seq_of_row = sequence_of(a.cu, a.n_seqs, first, r);

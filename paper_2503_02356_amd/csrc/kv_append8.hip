@@ -2,12 +2,12 @@
 //
 // A wavefront has a block of 16 keys of one head, of K or of V: the new rows that fall into it (a lane a unit of 16 elements of one or two
 // of them, rotation.h), their largest element, the block's scale, the older rows again where that grows, the new rows' numbers.  No other wavefront
-// writes the block, so a scale is found, compared and written without atomics, the same in every run.  blockIdx.y: groups of query heads, which are turned
-// by the way (a lane a unit of a row), then K and V of each head.
+// writes the block, so a scale is found, compared and written without atomics, the same in every run.  blockIdx.y: workgroups of rows and groups of
+// heads of the queries (a lane a unit of a row), one behind the other in as many rows of the grid as they fill, then K and V of each head.
 //
 // Bound by memory where a call is large, 2 bytes read and 1 written of each element (and the queries both ways), and by its launch and three trips to memory, one behind
-// the other (lists, table, rows), where it is small.  Measured, us: 8192 tokens of 28 + 4 heads x 128, 27 with their queries (5.2 TB/s: what it reads is partly in the
-// caches); one token of each of 256 sequences 7.9.  Queries in fewer workgroups than alone (rotate.hip), 128, since the blocks fill the chip with theirs (128 / 256 /
+// the other (lists, table, rows), where it is small.  Measured, us: 8192 tokens of 28 + 4 heads x 128, 26 with their queries (5.5 TB/s: what it reads is partly in the
+// caches); one token of each of 256 sequences 5.5.  Queries in fewer workgroups than alone (rotate.hip), 128, since the blocks fill the chip with theirs (128 / 256 /
 // 512: 4000 rows of 28 + 4 heads 13.0 / 13.0 / 15.4, of 16 + 4 x 64 8.4 / 9.2 / 10.9, 256 tokens of 64 + 8 11.3 / 11.6 / 13.2).
 #include <hip/hip_runtime.h>
 
@@ -26,6 +26,8 @@ struct Append8Args {
     int64_t page_tok, page_head;         // bytes
     float *k_scales, *v_scales;
     int64_t scale_page, scale_head;
+    int row_blocks, query_rows;          // workgroups of rows of queries; of the grid's y, those that they fill
+    int heads_first;                     // all heads of four blocks' places one behind the other, not all places of a head
 };
 
 // Four elements times `factor`, as numbers.
@@ -43,7 +45,7 @@ __device__ __forceinline__ unsigned again4(unsigned w, float factor)
 }
 
 template <typename T, int D, bool INTERLEAVED>
-__device__ __forceinline__ void add_to_block(const Append8Args &a, int end, int place, bool values, int h)
+__device__ __forceinline__ void add_to_block(const Append8Args &a, const BlockPlaces &places, int end, int place, bool values, int h)
 {
     constexpr int UNITS = D / 16, PASSES = UNITS / 4, STEP = 64 / UNITS;     // units of a row; times that a lane has a row; rows of each time
     const int lane = threadIdx.x & 63, n = a.turn.n_seqs;
@@ -51,14 +53,14 @@ __device__ __forceinline__ void add_to_block(const Append8Args &a, int end, int 
     int lo = 0, hi = n;
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) / 64, g = lo + lane * step;
-        const unsigned long long before = __ballot(g < hi && first_block_place(cu[min(g, hi - 1)], g) <= place);
+        const unsigned long long before = __ballot(g < hi && places.first(cu[min(g, hi - 1)], g) <= place);
         lo += (63 - __clzll((long long)before)) * step;      // (lane 0 always says yes)
         hi = min(hi, lo + step);
     }
     const int seq = __builtin_amdgcn_readfirstlane(lo), begin = cu[seq];
     const NewRows rows(begin, cu[seq + 1], a.turn.lens[seq]);
     const NewBlocks blocks(rows);
-    const int x = place - first_block_place(begin, seq);
+    const int x = place - places.first(begin, seq);
     if (x >= blocks.n) return;
     const int key0 = (blocks.first + x) * kBlock8;
     const int u = lane % UNITS;
@@ -131,12 +133,19 @@ template <typename T, int D, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(256) void append8_kernel(Append8Args a)
 {
     const int end = min(a.turn.n_tokens, a.turn.cu[a.turn.n_seqs]);
-    if ((int)blockIdx.y < a.turn.t[0].groups) {
-        turn_rows<INTERLEAVED, STREAM>(a.turn, end, blockIdx.y);
+    if ((int)blockIdx.y < a.query_rows) {
+        const unsigned id = blockIdx.y * gridDim.x + blockIdx.x, group = id / (unsigned)a.row_blocks;
+        if ((int)group < a.turn.t[0].groups) turn_rows<INTERLEAVED, STREAM>(a.turn, end, (int)group, (int)(id - group * (unsigned)a.row_blocks));
         return;
     }
-    const int which = blockIdx.y - a.turn.t[0].groups, place = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    if (place < (int)block_places(end, a.turn.n_seqs)) add_to_block<T, D, INTERLEAVED>(a, end, place, which & 1, which >> 1);
+    int which = blockIdx.y - a.query_rows, four = blockIdx.x;
+    if (a.heads_first) {
+        const unsigned id = (unsigned)which * gridDim.x + blockIdx.x, heads = gridDim.y - a.query_rows;
+        four = (int)(id / heads), which = (int)(id - (unsigned)four * heads);
+    }
+    const int place = four * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const BlockPlaces places(a.turn.n_tokens, a.turn.n_seqs);
+    if (place < (int)places.all(end, a.turn.n_seqs)) add_to_block<T, D, INTERLEAVED>(a, places, end, place, which & 1, which >> 1);
 }
 
 template <typename T, int D, bool STREAM>
@@ -164,7 +173,7 @@ extern "C" int cf_kv_append8(const cf_kv_append8_params *p8, const cf_append_rot
     if (r)
         if (int rc = cf::check_append_rotation(who, r, p->dtype, p->head_dim)) return rc;
     if (int rc = cf::check_rows(who, p->n_tokens, p->head_dim)) return rc;
-    const int64_t blocks = (cf::block_places(p->n_tokens, p->n_seqs) + 3) / 4;
+    const int64_t blocks = (cf::BlockPlaces(p->n_tokens, p->n_seqs).all(p->n_tokens, p->n_seqs) + 3) / 4;
     if (blocks * 256 > 0xffffffffLL) return cf::fail(CF_EINVAL, "%s: %d sequences are more than one launch holds", who, p->n_seqs);
     cf::Append8Args a;
     a.turn = cf::turn_args(r ? &r->rotation : nullptr, p->head_dim, p->n_tokens, p->n_seqs, p->cu_seqlens_q, p->kv_lens);
@@ -174,10 +183,15 @@ extern "C" int cf_kv_append8(const cf_kv_append8_params *p8, const cf_append_rot
     a.k = p->k, a.v = p->v, a.kv_tok = p->kv_stride_tok, a.kv_head = p->kv_stride_head;
     a.k_pages = (char *)p->k_pages, a.v_pages = (char *)p->v_pages, a.page_tok = p->page_stride_tok, a.page_head = p->page_stride_head;
     a.k_scales = p8->k_scales, a.v_scales = p8->v_scales, a.scale_page = p8->scale_stride_page, a.scale_head = p8->scale_stride_head;
-    const int rows = 256 / (p->head_dim / 16), y = a.turn.t[0].groups + 2 * p->n_kv_heads;
-    if (y > 65535) return cf::fail(CF_EINVAL, "%s: %d groups of heads are more than one launch holds", who, y);
-    const int64_t row_blocks = a.turn.t[0].groups ? ((int64_t)p->n_tokens + rows - 1) / rows : 0;
-    const dim3 grid((unsigned)std::max(blocks, row_blocks), (unsigned)y);
+    const int rows = 256 / (p->head_dim / 16);
+    a.row_blocks = (int)(((int64_t)p->n_tokens + rows - 1) / rows);
+    a.query_rows = (int)(((int64_t)a.turn.t[0].groups * a.row_blocks + blocks - 1) / blocks);
+    const int64_t y = (int64_t)a.query_rows + 2 * p->n_kv_heads;
+    if (y > 65535 || y * blocks > 0x7fffffffLL) return cf::fail(CF_EINVAL, "%s: %lld rows of workgroups are more than one launch holds", who, (long long)y);
+    const dim3 grid((unsigned)blocks, (unsigned)y);
+    // us, places / heads first: 16000 rows of 28 + 4 heads x 128 46.5 / 43.7, 4000 of 64 + 8 28.2 / 25.8; of 16 + 4 x 64 16000 20.4 / 22.8, 256 tokens 5.5 / 6.5,
+    // of 64 + 8 x 128 7.5 / 10.3.
+    a.heads_first = a.turn.stream && p->head_dim == 128;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (p->dtype == CF_FP32) p->head_dim == 64 ? cf::launch<float, 64>(a, grid, s) : cf::launch<float, 128>(a, grid, s);
     else p->head_dim == 64 ? cf::launch<unsigned short, 64>(a, grid, s) : cf::launch<unsigned short, 128>(a, grid, s);

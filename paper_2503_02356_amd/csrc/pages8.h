@@ -41,11 +41,15 @@ CF_BOTH float factor8(float scale)
 // 2^-e, by which elements are multiplied that a block of exponent e, kLeast8 .. 128, takes (128: NaN whatever they are).
 CF_BOTH float inverse8(int e) { return factor8(power8(-at_most(127, e))); }
 
-// The blocks of 16 keys that a sequence's new rows go into, [first, first + n), and those of all sequences in one list: sequence g's from
-// first_block_place(cu_seqlens_q[g], g) on.  Lq rows touch (Lq + 14) / 16 + 1 blocks at most, and two sequences' places are Lq / 16 + 2,
-// rounded either way, apart.
-CF_BOTH int first_block_place(int begin, int seq) { return begin / kBlock8 + 2 * seq; }
-CF_BOTH int64_t block_places(int64_t tokens, int64_t seqs) { return tokens / kBlock8 + 2 * seqs; }
+// The blocks of 16 keys that a sequence's new rows go into, [first, first + n), and those of all sequences in one list: sequence g's from place
+// first(cu_seqlens_q[g], g) on.  Lq rows touch (Lq + 14) / 16 + 1 blocks at most, and two sequences' places are Lq / 16 + 2, rounded either way, apart; or, where
+// that makes fewer places in all (single tokens), a place for each row, since Lq rows touch no more than Lq blocks.
+struct BlockPlaces {
+    bool of_rows;
+    CF_BOTH BlockPlaces(int64_t tokens, int64_t seqs) : of_rows(tokens < tokens / kBlock8 + 2 * seqs) {}
+    CF_BOTH int first(int begin, int seq) const { return of_rows ? begin : begin / kBlock8 + 2 * seq; }
+    CF_BOTH int64_t all(int64_t tokens, int64_t seqs) const { return of_rows ? tokens : tokens / kBlock8 + 2 * seqs; }
+};
 struct NewBlocks {
     int begin, end;                      // positions of the new rows
     int first, n;

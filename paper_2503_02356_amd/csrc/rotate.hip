@@ -16,7 +16,7 @@ namespace {
 template <bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(256) void turn_rows_kernel(TurnArgs a)
 {
-    turn_rows<INTERLEAVED, STREAM>(a, min(a.n_tokens, a.cu[a.n_seqs]), blockIdx.y);
+    turn_rows<INTERLEAVED, STREAM>(a, min(a.n_tokens, a.cu[a.n_seqs]), blockIdx.y, blockIdx.x);
 }
 
 }  // namespace

@@ -254,3 +254,26 @@ def test_a_block_keeps_any_larger_scale_and_no_smaller_one(D, dtype):
             assert P.same_numbers(got, w), e
             kept = ws.double() == 2.0 ** e                   # (what is as it was may be 0 still)
             assert bool(torch.equal(scales[~kept].double(), ws[~kept].double())) and bool((scales[kept] == (0.0 if e == -127 else 2.0 ** e)).all()), e
+
+
+@pytest.mark.parametrize("D,dtype,interleaved", [(128, BF16, False), (64, BF16, True), (128, FP32, True), (64, FP32, False)])
+def test_a_large_call_does_what_its_sequences_calls_do(D, dtype, interleaved):
+    """Queries, keys and values of several thousand rows, whose launch is laid out otherwise, against a call for each sequence, bit by bit."""
+    seqs = [(1500, 1600), (3, 40), (1, 900), (2600, 2600), (0, 5), (17, 17)]
+    T, Hq, pad = sum(a for a, _ in seqs), 14, 3
+    one, two = (Cache8(seqs, 2, D, dtype, 64, seed=9, pad=pad) for _ in range(2))
+    q = torch.randn(T + pad, Hq, D, device=DEV).to(dtype)
+    rotation = B.make_rotation(frequencies(D), interleaved)
+    outs = [torch.full_like(q, 7.0) for _ in range(2)]
+    B.cf_kv_append8(one.params(), B.make_append_rotation(rotation, q, outs[0]))
+    row = 0
+    for i, (a, n) in enumerate(seqs):
+        if a:
+            rows = slice(row, row + a)
+            B.cf_kv_append8(B.make_kv_append8_params(two.k[rows], two.v[rows], *two.codes, *two.scales, ints([0, a]), ints([n]), two.table[i:i + 1]),
+                            B.make_append_rotation(rotation, q[rows], outs[1][rows]))
+        row += a
+    torch.cuda.synchronize()
+    assert bool(torch.equal(outs[0], outs[1])) and bool((outs[0][T:] == 7.0).all())
+    for x, y in zip(one.codes + one.scales, two.codes + two.scales):
+        assert bool(torch.equal(x, y))

@@ -210,3 +210,21 @@ def test_graph_of_both():
         for x, y in ((b.q, q_out), (b.k, torch.stack([b.kp[int(b.table_host[i, j // 16]), j % 16] for i, j in zip((0, 1, 1), pos.tolist())]))):
             want, tol = P.turn_tolerance(x, pos, f, False, False, FP32)
             close(y, want, tol, step)
+
+
+@pytest.mark.parametrize("D,dtype,interleaved", [(128, BF16, False), (64, BF16, True), (128, FP32, False)])
+def test_a_large_call_does_what_its_segments_calls_do(D, dtype, interleaved):
+    """Several thousand rows, whose groups of heads and stores are others, against a call for each segment, bit by bit."""
+    lens, pad = [3000, 1, 2500, 0, 70], 3
+    T = sum(lens)
+    q, k = torch.randn(T + pad, 14, D, device=DEV).to(dtype), torch.randn(T + pad, 3, D, device=DEV).to(dtype)
+    rotation, cu = B.make_rotation(frequencies(D), interleaved), np.cumsum([0] + lens)
+    cu_k = np.cumsum([0] + [n + 100 * (n > 1) for n in lens])
+    ys = [[torch.full_like(x, 7.0) for x in (q, k)] for _ in range(2)]
+    B.cf_rotate(B.make_rotate_params(ints(cu), ints(cu_k), rotation, (q, ys[0][0]), (k, ys[0][1])))
+    for a, b, n in zip(cu[:-1], cu[1:], np.diff(cu_k)):
+        if b > a:
+            B.cf_rotate(B.make_rotate_params(ints([0, b - a]), ints([0, n]), rotation, (q[a:b], ys[1][0][a:b]), (k[a:b], ys[1][1][a:b])))
+    torch.cuda.synchronize()
+    for x, y in zip(*ys):
+        assert bool(torch.equal(x, y)) and bool((x[T:] == 7.0).all())

@@ -59,13 +59,16 @@ static int places()
         }
         const int n_seqs = (int)kv.size(), T = cu.back();
         std::vector<char> done(T, 0);
-        for (int place = 0; place < block_places(T, n_seqs); ++place) {
+        BlockPlaces places(T, n_seqs);
+        if (places.all(T, n_seqs) != (T < T / 16 + 2 * n_seqs ? T : T / 16 + 2 * n_seqs)) return std::printf("places %d %d\n", T, n_seqs), 1;
+        if (n % 2) places.of_rows = rng() % 2;       // (either way is right for any call)
+        for (int place = 0; place < places.all(T, n_seqs); ++place) {
             int seq = 0;
             for (int g = 0; g < n_seqs; ++g)
-                if (first_block_place(cu[g], g) <= place) seq = g;
+                if (places.first(cu[g], g) <= place) seq = g;
             const NewRows rows(cu[seq], cu[seq + 1], kv[seq]);
             const NewBlocks blocks(rows);
-            const int x = place - first_block_place(cu[seq], seq);
+            const int x = place - places.first(cu[seq], seq);
             if (x < 0) return std::printf("place %d\n", place), 1;
             if (x >= blocks.n) continue;
             const int key0 = (blocks.first + x) * kBlock8;
