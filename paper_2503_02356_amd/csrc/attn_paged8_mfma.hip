@@ -18,7 +18,7 @@
 // raised priority around the products 3.37, around the conversion 3.24; eight wavefronts of 256 rows 3.38.
 // Few rows: bound by memory.  64 tokens behind up to 16384 keys, 32/8 x 128: 257 us with its join for 1.22 GB (4.7 TB/s; 64 equally long sequences 5.3, a large copy's rate
 // 5.1).  Keys straight into registers 309 (a row's 64 bytes an instruction: twice the requests); 16-row tiles of five wavefronts 1 % slower, at D = 64 four wavefronts a SIMD
-// 4 %.  One token behind 4097 keys, 28/4: 9.5 us and 4.1 for the join.
+// 4 %.  One token behind 4097 keys, 28/4: 7.9 us and 4.1 for the join.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -676,9 +676,11 @@ hipError_t launch(const Paged8Args &c, hipStream_t s)
 
 int64_t paged8_mfma_launch_size(const PagedArgs &a) { return tiles_most(a.p) * a.p.n_kv_heads * a.parts * 256; }
 
-// Parts.  A part costs what it finds before its first keys and leaves behind its last ones, some 3 key tiles' time, and a join, 3 us and more: parts of 8 key
-// tiles at least (two to a wavefront; in fp32, whose tiles take longer, and beside chunks 4): 16 tokens behind up to 500 keys, 28/4 heads, whole 8.1 us, cut 10.3; 8 behind up to
-// 8000, 32/8, parts of 4 / 8 tiles at least 34.3 / 30.5.
+// Parts.  A part costs what it finds before its first keys and leaves behind its last ones, some 3 key tiles' time, and a join, 3 us and more: tiles of few rows are whole up to 8
+// key tiles (two to a wavefront; us, whole / cut: one token behind 300 keys, 28/4 heads, 7.8 / 9.3, fp32, 6/2, 9.0 / 10.1, 1000 keys 11.4 / 9.3), and parts have 8 tiles at least where
+// those of 4, one to a wavefront, are more than the workgroup slots (4 / 8 at least: one token behind 4097 keys 10.1 / 11.7, 4 behind 2000 9.5 / 11.2, 16 behind 2000
+// 14.0 / 15.2, 30 with a window of 512 12.4 / 14.2; 32 behind up to 1000 15.7 / 15.0, 4 behind 8000 14.8 / 14.3; beyond the slots, 8 behind up to 8000, 32/8, 34.3 / 30.5).
+// In fp32, whose tiles take longer, and beside chunks always 4.
 // Where all tiles see about as many keys (chunks, windows) the workgroup slots' rounds decide: of 1 .. 64 parts those whose rounds, of a part's tiles and those 3
 // each, are shortest (1000 rows behind 30000 keys, 28/4: 3 / 5 / 7 parts 565 / 541 / 488 us).
 // Single tokens whose lengths nobody knows here: enough parts for 5 rounds (us, rounds 3 / 4 / 5 / 6 / 8: 64 tokens behind up to 16384 keys, 32/8, 266 / 301 / 262 / 268 / 280; 32 up
@@ -696,7 +698,8 @@ void cut_paged8_mfma(PagedArgs &a)
     if (p.window > 0) tiles = std::min(tiles, ((int64_t)p.window + BM / G) / BN + 2 + ((int64_t)a.mask.sinks + BN - 1) / BN);
     const Mode mode = mode_of(p);
     const int64_t rows = mode == kFew ? few_of(p) : BM, groups = std::max<int64_t>(p.n_seqs, (p.n_tokens * G + rows - 1) / rows) * p.n_kv_heads;      // (tiles that there are at least)
-    const int64_t least = mode == kFew && p.dtype == CF_BF16 ? 8 : 4, most = std::min<int64_t>((tiles + least - 1) / least, kMostParts);
+    const int64_t least = mode == kFew && p.dtype == CF_BF16 && groups * ((tiles + 3) / 4) > slots ? 8 : 4;
+    const int64_t most = mode == kFew && tiles <= 8 ? 1 : std::min<int64_t>((tiles + least - 1) / least, kMostParts);
     auto rounds_of = [&](int64_t parts) { return (groups * parts + slots - 1) / slots; };
     int64_t parts = 1;
     if (groups < (mode == kMany ? 1 : 4) * slots) {
