@@ -608,8 +608,15 @@ __global__ __launch_bounds__(256, 2) void mfma_paged8_kernel(Paged8Args c)
     TileRows t;
     t.G = a.p.n_q_heads / a.p.n_kv_heads;
     int id = blockIdx.x;
-    t.kh = id % a.p.n_kv_heads;                      // (fastest: an XCD keeps reading the same heads; attn_mfma_fwd.hip)
-    id /= a.p.n_kv_heads;
+    if (D == 64 && MODE != kMany && a.p.n_kv_heads % 2 == 0) {
+        // Two heads' 64 bytes are a cache line: both workgroups on one XCD (workgroups take turns on 8), one soon after the other.
+        const HeadPair pair(id, gridDim.x);
+        t.kh = pair.pair % (a.p.n_kv_heads / 2) * 2 + pair.second;
+        id = pair.pair / (a.p.n_kv_heads / 2);
+    } else {
+        t.kh = id % a.p.n_kv_heads;                  // (fastest: an XCD keeps reading the same heads; attn_mfma_fwd.hip)
+        id /= a.p.n_kv_heads;
+    }
     const int part = id % a.parts;
     if (!find_tile<ROWS>(a, id / a.parts, t)) return;
     const int lowest = t.position(0), highest = t.position(t.rows - 1);

@@ -41,6 +41,18 @@ CF_BOTH float factor8(float scale)
 // 2^-e, by which elements are multiplied that a block of exponent e, kLeast8 .. 128, takes (128: NaN whatever they are).
 CF_BOTH float inverse8(int e) { return factor8(power8(-at_most(127, e))); }
 
+// Workgroup id of `all` (an even number) does one or the other half of a pair, 8 pairs in 16 workgroups: halves are 8 workgroups apart (behind the last 16, as
+// many as are left there).
+struct HeadPair {
+    int pair, second;
+    CF_BOTH HeadPair(int id, int all)
+    {
+        const int whole = all & ~15, half = id < whole ? 8 : (all - whole) / 2, begin = id < whole ? id & ~15 : whole;
+        second = id - begin >= half;
+        pair = begin / 2 + (id - begin) - (second ? half : 0);
+    }
+};
+
 // The blocks of 16 keys that a sequence's new rows go into, [first, first + n), and those of all sequences in one list: sequence g's from place
 // first(cu_seqlens_q[g], g) on.  Lq rows touch (Lq + 14) / 16 + 1 blocks at most, and two sequences' places are Lq / 16 + 2, rounded either way, apart; or, where
 // that makes fewer places in all (single tokens), a place for each row, since Lq rows touch no more than Lq blocks.

@@ -1,5 +1,5 @@
-"""CPU run of the arithmetic of a cache of 8 bits (csrc/pages8.h): powers of two of the blocks, and that every block which a call adds to has one
-place in the launch, and only one."""
+"""CPU run of the arithmetic of a cache of 8 bits (csrc/pages8.h): powers of two of the blocks, that every block which a call adds to has one place in
+the launch, and only one, and every head of a pair one workgroup."""
 import os
 import subprocess
 
@@ -89,7 +89,23 @@ static int places()
     return 0;
 }
 
-int main() { return powers() || places(); }
+static int pairs()
+{
+    for (int all = 2; all < 200; all += 2) {
+        std::vector<int> done(all, 0);
+        for (int id = 0; id < all; ++id) {
+            const HeadPair p(id, all);
+            if (p.pair < 0 || p.pair >= all / 2 || p.second < 0 || p.second > 1 || done[2 * p.pair + p.second]++) return std::printf("%d of %d: pair %d, %d\n", id, all, p.pair, p.second), 1;
+            if (id < (all & ~15) && p.second) {
+                const HeadPair q(id - 8, all);
+                if (q.pair != p.pair || q.second) return std::printf("%d of %d: not beside %d\n", id, all, id - 8), 1;
+            }
+        }
+    }
+    return 0;
+}
+
+int main() { return powers() || places() || pairs(); }
 """
 
 
