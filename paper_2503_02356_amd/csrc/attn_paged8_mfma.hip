@@ -17,8 +17,8 @@
 // more than the scalar registers, 3.50 -> 3.23; the conversion in front of the scores 3.23, between scores and values 3.56, behind the values 3.32;
 // raised priority around the products 3.37, around the conversion 3.24; eight wavefronts of 256 rows 3.38.
 // Few rows: bound by memory.  64 tokens behind up to 16384 keys, 32/8 x 128: 257 us with its join for 1.22 GB (4.7 TB/s; 64 equally long sequences 5.3, a large copy's rate
-// 5.1).  Keys straight into registers 309 (a row's 64 bytes an instruction: twice the requests); 16-row tiles of five wavefronts 1 % slower, at D = 64 four wavefronts a SIMD
-// 4 %.  One token behind 4097 keys, 28/4: 7.9 us and 4.1 for the join.
+// 5.1).  Keys straight into registers 309 (a row's 64 bytes an instruction: twice the requests); 16-row tiles of five wavefronts 1 % slower.  D = 64: 64 tokens
+// behind 16000 keys, 16/4, 108 us (4.9 TB/s; 161 with the heads of a cache line on different XCDs, which fetches each line twice).  One token behind 4097 keys, 28/4: 7.9 us and 4.1 for the join.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -31,7 +31,7 @@ namespace {
 
 constexpr int BM = 128, BN = 64;             // rows of a tile, keys of a key tile
 constexpr int FEW = 32;                      // rows that the wavefronts share
-constexpr int FEW_F32 = 16;
+constexpr int FEWER = 16;                    // in fp32, and at D = 64 where sequences have no more (see mode_of)
 
 // Key tiles as bytes in LDS: rows of D bytes, no padding, 16-byte unit u of row r at u ^ swz8(r).  Two rows (D = 128; four at 64) cover the 64 banks.
 //   keys     ds_read_b128, lane's row = lane % 16, unit 4 s + lane / 16; served in groups of lanes 0-3, 12-15, 20-23, 24-27 and 4-11, 16-19,
@@ -594,14 +594,13 @@ __device__ __forceinline__ void many_rows8(const Paged8Args &c, const TileRows &
     for_rows_not_finite<D, 16>(r.o, scale, rows, [&](int x) { row_again8<unsigned short, D>(e8, t, x0 + x, tiles, first, end, part); });
 }
 
-// MODE: kFew: tiles of FEW rows (FEW_F32 in fp32), kMany: of BM rows, kBoth: of BM rows, by what a tile holds.
-enum Mode { kFew, kMany, kBoth };
+// MODE: kFewer, kFew: tiles of FEWER and FEW rows, kMany: of BM rows, kBoth: of BM rows, by what a tile holds.
+enum Mode { kFewer, kFew, kMany, kBoth };
 template <typename T, int D, Mode MODE, int GROUPS>
-__global__ __launch_bounds__(256, 2) void mfma_paged8_kernel(Paged8Args c)
+__global__ __launch_bounds__(256, D == 64 && MODE == kFewer ? 4 : 2) void mfma_paged8_kernel(Paged8Args c)
 {
     // Separate arrays: the compiler must see that what is written to one does not touch what is read from the other.
-    constexpr bool F32 = sizeof(T) == 4;
-    constexpr int ROWS = MODE != kFew ? BM : F32 ? FEW_F32 : FEW, STAGE = MODE == kFew ? 4 * BN * D : 2 * BN * 2 * D;
+    constexpr int ROWS = MODE == kFewer ? FEWER : MODE == kFew ? FEW : BM, STAGE = MODE == kFewer || MODE == kFew ? 4 * BN * D : 2 * BN * 2 * D;
     __shared__ __attribute__((aligned(16))) char stage_a[STAGE];
     __shared__ __attribute__((aligned(16))) char stage_b[STAGE];
     const PagedArgs &a = c.a;
@@ -635,7 +634,7 @@ __global__ __launch_bounds__(256, 2) void mfma_paged8_kernel(Paged8Args c)
         }
         return;
     }
-    if constexpr (F32) {
+    if constexpr (MODE == kFewer) {
         few_rows8<T, D, 1, GROUPS>(c, t, tiles, first, end, keys, part, stage_a, stage_b);
     } else if (MODE == kMany || (MODE == kBoth && t.rows > FEW)) {
         many_rows8<D, GROUPS == 1>(c, t, tiles, first, end, keys, part, stage_a, stage_b);
@@ -645,17 +644,29 @@ __global__ __launch_bounds__(256, 2) void mfma_paged8_kernel(Paged8Args c)
     }
 }
 
-int few_of(const cf_attn_paged_params &p) { return p.dtype == CF_FP32 ? FEW_F32 : FEW; }
-// As in attn_paged_mfma.hip.
+constexpr int64_t kSlots = 512;              // workgroups that run at once, two to a compute unit
+// Key tiles that a tile of rows sees at most, as far as the host knows.
+int64_t key_tiles(const cf_attn_paged_params &p)
+{
+    const int64_t capacity = (int64_t)p.pages_per_seq * p.page_size, keys = p.max_kv_len > 0 ? std::min<int64_t>(p.max_kv_len, capacity) : capacity;
+    const int64_t tiles = (keys + BN - 1) / BN, sinks = std::min<int64_t>(p.n_sinks, capacity);
+    return p.window > 0 ? std::min(tiles, ((int64_t)p.window + BM / (p.n_q_heads / p.n_kv_heads)) / BN + 2 + (sinks + BN - 1) / BN) : tiles;
+}
+// As in attn_paged_mfma.hip; and at D = 64, where with 16 rows a tile four workgroups have room on a compute unit, not three, such tiles in calls whose lengths are
+// latencies more than bytes (us, FEW / FEWER rows, 16/4 heads: 32 tokens behind up to 4000 keys 19.5 / 15.9, 256 behind up to 500 17.1 / 14.4, 256 with a window of 1024 37.3 /
+// 34.4; 64/8: 128 behind up to 2000 63.4 / 54.4; but 64 behind 16000 229 / 245, 16/4 109 / 115, 256 behind 4000 102 / 105; at D = 128, two either way, 32/8: 32 behind up
+// to 4000 48.6 / 48.7, 128 behind up to 2000 84.3 / 91.7).
 Mode mode_of(const cf_attn_paged_params &p)
 {
-    if (p.dtype == CF_FP32) return kFew;
     const int64_t rows = (int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads);
+    if (p.dtype == CF_FP32) return kFewer;
+    if (p.head_dim == 64 && rows <= (int64_t)FEWER * p.n_seqs && key_tiles(p) * p.n_seqs * p.n_kv_heads <= 80 * kSlots) return kFewer;
     return rows <= (int64_t)FEW * p.n_seqs ? kFew : p.n_seqs == 1 || rows >= 512 * (int64_t)p.n_seqs ? kMany : kBoth;
 }
+int rows_of(Mode mode) { return mode == kFewer ? FEWER : mode == kFew ? FEW : BM; }
 int64_t tiles_most(const cf_attn_paged_params &p)
 {
-    return places_most(p.n_tokens, p.n_seqs, p.n_q_heads / p.n_kv_heads, mode_of(p) == kFew ? few_of(p) : BM);
+    return places_most(p.n_tokens, p.n_seqs, p.n_q_heads / p.n_kv_heads, rows_of(mode_of(p)));
 }
 
 template <typename T, int D, int GROUPS>
@@ -663,9 +674,16 @@ hipError_t launch(const Paged8Args &c, hipStream_t s)
 {
     const dim3 grid((unsigned)(tiles_most(c.a.p) * c.a.p.n_kv_heads * c.a.parts));
     if constexpr (sizeof(T) == 4) {
-        mfma_paged8_kernel<T, D, kFew, GROUPS><<<grid, 256, 0, s>>>(c);
+        mfma_paged8_kernel<T, D, kFewer, GROUPS><<<grid, 256, 0, s>>>(c);
     } else {
-        switch (mode_of(c.a.p)) {
+        const Mode mode = mode_of(c.a.p);
+        if constexpr (D == 64) {
+            if (mode == kFewer) {
+                mfma_paged8_kernel<T, D, kFewer, GROUPS><<<grid, 256, 0, s>>>(c);
+                return hipGetLastError();
+            }
+        }
+        switch (mode) {
             case kFew: mfma_paged8_kernel<T, D, kFew, GROUPS><<<grid, 256, 0, s>>>(c); break;
             case kMany: mfma_paged8_kernel<T, D, kMany, GROUPS == 1 ? 1 : 4><<<grid, 256, 0, s>>>(c); break;
             default: mfma_paged8_kernel<T, D, kBoth, GROUPS><<<grid, 256, 0, s>>>(c);
@@ -683,40 +701,39 @@ hipError_t launch(const Paged8Args &c, hipStream_t s)
 
 int64_t paged8_mfma_launch_size(const PagedArgs &a) { return tiles_most(a.p) * a.p.n_kv_heads * a.parts * 256; }
 
-// Parts.  A part costs what it finds before its first keys and leaves behind its last ones, some 3 key tiles' time, and a join, 3 us and more: tiles of few rows are whole up to 8
-// key tiles (two to a wavefront; us, whole / cut: one token behind 300 keys, 28/4 heads, 7.8 / 9.3, fp32, 6/2, 9.0 / 10.1, 1000 keys 11.4 / 9.3), and parts have 8 tiles at least where
-// those of 4, one to a wavefront, are more than the workgroup slots (4 / 8 at least: one token behind 4097 keys 10.1 / 11.7, 4 behind 2000 9.5 / 11.2, 16 behind 2000
-// 14.0 / 15.2, 30 with a window of 512 12.4 / 14.2; 32 behind up to 1000 15.7 / 15.0, 4 behind 8000 14.8 / 14.3; beyond the slots, 8 behind up to 8000, 32/8, 34.3 / 30.5).
-// In fp32, whose tiles take longer, and beside chunks always 4.
-// Where all tiles see about as many keys (chunks, windows) the workgroup slots' rounds decide: of 1 .. 64 parts those whose rounds, of a part's tiles and those 3
+// Parts.  A part costs what it finds before its first keys and leaves behind its last ones, some 3 key tiles' time, and a join, 3 us and more: tiles of few rows are whole
+// up to 8 key tiles, two to a wavefront (us, whole / cut: one token behind 300 keys, 28/4 heads, 7.8 / 9.3, fp32, 6/2, 9.0 / 10.1; 1000 keys 11.4 / 9.3).  Parts have 4
+// tiles at least, one to a wavefront, or 8 where that makes more parts than there are workgroup slots (4 / 8 at least: one token behind 4097 keys 10.1 / 11.7, 4 behind 2000 9.5 /
+// 11.2, 16 behind 2000 14.0 / 15.2, 30 with a window of 512 12.4 / 14.2; 4 behind 8000 14.8 / 14.3; 8 behind up to 8000, 32/8, 34.3 / 30.5); in fp32, whose tiles take
+// longer, and beside chunks always 4.
+// Where all tiles see about as many keys (chunks, windows) the rounds of the slots decide: of 1 .. 64 parts those whose rounds, of a part's tiles and those 3
 // each, are shortest (1000 rows behind 30000 keys, 28/4: 3 / 5 / 7 parts 565 / 541 / 488 us).
-// Single tokens whose lengths nobody knows here: enough parts for 5 rounds (us, rounds 3 / 4 / 5 / 6 / 8: 64 tokens behind up to 16384 keys, 32/8, 266 / 301 / 262 / 268 / 280; 32 up
-// to 16000 139 / 141 / 132 / 134 / 135; 128 up to 2000 85 / 85 / 73 / 73 / 101; 256 up to 4000, 16/4, D = 64, 127 / 127 / 97 / 97 / 108.  Longer parts first and short ones
-// last, in the order of the parts, gains nothing: the memory's rate, 5.3 TB/s where all sequences are equally long, is all but reached).
+// Single tokens whose lengths nobody knows here: enough parts for 5 rounds (us, rounds 3 / 4 / 5 / 6 / 8: 64 tokens behind up to 16384 keys, 32/8, 266 / 301 / 262 / 268 / 280;
+// 32 up to 16000 139 / 141 / 132 / 134 / 135; 128 up to 2000 85 / 85 / 73 / 73 / 101), in tiles of FEWER rows, of which more run at once, for 8 (5 / 8 / 10 / 12 / 16: 32 up
+// to 16000, 16/4, 46 / 42 / 42 / 42 / 42; 128 up to 2000, 64/8, 62 / 54 / 67 / 67 / 67; 256 up to 4000, 14/2, 52 / 46 / 45 / 57 / 57).  (Longer parts first and short ones last,
+// in the order of the parts, gains nothing: the memory's rate, 5.3 TB/s where all sequences are equally long, is all but reached.)
 // Tokens beside chunks, all cut alike: 5 rounds (us, rounds 3 / 5 / 8: 40 up to 9000 keys beside a chunk of 500, 32/8, 201 / 130 / 138; 100 up to 3000 beside three of 300
-// 151 / 142 / 181; 20 up to 20000 beside 1000, 28/4, 409 / 395 / 424; 30 up to 9000 beside 500, 64/8, 127 / 138 / 193; 60 up to 6000 beside two of 400, 16/4, D = 64, 54 / 74 /
-// 67; with chunks cut a third as often, as in attn_paged_mfma.hip, at 8 rounds 126, 234, 457, 260, 81).
+// 151 / 142 / 181; 20 up to 20000 beside 1000, 28/4, 409 / 395 / 424; 30 up to 9000 beside 500, 64/8, 127 / 138 / 193; with chunks cut a third as often, as in
+// attn_paged_mfma.hip, at 8 rounds 126, 234, 457, 260).
 void cut_paged8_mfma(PagedArgs &a)
 {
     const cf_attn_paged_params &p = a.p;
-    const int64_t capacity = (int64_t)p.pages_per_seq * p.page_size, G = p.n_q_heads / p.n_kv_heads, slots = 512;
-    int64_t keys = p.max_kv_len > 0 ? std::min<int64_t>(p.max_kv_len, capacity) : capacity;
-    int64_t tiles = (keys + BN - 1) / BN;
-    if (p.window > 0) tiles = std::min(tiles, ((int64_t)p.window + BM / G) / BN + 2 + ((int64_t)a.mask.sinks + BN - 1) / BN);
+    const int64_t tiles = key_tiles(p), G = p.n_q_heads / p.n_kv_heads, slots = kSlots;
     const Mode mode = mode_of(p);
-    const int64_t rows = mode == kFew ? few_of(p) : BM, groups = std::max<int64_t>(p.n_seqs, (p.n_tokens * G + rows - 1) / rows) * p.n_kv_heads;      // (tiles that there are at least)
-    const int64_t least = mode == kFew && p.dtype == CF_BF16 && groups * ((tiles + 3) / 4) > slots ? 8 : 4;
-    const int64_t most = mode == kFew && tiles <= 8 ? 1 : std::min<int64_t>((tiles + least - 1) / least, kMostParts);
+    const bool few = mode == kFewer || mode == kFew;
+    const int64_t rows = rows_of(mode), groups = std::max<int64_t>(p.n_seqs, (p.n_tokens * G + rows - 1) / rows) * p.n_kv_heads;      // (tiles that there are at least)
+    const int64_t least = few && p.dtype == CF_BF16 && groups * ((tiles + 3) / 4) > slots ? 8 : 4;
+    const int64_t most = few && tiles <= 8 ? 1 : std::min<int64_t>((tiles + least - 1) / least, kMostParts);
     auto rounds_of = [&](int64_t parts) { return (groups * parts + slots - 1) / slots; };
     int64_t parts = 1;
     if (groups < (mode == kMany ? 1 : 4) * slots) {
-        if (mode == kMany || (mode == kFew && p.window > 0)) {
+        if (mode == kMany || (few && p.window > 0)) {
             auto time = [&](int64_t n) { return rounds_of(n) * ((tiles + n - 1) / n + 3) + (n > 1 ? 3 : 0); };
             for (int64_t n = 2; n <= most; ++n)
                 if (time(n) < time(parts)) parts = n;
         } else {
             const int64_t places = tiles_most(p) * p.n_kv_heads;
-            parts = std::min((5 * slots + places - 1) / places, most);
+            parts = std::min(((mode == kFewer && p.dtype == CF_BF16 ? 8 : 5) * slots + places - 1) / places, most);
         }
     }
     a.parts = (int)std::max<int64_t>(1, parts);
