@@ -660,7 +660,7 @@ Mode mode_of(const cf_attn_paged_params &p)
 {
     const int64_t rows = (int64_t)p.n_tokens * (p.n_q_heads / p.n_kv_heads);
     if (p.dtype == CF_FP32) return kFewer;
-    if (p.head_dim == 64 && rows <= (int64_t)FEWER * p.n_seqs && key_tiles(p) * p.n_seqs * p.n_kv_heads <= 80 * kSlots) return kFewer;
+    if (p.head_dim == 64 && rows <= (int64_t)FEWER * p.n_seqs && key_tiles(p) <= 80 * kSlots / ((int64_t)p.n_seqs * p.n_kv_heads)) return kFewer;
     return rows <= (int64_t)FEW * p.n_seqs ? kFew : p.n_seqs == 1 || rows >= 512 * (int64_t)p.n_seqs ? kMany : kBoth;
 }
 int rows_of(Mode mode) { return mode == kFewer ? FEWER : mode == kFew ? FEW : BM; }
@@ -722,7 +722,7 @@ void cut_paged8_mfma(PagedArgs &a)
     const Mode mode = mode_of(p);
     const bool few = mode == kFewer || mode == kFew;
     const int64_t rows = rows_of(mode), groups = std::max<int64_t>(p.n_seqs, (p.n_tokens * G + rows - 1) / rows) * p.n_kv_heads;      // (tiles that there are at least)
-    const int64_t least = few && p.dtype == CF_BF16 && groups * ((tiles + 3) / 4) > slots ? 8 : 4;
+    const int64_t least = few && p.dtype == CF_BF16 && (tiles + 3) / 4 > slots / groups ? 8 : 4;
     const int64_t most = few && tiles <= 8 ? 1 : std::min<int64_t>((tiles + least - 1) / least, kMostParts);
     auto rounds_of = [&](int64_t parts) { return (groups * parts + slots - 1) / slots; };
     int64_t parts = 1;

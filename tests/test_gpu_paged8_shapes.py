@@ -129,3 +129,25 @@ def test_older_rows_of_a_block_are_as_the_attention_reads_them():
             got = P.values(c[1, :n, 0], s[1, 0, 0])
             want = torch.stack([r[i][0] for r in rows]).double()
             assert bool(((got - want).abs() <= 2 * torch.maximum(2.0 ** -4 * want.abs(), 2.0 ** -10 * s[1, 0, 0].double())).all()), n
+
+
+@pytest.mark.parametrize("page", [16, 32, 64])
+@pytest.mark.parametrize("seqs,Hq,Hkv,columns", [([(1, 900), (1, 40), (3, 3), (2, 500), (0, 7)], 8, 2, 200000),      # (rows of the table for 3 M keys and more)
+                                                 ([(2, 300), (2, 77), (1, 1)], 14, 1, 0), ([(2, 600), (2, 130)], 36, 3, 0)])
+def test_tiles_of_32_rows_at_head_dim_64(seqs, Hq, Hkv, columns, page):
+    """What the host takes for long calls, and sequences of 17 to 32 rows."""
+    b = Batch8(seqs, Hq, Hkv, 64, BF16, page, columns=columns, pad=2, seed=page)
+    for hint in (0, max(n for _, n in seqs)):
+        b.o.fill_(7), b.lse.fill_(7)
+        b.check(b.run(max_kv_len=hint), (page, hint))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("Hkv", [1, 2, 3, 4, 6, 8])
+def test_pairs_of_heads(dtype, Hkv):
+    """Heads one by one and two by two, any number of workgroups; a call with itself again."""
+    for seqs in ([(1, 100)], [(1, 70), (2, 300), (1, 5)], [(1, 40 * n + 1) for n in range(9)], [(40, 90), (1, 1000)]):
+        b = Batch8(seqs, 2 * Hkv, Hkv, 64, dtype, 32, seed=Hkv)
+        got, again = b.run(), b.run()
+        b.check(got, (seqs[:2], Hkv))
+        assert bool(torch.equal(got["o"], again["o"])) and bool(torch.equal(got["lse"], again["lse"]))
