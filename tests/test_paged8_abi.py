@@ -93,9 +93,13 @@ def test_append_rotated_refuses(name, value, code):
 
 @pytest.mark.parametrize("name,value,code", [("a__" + a, b, c) for a, b, c in COMMON] + SCALES + [
     ("a__n_kv_heads", 0, INVALID), ("a__n_kv_heads", 65535, INVALID), ("a__k", None, INVALID), ("a__v", 8, INVALID), ("a__page_stride_head", 136, INVALID),
-    ("a__page_stride_tok", 136, INVALID), ("a__page_stride", 64 * 256 + 8, INVALID), ("a__n_seqs", 1 << 29, INVALID)])
+    ("a__page_stride_tok", 136, INVALID), ("a__page_stride", 64 * 256 + 8, INVALID)])
 def test_append8_refuses(name, value, code):
     refused(code, B.cf_kv_append8, append8(**{name: value}))
+
+
+def test_append8_refuses_more_blocks_than_a_launch_holds():
+    refused(INVALID, B.cf_kv_append8, append8(a__n_tokens=1 << 27, a__n_seqs=1 << 29))      # (either one alone is less)
     assert B.lib().cf_kv_append8(None, None, None) == INVALID
 
 
