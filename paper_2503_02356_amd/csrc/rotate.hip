@@ -12,7 +12,7 @@ namespace cf {
 namespace {
 
 // A lane a unit of a row (rotation.h) of the heads of a group; a group of heads to each blockIdx.y.  The first heads' loads are on their way while the
-// row's sequence is looked for and its sines are taken.
+// row's page is looked up and its sines are taken.
 template <bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(256) void turn_rows_kernel(TurnArgs a)
 {
