@@ -707,7 +707,9 @@ int64_t paged8_mfma_launch_size(const PagedArgs &a) { return tiles_most(a.p) * a
 // 11.2, 16 behind 2000 14.0 / 15.2, 30 with a window of 512 12.4 / 14.2; 4 behind 8000 14.8 / 14.3; 8 behind up to 8000, 32/8, 34.3 / 30.5); in fp32, whose tiles take
 // longer, and beside chunks always 4.
 // Where all tiles see about as many keys (chunks, windows) the rounds of the slots decide: of 1 .. 64 parts those whose rounds, of a part's tiles and those 3
-// each, are shortest (1000 rows behind 30000 keys, 28/4: 3 / 5 / 7 parts 565 / 541 / 488 us).
+// each, are shortest.  Chunks: a key tile takes a workgroup 1.5 us alone on its compute unit, 2.5 beside another (D = 64: 2.3, and 3 beside two), a join 4 us and what its bytes
+// take (us, parts 1 / 2 / 3 / 4 / 8: 512 rows behind 8000 keys, 28/4, 207 / 120 / 114 / 92 / 100, 512 behind none 19 / 24 / 23 / 23 / 23, 1000 behind 1000 55 / 59 / 58 / 63 / 76,
+// 2048 behind 20000 702 / 752 / 723 / 683 / 715, 16/4, D = 64, 512 / 385 / 341 / 348 / 339).
 // Single tokens whose lengths nobody knows here: enough parts for 5 rounds (us, rounds 3 / 4 / 5 / 6 / 8: 64 tokens behind up to 16384 keys, 32/8, 266 / 301 / 262 / 268 / 280;
 // 32 up to 16000 139 / 141 / 132 / 134 / 135; 128 up to 2000 85 / 85 / 73 / 73 / 101), in tiles of FEWER rows, of which more run at once, for 8 (5 / 8 / 10 / 12 / 16: 32 up
 // to 16000, 16/4, 46 / 42 / 42 / 42 / 42; 128 up to 2000, 64/8, 62 / 54 / 67 / 67 / 67; 256 up to 4000, 14/2, 52 / 46 / 45 / 57 / 57).  (Longer parts first and short ones last,
@@ -727,10 +729,20 @@ void cut_paged8_mfma(PagedArgs &a)
     auto rounds_of = [&](int64_t parts) { return (groups * parts + slots - 1) / slots; };
     int64_t parts = 1;
     if (groups < (mode == kMany ? 1 : 4) * slots) {
-        if (mode == kMany || (few && p.window > 0)) {
-            auto time = [&](int64_t n) { return rounds_of(n) * ((tiles + n - 1) / n + 3) + (n > 1 ? 3 : 0); };
+        auto shortest = [&](auto time) {
             for (int64_t n = 2; n <= most; ++n)
                 if (time(n) < time(parts)) parts = n;
+        };
+        if (mode == kMany) {
+            // (quarters of a microsecond)
+            const int64_t per_cu = p.head_dim == 64 ? 3 : 2, tile[] = {0, 6, p.head_dim == 64 ? 9 : 10, 12};
+            shortest([&](int64_t n) {
+                const int64_t all = groups * n, full = all / (256 * per_cu), rest = all % (256 * per_cu);
+                const int64_t join = n == 1 ? 0 : 16 + n * p.n_tokens * p.n_q_heads * p.head_dim * 8 / 1500000;
+                return ((tiles + n - 1) / n + 3) * (full * tile[per_cu] + tile[(rest + 255) / 256]) + join;
+            });
+        } else if (few && p.window > 0) {
+            shortest([&](int64_t n) { return rounds_of(n) * ((tiles + n - 1) / n + 3) + (n > 1 ? 3 : 0); });
         } else {
             const int64_t places = tiles_most(p) * p.n_kv_heads;
             parts = std::min(((mode == kFewer && p.dtype == CF_BF16 ? 8 : 5) * slots + places - 1) / places, most);
