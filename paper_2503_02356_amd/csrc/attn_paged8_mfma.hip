@@ -705,11 +705,13 @@ int64_t paged8_mfma_launch_size(const PagedArgs &a) { return tiles_most(a.p) * a
 // up to 8 key tiles, two to a wavefront (us, whole / cut: one token behind 300 keys, 28/4 heads, 7.8 / 9.3, fp32, 6/2, 9.0 / 10.1; 1000 keys 11.4 / 9.3).  Parts have 4
 // tiles at least, one to a wavefront, or 8 where that makes more parts than there are workgroup slots (4 / 8 at least: one token behind 4097 keys 10.1 / 11.7, 4 behind 2000 9.5 /
 // 11.2, 16 behind 2000 14.0 / 15.2, 30 with a window of 512 12.4 / 14.2; 4 behind 8000 14.8 / 14.3; 8 behind up to 8000, 32/8, 34.3 / 30.5); in fp32, whose tiles take
-// longer, and beside chunks always 4.
-// Where all tiles see about as many keys (chunks, windows) the rounds of the slots decide: of 1 .. 64 parts those whose rounds, of a part's tiles and those 3
-// each, are shortest.  Chunks: a key tile takes a workgroup 1.5 us alone on its compute unit, 2.5 beside another (D = 64: 2.3, and 3 beside two), a join 4 us and what its bytes
-// take (us, parts 1 / 2 / 3 / 4 / 8: 512 rows behind 8000 keys, 28/4, 207 / 120 / 114 / 92 / 100, 512 behind none 19 / 24 / 23 / 23 / 23, 1000 behind 1000 55 / 59 / 58 / 63 / 76,
-// 2048 behind 20000 702 / 752 / 723 / 683 / 715, 16/4, D = 64, 512 / 385 / 341 / 348 / 339).
+// longer, and beside chunks always 4; chunks 2 (four wavefronts have a tile together: 100 rows behind 1000, 28/4, 4 / 2 tiles at least 18.9 / 18.0, 16/4, D = 64, 14.1 / 12.4).
+// Where all tiles see about as many keys (windows) the rounds of the slots decide: of 1 .. 64 parts those whose rounds, of a part's tiles and those 3 each, are shortest.
+// Chunks, and all calls in fp32: the same with what a step, a key tile (of few rows four), takes a workgroup alone on its compute unit and beside others, 1.5 and 2.5 us at D =
+// 128 (1.5, 2.3 and 3 at 64; fp32 2.4 and 3.2, 1.7 to 2.5), and a join 3 us, of many rows 4, and its bytes' time (us, parts 1 / 2 / 3 / 4 / 8: 512 rows behind 8000 keys, 28/4,
+// 207 / 120 / 114 / 92 / 100, behind none 19 / 24 / 23 / 23 / 23, 1000 behind 1000 55 / 59 / 58 / 63 / 76, 2048 behind 20000 702 / 752 / 723 / 683 / 715, 16/4, D = 64, 512 /
+// 385 / 341 / 348 / 339; fp32, 6/2 x 128: 300 behind 5000 59 / 37 / 34 / 30 / 37, 2000 behind none 37 / 55 / 52 / 72 / 102, 64 tokens behind up to 5000 59 / 47 / 37 / 35 / 40,
+// 200 behind up to 600 19 / 27 / 23 / 33 / 34).
 // Single tokens whose lengths nobody knows here: enough parts for 5 rounds (us, rounds 3 / 4 / 5 / 6 / 8: 64 tokens behind up to 16384 keys, 32/8, 266 / 301 / 262 / 268 / 280;
 // 32 up to 16000 139 / 141 / 132 / 134 / 135; 128 up to 2000 85 / 85 / 73 / 73 / 101), in tiles of FEWER rows, of which more run at once, for 8 (5 / 8 / 10 / 12 / 16: 32 up
 // to 16000, 16/4, 46 / 42 / 42 / 42 / 42; 128 up to 2000, 64/8, 62 / 54 / 67 / 67 / 67; 256 up to 4000, 14/2, 52 / 46 / 45 / 57 / 57).  (Longer parts first and short ones last,
@@ -724,7 +726,7 @@ void cut_paged8_mfma(PagedArgs &a)
     const Mode mode = mode_of(p);
     const bool few = mode == kFewer || mode == kFew;
     const int64_t rows = rows_of(mode), groups = std::max<int64_t>(p.n_seqs, (p.n_tokens * G + rows - 1) / rows) * p.n_kv_heads;      // (tiles that there are at least)
-    const int64_t least = few && p.dtype == CF_BF16 && (tiles + 3) / 4 > slots / groups ? 8 : 4;
+    const int64_t least = few && p.dtype == CF_BF16 && (tiles + 3) / 4 > slots / groups ? 8 : mode == kMany ? 2 : 4;
     const int64_t most = few && tiles <= 8 ? 1 : std::min<int64_t>((tiles + least - 1) / least, kMostParts);
     auto rounds_of = [&](int64_t parts) { return (groups * parts + slots - 1) / slots; };
     int64_t parts = 1;
@@ -733,13 +735,16 @@ void cut_paged8_mfma(PagedArgs &a)
             for (int64_t n = 2; n <= most; ++n)
                 if (time(n) < time(parts)) parts = n;
         };
-        if (mode == kMany) {
-            // (quarters of a microsecond)
-            const int64_t per_cu = p.head_dim == 64 ? 3 : 2, tile[] = {0, 6, p.head_dim == 64 ? 9 : 10, 12};
+        if (mode == kMany || p.dtype == CF_FP32) {
+            // Hundredths of a microsecond; t[k]: a step's, of one of k workgroups on a compute unit.
+            constexpr int many64[] = {150, 150, 225, 300}, many128[] = {150, 150, 250}, fp32_64[] = {170, 170, 190, 220, 250}, fp32_128[] = {240, 240, 320};
+            const bool wide = p.head_dim == 128, chunk = mode == kMany;
+            const int *t = chunk ? (wide ? many128 : many64) : wide ? fp32_128 : fp32_64;
+            const int64_t together = 256 * (wide ? 2 : chunk ? 3 : 4), at_once = chunk ? 1 : 4, around = chunk ? 3 : 2;
             shortest([&](int64_t n) {
-                const int64_t all = groups * n, full = all / (256 * per_cu), rest = all % (256 * per_cu);
-                const int64_t join = n == 1 ? 0 : 16 + n * p.n_tokens * p.n_q_heads * p.head_dim * 8 / 1500000;
-                return ((tiles + n - 1) / n + 3) * (full * tile[per_cu] + tile[(rest + 255) / 256]) + join;
+                const int64_t steps = ((tiles + n - 1) / n + at_once - 1) / at_once + around, full = groups * n / together, rest = groups * n % together, k = rest / 256;
+                const int64_t last = rest == 0 ? 0 : chunk ? t[(rest + 255) / 256] : t[k] + (t[k + 1] - t[k]) * (rest % 256) / 256;
+                return steps * (full * t[together / 256] + last) + (n == 1 ? 0 : (chunk ? 400 : 300) + n * p.n_tokens * p.n_q_heads * p.head_dim * 8 / 50000);
             });
         } else if (few && p.window > 0) {
             shortest([&](int64_t n) { return rounds_of(n) * ((tiles + n - 1) / n + 3) + (n > 1 ? 3 : 0); });
