@@ -18,7 +18,7 @@
 // raised priority around the products 3.37, around the conversion 3.24; eight wavefronts of 256 rows 3.38.
 // Few rows: bound by memory.  64 tokens behind up to 16384 keys, 32/8 x 128: 257 us with its join for 1.22 GB (4.7 TB/s; 64 equally long sequences 5.3, a large copy's rate
 // 5.1).  Keys straight into registers 309 (a row's 64 bytes an instruction: twice the requests); 16-row tiles of five wavefronts 1 % slower.  D = 64: 64 tokens
-// behind 16000 keys, 16/4, 108 us (4.9 TB/s; 161 with the heads of a cache line on different XCDs, which fetches each line twice).  One token behind 4097 keys, 28/4: 7.9 us and 4.1 for the join.
+// behind 16000 keys, 16/4, 108 us (4.9 TB/s; 161 with the heads of a cache line on different XCDs, which fetches each line twice).  One token behind 4097 keys, 28/4: 7.1 us and 4 for the join.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -6,7 +6,7 @@
 // heads of the queries (a lane a unit of a row), one behind the other in as many rows of the grid as they fill, then K and V of each head.
 //
 // Bound by memory where a call is large, 2 bytes read and 1 written of each element (and the queries both ways), and by its launch and three trips to memory, one behind
-// the other (lists, table, rows), where it is small.  Measured, us: 8192 tokens of 28 + 4 heads x 128, 26 with their queries (5.5 TB/s: what it reads is partly in the
+// the other (lists, rows and table, the scale that there is), where it is small.  Measured, us: 8192 tokens of 28 + 4 heads x 128, 26 with their queries (5.5 TB/s: what it reads is partly in the
 // caches); one token of each of 256 sequences 5.5.  Queries in fewer workgroups than alone (rotate.hip), 128, since the blocks fill the chip with theirs (128 / 256 /
 // 512: 4000 rows of 28 + 4 heads 13.0 / 13.0 / 15.4, of 16 + 4 x 64 8.4 / 9.2 / 10.9, 256 tokens of 64 + 8 11.3 / 11.6 / 13.2).
 #include <hip/hip_runtime.h>
