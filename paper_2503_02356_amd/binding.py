@@ -4,6 +4,7 @@ PyTorch appears here only as the owner of device memory and streams (data_ptr(),
 There is no CPU fallback: if the library is missing or an entry point fails, the call raises.
 """
 import ctypes as C
+import math
 import os
 
 import numpy as np
@@ -711,6 +712,16 @@ def make_paged8_params(q, k_pages, v_pages, k_scales, v_scales, o, lse, cu_q, kv
     workspace = _paged_workspace(p.a, cf_attn_paged8_workspace_bytes, p, q, workspace)
     p._keepalive = (q, k_pages, v_pages, k_scales, v_scales, o, lse, cu_q, kv_lens, block_table, workspace)      # see make_fwd_params
     return p
+
+
+def paged8_refuses(params):
+    """Whether cf_attn_paged8_fwd refuses the addresses, the strides or the scale of make_paged8_params.  (Sizes have been looked at there; pages, scales
+    and lists are cf_kv_append8's too.)"""
+    a = params.a
+    step = 8 if a.dtype == CF_BF16 else 4
+    strides = (a.q_stride_tok, a.q_stride_head, a.o_stride_tok, a.o_stride_head)
+    return (any(s < a.head_dim or s % step for s in strides) or any(not x or x % 16 for x in (a.q, a.o)) or (a.lse or 0) % 4 != 0 or
+            not math.isfinite(a.softmax_scale))
 
 
 def cf_attn_paged8_workspace_bytes(params):

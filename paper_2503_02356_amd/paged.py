@@ -122,12 +122,12 @@ class PagedCache:
             turn = B.make_append_rotation(self.rotation, q, queries)
         if self.eight_bits:
             assert q.dtype == self.dtype
-            if not abs(scale) < 3.4e38 or (turn is None and (q.data_ptr() % 16 or any(s * q.element_size() % 16 for s in q.stride()[:2]))):
-                # (the append may round older rows again: what the attention would refuse is refused before)
-                raise ValueError("q must be 16-byte aligned, with strides that are, and scale a finite fp32 number")
             cache = (self.k_pages, self.v_pages, self.k_scales, self.v_scales)
             append = B.make_kv_append8_params(k, v, *cache, *where)
             attention = B.make_paged8_params(queries, *cache, o, lse, *where, scale, **how)
+            if B.paged8_refuses(attention):
+                # (the append may round older rows again: what the attention would refuse is refused before)
+                raise ValueError("q and lse must be aligned, with strides of at least head_dim that are, and scale a finite fp32 number")
             B.cf_kv_append8(append, turn)
             B.cf_attn_paged8_fwd(attention)
             return o

@@ -153,3 +153,24 @@ def test_serving_from_8_bits(dtype, D, rotated, window, sinks):
     for name in "abc":
         cache.close(name)
     assert cache.used_pages() == 0
+
+
+def test_a_refused_call_leaves_the_numbers_as_they_were():
+    """Queries whose rows are one row (a stride of 0): refused before anything is appended, since larger rows would have the block's older numbers rounded
+    again.  The same call with rows of their own goes through, and does that."""
+    cache = PagedCache(4, 32, 2, 64, BF16, eight_bits=True)
+    q, k, v = (torch.randn(5, H, 64, device=DEV).to(BF16) for H in (4, 2, 2))
+    cache.attend(["a"], [5], q, k, v)
+    held = lambda: [x.view(torch.uint8).clone() for x in (cache.k_pages, cache.v_pages, cache.k_scales, cache.v_scales)]
+    before, pages, free = held(), list(cache.seqs["a"][1]), list(cache.free)
+    for bad, scale in ((q[:1].expand(3, 4, 64), None), (q[:3, :1].expand(3, 4, 64), None), (q[:3], float("inf"))):
+        with pytest.raises(ValueError):
+            cache.attend(["a"], [3], bad, 100 * k[:3], 100 * v[:3], scale=scale)
+        torch.cuda.synchronize()
+        assert all(bool(torch.equal(x, y)) for x, y in zip(held(), before))
+        assert cache.seqs == {"a": [5, pages]} and cache.free == free
+    cache.attend(["a"], [3], q[:1].expand(3, 4, 64).contiguous(), 100 * k[:3], 100 * v[:3])
+    torch.cuda.synchronize()
+    number = pages[0]
+    assert cache.lengths() == {"a": 8}
+    assert not any(bool(torch.equal(x[number], y[number])) for x, y in zip(held(), before))
