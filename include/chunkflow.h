@@ -439,8 +439,8 @@ int cf_kv_append(const cf_kv_append_params *p, void *hip_stream);
 /*
  * Rotation of queries and keys by their positions.  The elements of a head are taken in rot_dim / 2 pairs, pair i being elements
  * (i, i + rot_dim / 2), or (2 i, 2 i + 1) where interleaved is not 0; those from rot_dim on are in no pair and stay.  At position p pair i = (a, b)
- * becomes (a cos t - b sin t, a sin t + b cos t), t = p * inv_freq[i].  The angle is taken in 64 bits, so that far positions are as exact as near
- * ones, sines and products in fp32; results are rounded once.
+ * becomes (a cos t - b sin t, a sin t + b cos t), t = p * inv_freq[i].  Whole turns leave the angle before anything is rounded to fp32, so that at
+ * any position it is off by 2^-25 of a turn at most (where it is below 2^40 radians); sines and products are in fp32, results are rounded once.
  */
 typedef struct {
     const float *inv_freq;              /* device, [rot_dim/2]: angle of a pair per position, in radians */

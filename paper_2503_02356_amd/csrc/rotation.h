@@ -2,12 +2,13 @@
 //
 // A lane has a unit of a row: 16 elements in two runs of 8, the 8 pairs of which it turns (or that are in no pair).  It takes the sines and
 // cosines of its pairs once and turns its unit of several heads with them; since both elements of a pair are a lane's own, x may be y.
-// The angle p * inv_freq / 2 pi is taken in 64 bits and its whole turns are dropped there: what is left has an error of 2^-25 of a turn
-// (its rounding to fp32) for any position.  (In fp32 an angle of 2^18 radians would be off by 2^-6.)
+// The angle p * inv_freq loses its whole turns in twice 64 bits (angle.h): what is left has an error of 2^-25 of a turn (its rounding to
+// fp32) for any position.  (In fp32 an angle of 2^18 radians would be off by 2^-6.)
 // Bound by memory, one read and one write of every element, where a call is large; by its launch and one trip to memory where it is small.
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include "angle.h"
 #include "pages.h"
 #include "scalar_rows.h"
 
@@ -106,8 +107,7 @@ struct Turn {
         for (int i = 0; i < 8; ++i) f[i] = unit.turned[i / 4] ? inv_freq[unit.first[i / 4] + i % 4] : 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const double turns = (double)f[i] * (double)position * 0.15915494309189533577;
-            sincospif((float)(2.0 * (turns - rint(turns))), &s[i], &c[i]);
+            sincospif(half_turns(f[i], position), &s[i], &c[i]);
             if (back) s[i] = -s[i];
         }
     }

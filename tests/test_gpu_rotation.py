@@ -1,4 +1,6 @@
 """Rotation of a chunk's queries and keys, their gradients, and the append that rotates on the way, against the definition in 64 bits."""
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -228,3 +230,50 @@ def test_a_large_call_does_what_its_segments_calls_do(D, dtype, interleaved):
     torch.cuda.synchronize()
     for x, y in zip(*ys):
         assert bool(torch.equal(x, y)) and bool((x[T:] == 7.0).all())
+
+
+PI = Fraction(3141592653589793238462643383279502884197169399375105820974944592, 10 ** 63)
+
+
+def turned_exactly(x, pos, f, interleaved):
+    """P.turned with whole turns taken from the angles as fractions, and the tolerance of fp32 results: a part of a turn rounded to fp32 (half a step of a number of
+    half-turns, which may lie above 1: pi 2^-24), sine and cosine (2 steps of numbers up to 1: 2^-23), products and their sum (2^-24 each), fp64 besides."""
+    angle = torch.tensor([[float((Fraction(w) * p / PI) % 2) * np.pi for w in f.tolist()] for p in pos.tolist()], dtype=torch.float64, device=DEV)
+    rot = 2 * f.numel()
+    first, second = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    a, b, c, s = x[..., first].double(), x[..., second].double(), torch.cos(angle)[:, None], torch.sin(angle)[:, None]
+    y, tol = x.double(), torch.zeros_like(x, dtype=torch.float64)
+    y[..., first], y[..., second] = a * c - b * s, a * s + b * c
+    w = 3.15 * 2.0 ** -24 + 2.0 ** -23 + 2.0 ** -48
+    for part, size in ((first, (a * c).abs() + (b * s).abs()), (second, (a * s).abs() + (b * c).abs())):
+        tol[..., part] = w * (a.abs() + b.abs()) + 3 * 2.0 ** -24 * size
+    return y, 1.001 * tol
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D,rot", [(64, 64), (128, 64)])
+@pytest.mark.parametrize("segs", [[(3, 2**31 - 1)], [(2, 2**30 + 1), (1, 229377), (1, 1)]])
+def test_far_positions_are_as_exact_as_near_ones(segs, D, rot, interleaved):
+    """Frequencies up to a turn a position and more: no part of the tolerance grows with the position.  And so are the keys and queries of an append."""
+    f = frequencies(rot)
+    f[:6] = torch.tensor([2 * np.pi, np.pi, 1.0, 100.0, -3.0, 1e-30], device=DEV)
+    pos, (cu_q, cu_k), r = positions(segs), lists(segs), B.make_rotation(f, interleaved)
+    x = torch.randn(int(cu_q[-1]), 2, D, device=DEV)
+    y = torch.empty_like(x)
+    B.cf_rotate(B.make_rotate_params(cu_q, cu_k, r, q=(x, y)))
+    torch.cuda.synchronize()
+    want, tol = turned_exactly(x, pos, f, interleaved)
+    close(y, want, tol, (segs, D, interleaved))
+    page, columns = 65536, 2**30 // 65536
+    pos = torch.tensor([2**30 - 3, 2**30 - 2, 2**30 - 1], device=DEV)
+    x = torch.randn(3, 4, D, device=DEV)
+    table = torch.full((1, columns), -1, device=DEV, dtype=torch.int32)
+    table[0, -1] = 0
+    pages, q_out = torch.zeros(2, 1, page, 1, D, device=DEV), torch.empty(3, 2, D, device=DEV)
+    append = B.make_kv_append_params(x[:, 2:3], x[:, 3:], pages[0], pages[1], ints([0, 3]), ints([2**30]), table)
+    B.cf_kv_append_rotated(append, B.make_append_rotation(r, x[:, :2], q_out))
+    torch.cuda.synchronize()
+    for got, of in ((q_out, x[:, :2]), (pages[0, 0, -3:], x[:, 2:3])):
+        want, tol = turned_exactly(of, pos, f, interleaved)
+        close(got, want, tol, (D, interleaved))
+    assert bool(torch.equal(pages[1, 0, -3:], x[:, 3:])) and not bool(pages[:, 0, :-3].any())
