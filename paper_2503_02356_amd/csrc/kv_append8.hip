@@ -9,6 +9,9 @@
 // the other (lists, rows and table, the scale that there is), where it is small.  Measured, us: 8192 tokens of 28 + 4 heads x 128, 26 with their queries (5.5 TB/s: what it reads is partly in the
 // caches); one token of each of 256 sequences 5.5.  Queries in fewer workgroups than alone (rotate.hip), 128, since the blocks fill the chip with theirs (128 / 256 /
 // 512: 4000 rows of 28 + 4 heads 13.0 / 13.0 / 15.4, of 16 + 4 x 64 8.4 / 9.2 / 10.9, 256 tokens of 64 + 8 11.3 / 11.6 / 13.2).
+// All places of a head one behind the other.  All heads of a place beside each other, which touches a page once, gains 2 - 8 % in prompts whose inputs are in the caches and
+// loses elsewhere (us, places / heads beside each other, heads x 128, three sets of inputs in turn: 1200 tokens of as many sequences, 28 + 4 13.7 / 16.7, 2048 of 28 + 4 20.6 / 25.4, 16000 rows of 28 + 4
+// 59.6 / 60.9, of 8 + 8 40.2 / 44.9, 4000 of 64 + 8 33.7 / 34.4, 16000 keys and values of 8 heads alone 20.3 / 20.1; one set, in the caches, 16000 of 28 + 4 47.2 / 44.1).
 #include <hip/hip_runtime.h>
 
 #include "kv_append.h"
@@ -27,7 +30,6 @@ struct Append8Args {
     float *k_scales, *v_scales;
     int64_t scale_page, scale_head;
     int row_blocks, query_rows;          // workgroups of rows of queries; of the grid's y, those that they fill
-    int heads_first;                     // all heads of four blocks' places one behind the other, not all places of a head
 };
 
 // Four elements times `factor`, as numbers.
@@ -138,12 +140,7 @@ __global__ __launch_bounds__(256) void append8_kernel(Append8Args a)
         if ((int)group < a.turn.t[0].groups) turn_rows<INTERLEAVED, STREAM>(a.turn, end, (int)group, (int)(id - group * (unsigned)a.row_blocks));
         return;
     }
-    int which = blockIdx.y - a.query_rows, four = blockIdx.x;
-    if (a.heads_first) {
-        const unsigned id = (unsigned)which * gridDim.x + blockIdx.x, heads = gridDim.y - a.query_rows;
-        four = (int)(id / heads), which = (int)(id - (unsigned)four * heads);
-    }
-    const int place = four * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int which = blockIdx.y - a.query_rows, place = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const BlockPlaces places(a.turn.n_tokens, a.turn.n_seqs);
     if (place < (int)places.all(end, a.turn.n_seqs)) add_to_block<T, D, INTERLEAVED>(a, places, end, place, which & 1, which >> 1);
 }
@@ -189,9 +186,6 @@ extern "C" int cf_kv_append8(const cf_kv_append8_params *p8, const cf_append_rot
     const int64_t y = (int64_t)a.query_rows + 2 * p->n_kv_heads;
     if (y > 65535 || y * blocks > 0x7fffffffLL) return cf::fail(CF_EINVAL, "%s: %lld rows of workgroups are more than one launch holds", who, (long long)y);
     const dim3 grid((unsigned)blocks, (unsigned)y);
-    // us, places / heads first: 16000 rows of 28 + 4 heads x 128 46.5 / 43.7, 4000 of 64 + 8 28.2 / 25.8; of 16 + 4 x 64 16000 20.4 / 22.8, 256 tokens 5.5 / 6.5,
-    // of 64 + 8 x 128 7.5 / 10.3.
-    a.heads_first = a.turn.stream && p->head_dim == 128;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     if (p->dtype == CF_FP32) p->head_dim == 64 ? cf::launch<float, 64>(a, grid, s) : cf::launch<float, 128>(a, grid, s);
     else p->head_dim == 64 ? cf::launch<unsigned short, 64>(a, grid, s) : cf::launch<unsigned short, 128>(a, grid, s);
