@@ -518,7 +518,8 @@ int cf_kv_append8(const cf_kv_append8_params *p, const cf_append_rotation *r, vo
 /*
  * cf_attn_paged_fwd over a cache of 8 bits: the same mask, pages, lengths, workspace (cf_attn_paged8_workspace_bytes), results and errors, with keys
  * and values that are number * scale.  a.dtype is that of q and o; a's pages are bytes, a.page_stride, a.kv_stride_tok and a.kv_stride_head multiples of
- * 16, at least head_dim.  The numbers enter the products as they are, with the precision that those of a cache of a.dtype have.
+ * 16, at least head_dim.  The numbers enter the products as they are.  Probabilities keep 16 bits in them and more, as over a cache of a.dtype, but in bf16 at
+ * head_dim 128: there more than 32 rows that share keys (a sequence's new tokens, each times the query heads of a key/value head) have them rounded to bf16, as in cf_attn_fwd.
  */
 typedef struct {
     cf_attn_paged_params a;

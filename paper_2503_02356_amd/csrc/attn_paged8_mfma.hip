@@ -10,13 +10,19 @@
 // fp32: queries and P enter as three bf16 operands each, which make up all 24 bits of them; tiles of 16 rows, all of them few.
 // (Products of bytes would take half the instructions, but queries would have to be bytes too, and the sums of the scaled 16x16x128 one are off by up to 6e-5 of
 // the sum of their sizes: too much for scores, whose error is lse's.)
+// P's sum is taken in fp32.  Into the second product P goes, in bf16, as over a cache of bf16 (attn_paged_mfma.hip):
+//   few rows              two operands, the second one the rounding of what the first one's leaves (2^-16 of the value is left over).  64 tokens behind up to 16384 keys,
+//                         32/8 x 128, 260.2 us and an error of o against 64 bits of 1.63e-3, which is o's own rounding; with one operand 259.7 and 1.75e-3
+//   many rows, D = 64     two.  2048 rows behind 20000 keys, 16/4, 341 us and 1.58e-3; one 242 and 1.72e-3
+//   many rows, D = 128    one: half a step, 2^-8 of the value, as o itself is rounded.  8192 rows behind 24576 keys, 28/4, 3.25 ms and 1.92e-3; two 4.37 and
+//                         1.61e-3; 512 behind 8000 92 us and 1.82e-3; two 116 and 1.65e-3
 //
 // Many rows: bound by the matrix instructions and the vector ones between them (a wavefront's key tile takes 257 vector instructions, 224 of them the bf16
-// kernel's, and 64 products).  8192 rows behind 24576 keys, 28/4 heads x 128: 3.22 ms, 1047 TFLOP/s (the bf16 kernel over a cache of twice the bytes 2.88 ms; a large
+// kernel's, and 64 products).  8192 rows behind 24576 keys, 28/4 heads x 128: 3.25 ms, 1038 TFLOP/s (the bf16 kernel over a cache of twice the bytes 2.88 ms; a large
 // matrix product 1234).  Steps there, ms: LDS writes spread over the banks 4.14 -> 3.50; lane addresses instead of descriptors, which with the tile's scalars were
 // more than the scalar registers, 3.50 -> 3.23; the conversion in front of the scores 3.23, between scores and values 3.56, behind the values 3.32;
 // raised priority around the products 3.37, around the conversion 3.24; eight wavefronts of 256 rows 3.38.
-// Few rows: bound by memory.  64 tokens behind up to 16384 keys, 32/8 x 128: 257 us with its join for 1.22 GB (4.7 TB/s; 64 equally long sequences 5.3, a large copy's rate
+// Few rows: bound by memory.  64 tokens behind up to 16384 keys, 32/8 x 128: 260 us with its join for 1.22 GB (4.7 TB/s; 64 equally long sequences 5.3, a large copy's rate
 // 5.1).  Keys straight into registers 309 (a row's 64 bytes an instruction: twice the requests); 16-row tiles of five wavefronts 1 % slower.  D = 64: 64 tokens
 // behind 16000 keys, 16/4, 108 us (4.9 TB/s; 161 with the heads of a cache line on different XCDs, which fetches each line twice).  One token behind 4097 keys, 28/4: 7.1 us and 4 for the join.
 #include <hip/hip_runtime.h>
@@ -251,7 +257,7 @@ struct Rows8 {
 
 // Few rows: all of them in every wavefront, which has key tiles of its own.
 // GROUPS: of a key tile, each in one page: 1 where a page holds 64 keys or more, 2 of 32, 4 of 16.  (256 tokens with a window of 1024 in pages of 32, 16/4 heads x 64,
-// with their append: 59.5 us with 4, 56.5 with 2.)
+// with their append: 40.3 us with 4, 39.6 with 2.)
 template <typename T, int D, int QB, int GROUPS>
 __device__ __forceinline__ void few_rows8(const Paged8Args &c, const TileRows &t, const KeyTiles<BN, WindowMask> &tiles, int first, int end, int keys, int part,
                                           char *k_stage, char *v_stage)
@@ -644,7 +650,7 @@ __global__ __launch_bounds__(256, D == 64 && MODE == kFewer ? 4 : 2) void mfma_p
     }
 }
 
-constexpr int64_t kSlots = 512;              // workgroups that run at once, two to a compute unit
+constexpr int64_t kSlots = 512;              // workgroups that run at once, two to a compute unit (of FEWER rows at D = 64 four; see cut_paged8_mfma)
 // Key tiles that a tile of rows sees at most, as far as the host knows.
 int64_t key_tiles(const cf_attn_paged_params &p)
 {
@@ -707,6 +713,9 @@ int64_t paged8_mfma_launch_size(const PagedArgs &a) { return tiles_most(a.p) * a
 // 11.2, 16 behind 2000 14.0 / 15.2, 30 with a window of 512 12.4 / 14.2; 4 behind 8000 14.8 / 14.3; 8 behind up to 8000, 32/8, 34.3 / 30.5); in fp32, whose tiles take
 // longer, and beside chunks always 4; chunks 2 (four wavefronts have a tile together: 100 rows behind 1000, 28/4, 4 / 2 tiles at least 18.9 / 18.0, 16/4, D = 64, 14.1 / 12.4).
 // Where all tiles see about as many keys (windows) the rounds of the slots decide: of 1 .. 64 parts those whose rounds, of a part's tiles and those 3 each, are shortest.
+// (Two workgroups a compute unit are counted there also in tiles of FEWER rows at D = 64, of which four have room: what the others take of the memory's rate and a join cost more than
+// the room gives, but for the longest windows.  us, for 512 / 1024 slots: 128 tokens of 16/4 with a window of 512 12.4 / 17.5, of 1024 17.9 / 21.4, of 2048 38.4 / 38.0, of 4096 70.5 / 62.7; 64
+// of 64/8, 1024 to 4096, 16.5 / 22.7, 33.6 / 42.6, 60.6 / 73.9; 256 of 14/2 17.5 / 22.8, 37.2 / 40.6, 67.4 / 65.8; 32 of 32/8 15.4 / 15.6, 21.0 / 20.7, 45.7 / 38.0.)
 // Chunks, and all calls in fp32: the same with what a step, a key tile (of few rows four), takes a workgroup alone on its compute unit and beside others, 1.5 and 2.5 us at D =
 // 128 (1.5, 2.3 and 3 at 64; fp32 2.4 and 3.2, 1.7 to 2.5), and a join 3 us, of many rows 4, and its bytes' time (us, parts 1 / 2 / 3 / 4 / 8: 512 rows behind 8000 keys, 28/4,
 // 207 / 120 / 114 / 92 / 100, behind none 19 / 24 / 23 / 23 / 23, 1000 behind 1000 55 / 59 / 58 / 63 / 76, 2048 behind 20000 702 / 752 / 723 / 683 / 715, 16/4, D = 64, 512 /

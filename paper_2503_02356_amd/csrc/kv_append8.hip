@@ -6,9 +6,9 @@
 // heads of the queries (a lane a unit of a row), one behind the other in as many rows of the grid as they fill, then K and V of each head.
 //
 // Bound by memory where a call is large, 2 bytes read and 1 written of each element (and the queries both ways), and by its launch and three trips to memory, one behind
-// the other (lists, rows and table, the scale that there is), where it is small.  Measured, us: 8192 tokens of 28 + 4 heads x 128, 26 with their queries (5.5 TB/s: what it reads is partly in the
-// caches); one token of each of 256 sequences 5.5.  Queries in fewer workgroups than alone (rotate.hip), 128, since the blocks fill the chip with theirs (128 / 256 /
-// 512: 4000 rows of 28 + 4 heads 13.0 / 13.0 / 15.4, of 16 + 4 x 64 8.4 / 9.2 / 10.9, 256 tokens of 64 + 8 11.3 / 11.6 / 13.2).
+// the other (lists, rows and table, the scale that there is), where it is small.  Measured, us: 8192 tokens of 28 + 4 heads x 128, 28.4 with their queries (5.0 TB/s; what it reads is partly in the
+// caches); one token of each of 256 sequences 5.6.  Queries in fewer workgroups than alone (rotate.hip), 128, since the blocks fill the chip with theirs (128 / 256 /
+// 512: 4000 rows of 28 + 4 heads 14.2 / 13.8 / 15.6, of 16 + 4 x 64 7.9 / 8.9 / 10.0, 256 tokens of 64 + 8 7.9 / 9.4 / 10.1).
 // All places of a head one behind the other.  All heads of a place beside each other, which touches a page once, gains 2 - 8 % in prompts whose inputs are in the caches and
 // loses elsewhere (us, places / heads beside each other, heads x 128, three sets of inputs in turn: 1200 tokens of as many sequences, 28 + 4 13.7 / 16.7, 2048 of 28 + 4 20.6 / 25.4, 16000 rows of 28 + 4
 // 59.6 / 60.9, of 8 + 8 40.2 / 44.9, 4000 of 64 + 8 33.7 / 34.4, 16000 keys and values of 8 heads alone 20.3 / 20.1; one set, in the caches, 16000 of 28 + 4 47.2 / 44.1).

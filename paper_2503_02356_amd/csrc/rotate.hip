@@ -1,7 +1,7 @@
 // Rotation of a training chunk's queries and keys and of their gradients, and the append to a paged cache that rotates on the way.
 //
 // One launch for all tensors of a call.  Measured, us: 64 + 8 heads x 128 of 32768 rows in bf16, there and back, 526, which is
-// 92 % of the rate of a large copy (5.1 TB/s); 28 + 4 heads of 8192 packed rows there and back 58 (93 %); one token into pages 4.3, 7.8 with its launch.
+// 92 % of the rate of a large copy (5.1 TB/s); 28 + 4 heads of 8192 packed rows there and back 58 (93 %); one token into pages 4.7, 5.5 with its launch.
 #include <hip/hip_runtime.h>
 
 #include "kv_append.h"
@@ -103,9 +103,9 @@ void pages_of(TurnArgs &a, const cf_kv_append_params *p)
 
 // Heads of a group: the more, the fewer sines (one set a unit and group); the fewer, the more workgroups.  So many that `workgroups` are left, 16 at most, one
 // in small calls (a trip to memory each, all at once).  us, 256 / 512 / 1024 / 2048 workgroups, 28 + 4 heads x 128 in bf16: 2000 rows there and back
-// 17.1 / 15.9 / 22.9 / 22.8, 4000 rows 27.4 / 25.9 / 28.5 / 40.2, 2000 rows into pages 8.9 / 8.2 / 9.1 / 11.6; less than 1 % apart from 8192 rows there and back on.
-// Stores go past the caches from 1024 blocks of rows and heads on (in the caches / past them: 2000 rows there and back 18.9 / 15.9, 4000 34.9 / 25.9, 8192 rows
-// into pages 33.9 / 23.9; 250 rows 14.5 / 14.5: small results stay where the next call finds them).
+// 16.9 / 15.6 / 21.9 / 21.9, 4000 rows 26.9 / 25.3 / 27.8 / 38.1, 2000 rows into pages 8.9 / 8.2 / 9.1 / 11.6; less than 1 % apart from 8192 rows there and back on.
+// Stores go past the caches from 1024 blocks of rows and heads on (in the caches / past them: 2000 rows there and back 18.7 / 15.6, 4000 34.1 / 25.3, 8192 rows
+// into pages 33.8 / 23.9; 250 rows 9.8 / 9.8: small results stay where the next call finds them).
 void TurnArgs::group(int workgroups)
 {
     int heads = 0;

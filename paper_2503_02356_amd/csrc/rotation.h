@@ -149,7 +149,7 @@ struct TurnTensor {
 template <typename In, typename Out, bool INTERLEAVED, bool STREAM, typename Place, typename Angles>
 __device__ __forceinline__ void turn_heads(const TurnTensor &t, const Unit &unit, int64_t row, int h0, int h1, Place place, Angles angles)
 {
-    constexpr int AT_ONCE = 4;                       // (us, 2 / 4 / 8: 32768 rows of 64 + 8 heads there and back 549 / 537 / 553, one token into pages 8.5 / 7.6 / 10.1)
+    constexpr int AT_ONCE = 4;                       // (us, 2 / 4 / 8: 32768 rows of 64 + 8 heads there and back 530 / 527 / 531, 8192 of 28 + 4 60.5 / 58.1 / 60.8; one token into pages 5.3 each)
     const In *x = (const In *)t.x + row * t.x_tok;
     const bool turned = t.turned && unit.any();
     if (!turned && t.x == t.y) return;               // in place
