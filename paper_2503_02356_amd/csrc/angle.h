@@ -5,8 +5,8 @@
 namespace cf {
 
 // position * frequency (radians) in half-turns, -1 .. 1 but for a rounding, off by 2^-24 of one, its rounding to fp32, whatever the position, where the angle is below
-// 2^40 radians.  The product has 55 bits and 1 / 2 pi more than any type, so both are taken as a double and what that leaves: with the double alone the error is
-// 4 * 2^-53 of the angle, 2^-21 of a half-turn at 2^31 turns.  (The whole turns' subtraction is exact.)
+// 2^40 radians.  The product has 55 bits and 1 / 2 pi more than any type, so both are taken as a double and what that leaves: with the double alone the error
+// grows with the angle, to 2^-21 of a half-turn at 2^30 turns.  (The whole turns' subtraction is exact.)
 // Infinities and NaNs become NaN.
 CF_BOTH float half_turns(float frequency, int position)
 {
